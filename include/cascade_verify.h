@@ -12,6 +12,9 @@
  * and, between two steps, kv_commit appends the keys / values of the tokens that were kept to the
  * prefix cache.
  *
+ * Around the step: paged_slots, paged_append and paged_attn keep the prefixes of many requests in pages (prompts, single tokens,
+ * drafted trees), sample_tokens draws tokens from rows of logits.
+ *
  * General conventions
  * -------------------
  *  - C99, no C++ types.  Every pointer inside an args struct is a DEVICE pointer unless its
@@ -24,8 +27,8 @@
  *    The calls of a context share its workspace and are ordered by its stream.  Replays of graphs captured
  *    from it: tree_verify_attn (keys in parts) and lmhead_softmax_cfg (packed or mixed rows) use that
  *    workspace, so replays that hold them have to be ordered with each other and with further such calls.
- *    Captured cascade_accept, select_path, kv_commit and convergence_weights use none of it: their replays
- *    may overlap with each other and with anything else.
+ *    Captured cascade_accept, select_path, kv_commit, convergence_weights, paged_slots, paged_append, paged_attn and sample_tokens
+ *    use none of it: their replays may overlap with each other and with anything else.
  *  - Errors: 0 = CASCADE_OK, negative = cascade_status.  Errors detectable from host-visible
  *    arguments (null pointers, shapes, limits, dtype) are reported before anything is enqueued and
  *    leave outputs untouched.  HIP runtime failures give CASCADE_EHIP.  Preconditions on device
@@ -97,8 +100,8 @@ const char* cascade_strerror(int status);
  * sized for - tree_attn_args.max_nodes_per_tree, cascade_limits.max_nodes_per_tree - whose nodes are
  * then not verified: bf16 attention rows of such a tree are written as zeros with lse = -inf (the f32
  * path has no such bound), acceptance scalars beyond the bound as zeros, the walk sees only the nodes
- * inside the bound; a kv_commit row without room or with a path entry outside its tree), and clears
- * the flag. */
+ * inside the bound; a kv_commit row without room or with a path entry outside its tree; what paged_slots, paged_append and
+ * paged_attn say of themselves), and clears the flag. */
 int cascade_device_status(cascade_ctx* ctx);
 /* Bytes of device workspace the ctx holds (HOST query). */
 int64_t cascade_workspace_bytes(const cascade_ctx* ctx);
@@ -118,7 +121,12 @@ typedef enum {
   CASCADE_K_COMMIT = 6,      /* kv_commit */
   CASCADE_K_WEIGHTS = 7,     /* convergence_weights */
   CASCADE_K_PACK = 8,        /* hidden-state repacking in front of the packed projection */
-  CASCADE_K_COUNT = 9
+  CASCADE_K_SLOTS = 9,       /* paged_slots */
+  CASCADE_K_APPEND = 10,     /* paged_append */
+  CASCADE_K_PAGED_ATTN = 11, /* paged_attn main kernel */
+  CASCADE_K_PAGED_MERGE = 12, /* its merge of keys in parts */
+  CASCADE_K_SAMPLE = 13,     /* sample_tokens */
+  CASCADE_K_COUNT = 14
 } cascade_kernel_id;
 int cascade_set_kernel_timing(cascade_ctx* ctx, int enable);
 int cascade_read_kernel_timing(cascade_ctx* ctx, int kernel_id, double* total_ms, int32_t* launches);
@@ -399,6 +407,158 @@ typedef struct {
   float* cos_next;            /* nullable */
 } conv_weight_args;
 int convergence_weights(cascade_ctx* ctx, const conv_weight_args* args);
+
+/* ---------------------------------------------------------------------------------------------
+ * A cache in pages.  paged_slots gives pages to rows (requests) that grow and says where their new tokens go, paged_append
+ * copies the tokens' keys and values there, paged_attn is the attention of new tokens over such a cache.  A row's new tokens are
+ * a chain (a prompt, a chunk of one, a single token) or, for paged_attn, a drafted tree; after select_path, paged_slots and
+ * paged_append commit the accepted path to the pages as kv_commit does to a contiguous cache.
+ *
+ * Layouts (element type = dtype; strides in ELEMENTS):
+ *     k_pages, v_pages   a pool of n_pages pages of page_size positions; element (page, kvh, x, d) at page*stride_page +
+ *                        kvh*stride_head + x*stride_pos + d (paged_append: + layer*stride_layer), any order of pages, heads and
+ *                        positions.  page_size: a multiple of 16, at most CASCADE_MAX_PAGE; n_pages * page_size <= 2^31 - 1
+ *     block_table        [n_rows, table_width] int32, rows table_stride apart: position x of row s lies in page
+ *                        block_table[s, x / page_size], at x % page_size in it.  Pages of a row's own; what stands behind the
+ *                        pages that hold its positions is not read
+ *     slot               page * page_size + x % page_size
+ */
+#define CASCADE_MAX_PAGE 1024
+
+/* paged_slots — for row s with L = seq_len[s] positions in the cache and n = new_len[s] tokens to add:
+ *     q_off        [n_rows+1]: where each row's new tokens begin in packed arrays, and their number
+ *     position     [max_tokens]: L, L + 1, ... L + n - 1 for the row's tokens; may be NULL
+ *     slot_map     [max_tokens]: their slots
+ *     block_table  gets the pages that positions L .. L + n - 1 need and the row does not hold (it holds those of positions
+ *                  0 .. L - 1); they are taken from the end of free_pages [free_capacity], of which the first free_count[0] are free
+ *     seq_len_out  [n_rows]: L + n;  free_count_out [1]: what is left (neither may alias its input)
+ * Rows are served in order.  A row without room - pages left, table_width, max_tokens - gets none: nothing of its table is
+ * written, its slots are -1, seq_len_out is L, and the flag that cascade_device_status reports is set; where pages have run out,
+ * every later row that needs one goes without, and rows that need none go on.  q_off counts its tokens all the same (up to max_tokens).
+ * Places of slot_map, position and source behind the last token are -1.
+ *
+ * new_len == NULL: the rows keep what select_path accepted, n = 1 + accept_len[row_prompt[s]] (the root, then the path), and
+ * source [max_tokens] receives each token's packed node node_off[s] + node; an entry outside the row's tree gets slot and source -1
+ * and the flag.  Otherwise source (may be NULL) is the token's own index.
+ */
+typedef struct {
+  int32_t n_rows, page_size, n_pages, table_width;
+  int64_t table_stride;
+  int32_t max_tokens;           /* HOST: entries of slot_map, position and source */
+  int32_t free_capacity;        /* HOST: entries of free_pages */
+  const int32_t* seq_len;       /* [n_rows] */
+  const int32_t* new_len;       /* [n_rows]; NULL: from select_path's results below */
+  const int32_t* node_off;      /* [n_rows+1] row packing as in tree_verify_attn; these five only if new_len is NULL */
+  const int32_t* row_prompt;    /* [n_rows] */
+  const int32_t* accept_len;    /* [n_prompts] */
+  const int32_t* path_nodes;    /* [n_prompts, max_depth] */
+  int32_t n_prompts, max_depth, n_nodes_total;
+  int32_t* block_table;
+  const int32_t* free_pages;
+  const int32_t* free_count;    /* [1] */
+  int32_t* free_count_out;      /* [1] */
+  int32_t* q_off;               /* [n_rows+1] */
+  int32_t* slot_map;            /* [max_tokens] */
+  int32_t* position;            /* [max_tokens], nullable */
+  int32_t* source;              /* [max_tokens], nullable with new_len */
+  int32_t* seq_len_out;         /* [n_rows] */
+} paged_slots_args;
+int paged_slots(cascade_ctx* ctx, const paged_slots_args* args);
+
+/* paged_append — for every layer, token t of n_tokens and kv head, keys and values bit for bit:
+ *     pool[layer, slot / page_size, kvh, slot % page_size, :] = new[layer, source[t], kvh, :],  slot = slot_map[t]
+ * Tokens with slot -1 are skipped; slots or sources that are outside the pool or the packed tokens are too, and set the flag.
+ * Slots are expected to differ: of two tokens with one slot, either's pieces of 16 bytes may stay.
+ *     k_new, v_new   [n_layers, n_source, n_kv_heads, head_dim] dtype, contiguous
+ *     head_dim and all strides multiples of 16 bytes, buffers on 16-byte boundaries
+ */
+typedef struct {
+  cascade_dtype dtype;
+  int32_t n_layers, n_tokens, n_source, n_kv_heads, head_dim;
+  const int32_t* slot_map;      /* [n_tokens] */
+  const int32_t* source;        /* [n_tokens]; NULL: token t itself (n_source >= n_tokens) */
+  const void *k_new, *v_new;
+  void *k_pages, *v_pages;
+  int64_t stride_layer, stride_page, stride_head, stride_pos;
+  int32_t n_pages, page_size;
+} paged_append_args;
+int paged_append(cascade_ctx* ctx, const paged_append_args* args);
+
+/* paged_attn — token i of row s, at position x(i), query head g (kv head g / (n_heads / n_kv_heads)), attends
+ *     the positions y of 0 .. prefix_len[s] - 1, through the table, and those of the row's new tokens that are on its path:
+ *       parent NULL: tokens 0 .. i (a chain), x(i) = prefix_len[s] + i
+ *       otherwise:   its ancestors and itself, as in tree_verify_attn; x(i) = prefix_len[s] + its depth
+ *     with window > 0 only those with  x(i) - y < window  or  y < n_sink
+ *     out = sum softmax(scale * <q, k>) v,   lse = log-sum-exp of the scaled scores
+ * The row's new tokens are read from k_new, v_new, so appending them may come before or after.  Pages none of whose positions a
+ * token of the row attends (a window has passed them) are not read, nor are their entries in the table.
+ *     q        element (t, g, d) at t*q_stride + g*head_dim + d;  k_new, v_new at t*kv_stride + kvh*head_dim + d
+ *     out      [n_tokens, n_heads, head_dim] contiguous, dtype;  lse [n_tokens, n_heads] float32, may be NULL
+ * Accumulation and softmax are float32.  Keys and values that a token does not attend, infinities and NaN among them, do not reach
+ * its output.  Tokens behind q_off[n_rows] are not written.  A row whose q_off is not in order or in n_tokens, that has more than
+ * max_new tokens, or whose prefix is negative or longer than max_prefix_len or its table, gets zeros and lse = -inf and sets the flag; an
+ * entry of the table outside the pool sets it too, and what the tokens that need it get is then not defined (the pool's first page is read).
+ * bf16: head_dim 64 or 128; strides multiples of 8 elements, buffers on 16-byte boundaries.  f32: any head_dim up to 256.
+ *
+ * Keys may be cut into parts whose results are joined by a second kernel.  Those partial results lie in `workspace` if it is given,
+ * else in the context's.  A call that is recorded into a graph without a workspace of its own takes its keys whole, so
+ * that its replays may overlap with anything; with one they may overlap with whatever does not use that one.
+ * paged_attn_workspace: the bytes (HOST) with which no cut of a call with these arguments has to be given up.
+ */
+typedef struct {
+  cascade_dtype dtype;
+  int32_t n_rows;
+  const int32_t* q_off;         /* [n_rows+1] */
+  const int32_t* parent;        /* [n_tokens] local indices; NULL: chains */
+  const int32_t* prefix_len;    /* [n_rows] */
+  int32_t n_tokens;             /* HOST: tokens that q, k_new, v_new and out hold */
+  int32_t max_new;              /* HOST upper bound on any row's tokens (trees: at most CASCADE_MAX_TREE) */
+  int32_t max_prefix_len;       /* HOST upper bound on any prefix_len[s] */
+  int32_t n_heads, n_kv_heads, head_dim;
+  float scale;                  /* 0 => 1/sqrt(head_dim) */
+  int32_t window, n_sink;       /* 0: no window; n_sink counts only with one */
+  const void *q, *k_new, *v_new;
+  int64_t q_stride, kv_stride;
+  const void *k_pages, *v_pages;  /* nullable with max_prefix_len 0, as block_table */
+  int64_t stride_page, stride_head, stride_pos;
+  int32_t n_pages, page_size;
+  const int32_t* block_table;
+  int64_t table_stride;
+  int32_t table_width;
+  void* out;
+  float* lse;                   /* nullable */
+  void* workspace;              /* nullable; 16-byte boundary */
+  int64_t workspace_bytes;
+} paged_attn_args;
+int paged_attn(cascade_ctx* ctx, const paged_attn_args* args);
+int paged_attn_workspace(const cascade_ctx* ctx, const paged_attn_args* args, int64_t* bytes);
+
+/* ---------------------------------------------------------------------------------------------
+ * sample_tokens — a token from each row of logits, with the row's own parameters and uniform (plain decoding; the tokens of a
+ * drafted tree, whose probabilities select_path asks for).  With m the row's maximum and T its temperature, w_v = exp((l_v - m) / T):
+ *     kept:   l_v >= the top_k-th largest entry (as in lmhead_softmax_cfg: ties with it stay);
+ *             of those, l_v >= the largest t for which the entries with l_v >= t hold top_p of their mass (ties stay);
+ *             of those, w_v >= min_p
+ *     token = the smallest v for which the kept mass of entries 0 .. v exceeds u times the kept mass;  prob = w_token / the kept mass
+ * T <= 0 or NaN: greedy, the first of the largest entries, prob 1.  top_k <= 0 or >= vocab, top_p >= 1 or NaN, min_p <= 0 or NaN: no
+ * such cut; top_p <= 0, min_p >= 1: the largest entries alone.  NaN among the logits is never drawn; entries at +infinity share the mass; a row
+ * without any entry above -infinity gives token -1, prob 0.  u is expected in [0, 1); beyond it the first or the last kept entry is taken.
+ * Weights and sums are held in 64 bits.
+ *     logits [n_rows, vocab] dtype, rows row_stride ELEMENTS apart;  temperature, top_p, min_p, u [n_rows] float32, top_k [n_rows]
+ */
+typedef struct {
+  cascade_dtype dtype;
+  int32_t n_rows, vocab;
+  const void* logits;
+  int64_t row_stride;
+  const float* temperature;     /* nullable => 1 */
+  const int32_t* top_k;         /* nullable => no cut, like the next two */
+  const float *top_p, *min_p;
+  const float* u;
+  int32_t* token;               /* [n_rows] */
+  float* prob;                  /* [n_rows], nullable */
+} sample_args;
+int sample_tokens(cascade_ctx* ctx, const sample_args* args);
 
 #ifdef __cplusplus
 }

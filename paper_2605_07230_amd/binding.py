@@ -21,6 +21,7 @@ F32, BF16 = 0, 1
 WALK_SEQUENTIAL, WALK_LONGEST = 0, 1
 FEATURES_HIDDEN, FEATURES_LOGITS = 0, 1
 K_ATTN, K_ATTN_MERGE, K_LMHEAD, K_ROW_STATS, K_ACCEPT, K_SELECT = range(6)
+K_SLOTS, K_APPEND, K_PAGED_ATTN, K_PAGED_MERGE, K_SAMPLE = range(9, 14)
 W_ROWMAJOR, W_PACKED32 = 0, 1
 CFG_MIX_LOGITS, CFG_MIX_HIDDEN = 0, 1
 OK, EINVAL, ESHAPE, EDTYPE, ENOMEM, EHIP, ETREE = 0, -1, -2, -3, -4, -5, -6
@@ -28,7 +29,8 @@ OK, EINVAL, ESHAPE, EDTYPE, ENOMEM, EHIP, ETREE = 0, -1, -2, -3, -4, -5, -6
 EXPORTS = ["cascade_create", "cascade_destroy", "cascade_strerror", "cascade_device_status", "cascade_workspace_bytes",
            "cascade_set_kernel_timing", "cascade_read_kernel_timing", "cascade_measure_hbm_read",
            "cascade_measure_mfma_bf16", "cascade_pack_lmhead_w", "tree_verify_attn", "tree_verify_attn_static",
-           "lmhead_softmax_cfg", "cascade_attention_cut", "cascade_projection_tiles", "cascade_projection_streams", "cascade_accept", "select_path", "kv_commit", "convergence_weights"]
+           "lmhead_softmax_cfg", "cascade_attention_cut", "cascade_projection_tiles", "cascade_projection_streams", "cascade_accept", "select_path", "kv_commit", "convergence_weights",
+           "paged_slots", "paged_append", "paged_attn", "paged_attn_workspace", "sample_tokens"]
 
 _vp, _i32, _i64, _f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
 
@@ -80,6 +82,34 @@ class conv_weight_args(C.Structure):
                 ("tau_seq", _f32), ("c", _f32), ("weights", _vp), ("cos_next", _vp)]
 
 
+class paged_slots_args(C.Structure):
+    _fields_ = [("n_rows", _i32), ("page_size", _i32), ("n_pages", _i32), ("table_width", _i32), ("table_stride", _i64), ("max_tokens", _i32),
+                ("free_capacity", _i32), ("seq_len", _vp), ("new_len", _vp), ("node_off", _vp), ("row_prompt", _vp), ("accept_len", _vp),
+                ("path_nodes", _vp), ("n_prompts", _i32), ("max_depth", _i32), ("n_nodes_total", _i32), ("block_table", _vp), ("free_pages", _vp),
+                ("free_count", _vp), ("free_count_out", _vp), ("q_off", _vp), ("slot_map", _vp), ("position", _vp), ("source", _vp),
+                ("seq_len_out", _vp)]
+
+
+class paged_append_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("n_layers", _i32), ("n_tokens", _i32), ("n_source", _i32), ("n_kv_heads", _i32), ("head_dim", _i32),
+                ("slot_map", _vp), ("source", _vp), ("k_new", _vp), ("v_new", _vp), ("k_pages", _vp), ("v_pages", _vp), ("stride_layer", _i64),
+                ("stride_page", _i64), ("stride_head", _i64), ("stride_pos", _i64), ("n_pages", _i32), ("page_size", _i32)]
+
+
+class paged_attn_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("n_rows", _i32), ("q_off", _vp), ("parent", _vp), ("prefix_len", _vp), ("n_tokens", _i32), ("max_new", _i32),
+                ("max_prefix_len", _i32), ("n_heads", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("scale", _f32), ("window", _i32),
+                ("n_sink", _i32), ("q", _vp), ("k_new", _vp), ("v_new", _vp), ("q_stride", _i64), ("kv_stride", _i64), ("k_pages", _vp),
+                ("v_pages", _vp), ("stride_page", _i64), ("stride_head", _i64), ("stride_pos", _i64), ("n_pages", _i32), ("page_size", _i32),
+                ("block_table", _vp), ("table_stride", _i64), ("table_width", _i32), ("out", _vp), ("lse", _vp), ("workspace", _vp),
+                ("workspace_bytes", _i64)]
+
+
+class sample_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("n_rows", _i32), ("vocab", _i32), ("logits", _vp), ("row_stride", _i64), ("temperature", _vp), ("top_k", _vp),
+                ("top_p", _vp), ("min_p", _vp), ("u", _vp), ("token", _vp), ("prob", _vp)]
+
+
 # Argument records of the calls of a step are packed in one go: setting the fields of a ctypes structure one by one took most of a call's host
 # time (the four calls of a step of 15 nodes with their five launches: 28-29 us, now 22-27).
 _CODES = {_vp: "P", _i32: "i", C.c_int: "i", _i64: "q", _f32: "f"}
@@ -100,6 +130,7 @@ class _Record:
 
 
 _TREE_ATTN, _LMHEAD, _ACCEPT, _SELECT, _COMMIT, _WEIGHTS = map(_Record, (tree_attn_args, lmhead_args, accept_args, select_args, kv_commit_args, conv_weight_args))
+_SLOTS, _APPEND, _PAGED_ATTN, _SAMPLE = map(_Record, (paged_slots_args, paged_append_args, paged_attn_args, sample_args))
 
 _lib = None
 
@@ -141,9 +172,12 @@ def load_library() -> C.CDLL:
     lib.cascade_projection_tiles.restype = C.c_int
     lib.cascade_projection_streams.argtypes = [_vp, C.POINTER(lmhead_args)] + [C.POINTER(_i32)] * 2
     lib.cascade_projection_streams.restype = C.c_int
+    lib.paged_attn_workspace.argtypes = [_vp, C.POINTER(paged_attn_args), C.POINTER(_i64)]
+    lib.paged_attn_workspace.restype = C.c_int
     for name, st in (("tree_verify_attn", tree_attn_args), ("lmhead_softmax_cfg", lmhead_args),
                      ("cascade_accept", accept_args), ("select_path", select_args), ("kv_commit", kv_commit_args),
-                     ("convergence_weights", conv_weight_args)):
+                     ("convergence_weights", conv_weight_args), ("paged_slots", paged_slots_args), ("paged_append", paged_append_args),
+                     ("paged_attn", paged_attn_args), ("sample_tokens", sample_args)):
         fn = getattr(lib, name)
         fn.argtypes = [_vp, C.POINTER(st)]
         fn.restype = C.c_int
@@ -360,6 +394,72 @@ def convergence_weights(ctx: Context, *, features, tau_seq: float, c: float, wei
     seqs, length, hidden = features.shape
     _check(ctx.lib.convergence_weights_record(ctx.handle, _WEIGHTS(_dtype_code(features), seqs, length, hidden, features.data_ptr(), tau_seq, c,
                                                                    _ptr(weights), _ptr(cos_next))))
+
+
+def paged_slots(ctx: Context, *, seq_len, block_table, free_pages, free_count, page_size: int, n_pages: int, q_off, slot_map, seq_len_out, free_count_out,
+                new_len=None, position=None, source=None, node_off=None, row_prompt=None, accept_len=None, path_nodes=None, n_nodes_total: int = 0) -> None:
+    """block_table [S, width] int32 (last dim contiguous), extended in place; seq_len / seq_len_out / new_len [S]; free_pages [any], free_count /
+    free_count_out [1]; q_off [S+1]; slot_map / position / source [max_tokens].  Without new_len the rows keep select_path's paths."""
+    assert block_table.stride(1) == 1
+    _check(ctx.lib.paged_slots_record(ctx.handle, _SLOTS(
+        seq_len.numel(), page_size, n_pages, block_table.shape[1], block_table.stride(0), slot_map.numel(), free_pages.numel(), seq_len.data_ptr(),
+        *_ptrs(new_len, node_off, row_prompt, accept_len, path_nodes), accept_len.numel() if accept_len is not None else 0,
+        path_nodes.shape[1] if path_nodes is not None else 0, n_nodes_total,
+        *_ptrs(block_table, free_pages, free_count, free_count_out, q_off, slot_map, position, source, seq_len_out))))
+
+
+def paged_append(ctx: Context, *, k_new, v_new, slot_map, k_pages, v_pages, source=None) -> None:
+    """k_new/v_new [L,N,Hkv,D]; k_pages/v_pages [L,pages,Hkv,page_size,D] in any order of memory (last dim contiguous); slot_map/source [tokens]."""
+    shape, stride = k_pages.shape, k_pages.stride()
+    assert k_new.is_contiguous() and v_new.is_contiguous() and k_new.shape == v_new.shape and k_new.dtype == v_new.dtype == k_pages.dtype == v_pages.dtype
+    assert v_pages.shape == shape and stride == v_pages.stride() and stride[4] == 1 and k_new.shape[0] == shape[0] and k_new.shape[2:] == (shape[2], shape[4])
+    _check(ctx.lib.paged_append_record(ctx.handle, _APPEND(
+        _dtype_code(k_new), shape[0], slot_map.numel(), k_new.shape[1], shape[2], shape[4], *_ptrs(slot_map, source, k_new, v_new, k_pages, v_pages),
+        *stride[:4], shape[1], shape[3])))
+
+
+def _paged_attn_record(q_off, prefix_len, block_table, q, k_new, v_new, k_pages, v_pages, out, lse, parent, scale, window, n_sink, max_new,
+                       max_prefix_len, workspace) -> bytes:
+    shape, q_stride, kv_stride = q.shape, q.stride(), k_new.stride()
+    D = shape[2]
+    assert out.is_contiguous() and out.shape == shape and out.dtype == q.dtype == k_new.dtype == v_new.dtype and k_new.shape == v_new.shape
+    assert q_stride[1:] == (D, 1) and kv_stride == v_new.stride() and kv_stride[1:] == (D, 1) and k_new.shape[2] == D and k_new.shape[0] == shape[0]
+    if k_pages is not None:
+        pages, page_size, stride = k_pages.shape[0], k_pages.shape[2], k_pages.stride()
+        assert stride == v_pages.stride() and k_pages.shape == v_pages.shape and stride[3] == 1 and k_pages.shape[1::2] == k_new.shape[1:]
+        assert k_pages.dtype == v_pages.dtype == q.dtype and block_table.stride(1) == 1
+        width, table_stride = block_table.shape[1], block_table.stride(0)
+    else:
+        pages, page_size, stride, width, table_stride = 0, 16, (0, 0, 0, 1), 0, 0
+    return _PAGED_ATTN(_dtype_code(q), prefix_len.numel(), *_ptrs(q_off, parent, prefix_len), shape[0], max_new, max_prefix_len, shape[1], k_new.shape[1], D,
+                       scale, window, n_sink, *_ptrs(q, k_new, v_new), q_stride[0], kv_stride[0], *_ptrs(k_pages, v_pages), *stride[:3], pages, page_size,
+                       _ptr(block_table), table_stride, width, *_ptrs(out, lse, workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0)
+
+
+def paged_attn(ctx: Context, *, q_off, prefix_len, block_table, q, k_new, v_new, k_pages, v_pages, out, lse=None, parent=None, scale: float = 0.0,
+               window: int = 0, n_sink: int = 0, max_new: int, max_prefix_len: int, workspace: Optional[torch.Tensor] = None) -> None:
+    """q/out [N,Hq,D], k_new/v_new [N,Hkv,D] (tokens any stride apart; out contiguous), k_pages/v_pages [pages,Hkv,page_size,D] in any order of memory
+    (last dim contiguous), block_table [S,width].  parent None: chains.  workspace: scratch for calls that are recorded into a graph
+    (paged_attn_workspace says how much)."""
+    _check(ctx.lib.paged_attn_record(ctx.handle, _paged_attn_record(q_off, prefix_len, block_table, q, k_new, v_new, k_pages, v_pages, out, lse, parent, scale,
+                                                                    window, n_sink, max_new, max_prefix_len, workspace)))
+
+
+def paged_attn_workspace(ctx: Context, *, q_off, prefix_len, block_table, q, k_new, v_new, k_pages, v_pages, out, lse=None, parent=None, scale: float = 0.0,
+                         window: int = 0, n_sink: int = 0, max_new: int, max_prefix_len: int) -> int:
+    """Bytes of scratch with which a paged_attn call with these arguments never takes fewer parts than it would like."""
+    a = paged_attn_args.from_buffer_copy(_paged_attn_record(q_off, prefix_len, block_table, q, k_new, v_new, k_pages, v_pages, out, lse, parent, scale, window,
+                                                            n_sink, max_new, max_prefix_len, None))
+    n = _i64()
+    _check(ctx.lib.paged_attn_workspace(ctx.handle, C.byref(a), C.byref(n)))
+    return n.value
+
+
+def sample_tokens(ctx: Context, *, logits, u, token, prob=None, temperature=None, top_k=None, top_p=None, min_p=None) -> None:
+    """logits [rows, vocab] (last dim contiguous); temperature / top_p / min_p / u [rows] float32, top_k [rows] int32; token [rows] int32, prob [rows]."""
+    assert logits.stride(1) == 1
+    _check(ctx.lib.sample_tokens_record(ctx.handle, _SAMPLE(_dtype_code(logits), logits.shape[0], logits.shape[1], logits.data_ptr(), logits.stride(0),
+                                                            *_ptrs(temperature, top_k, top_p, min_p, u, token, prob))))
 
 
 # ------------------------------------------------------------------------------------------------

@@ -424,4 +424,114 @@ int convergence_weights(cascade_ctx* ctx, const conv_weight_args* a) {
   return err == hipSuccess ? CASCADE_OK : hip_fail(err);
 }
 
+// what all calls on a pool of pages ask of it
+static int check_pages(int32_t n_pages, int32_t page_size) {
+  if (n_pages < 0 || page_size <= 0) return CASCADE_EINVAL;
+  if (page_size % 16 || page_size > CASCADE_MAX_PAGE || (int64_t)n_pages * page_size > 0x7fffffff) return CASCADE_ESHAPE;
+  return CASCADE_OK;
+}
+
+int paged_slots(cascade_ctx* ctx, const paged_slots_args* a) {
+  if (!ctx || !a) return CASCADE_EINVAL;
+  if (!a->seq_len || !a->block_table || !a->free_count || !a->free_count_out || !a->q_off || !a->seq_len_out || a->seq_len == a->seq_len_out ||
+      a->free_count == a->free_count_out)
+    return CASCADE_EINVAL;
+  if (a->n_rows < 0 || a->table_width < 0 || a->table_stride < a->table_width || a->max_tokens < 0 || a->free_capacity < 0) return CASCADE_EINVAL;
+  if ((a->max_tokens > 0 && !a->slot_map) || (a->free_capacity > 0 && !a->free_pages)) return CASCADE_EINVAL;
+  if (!a->new_len) {
+    if (!a->node_off || !a->row_prompt || !a->accept_len || (a->max_tokens > 0 && !a->source)) return CASCADE_EINVAL;
+    if (a->n_prompts < 0 || a->max_depth < 0 || a->n_nodes_total < 0 || (a->max_depth > 0 && !a->path_nodes)) return CASCADE_EINVAL;
+    if (a->max_depth > CASCADE_MAX_DEPTH || a->n_nodes_total > ctx->lim.max_nodes_total) return CASCADE_ESHAPE;
+  }
+  const int st = check_pages(a->n_pages, a->page_size);
+  if (st != CASCADE_OK) return st;
+  if (a->n_rows > ctx->lim.max_rows || (int64_t)a->table_width * a->page_size > 0x7fffffff) return CASCADE_ESHAPE;
+  if (a->n_rows == 0) return CASCADE_OK;
+  hipError_t err = launch_paged_slots(ctx, a);
+  return err == hipSuccess ? CASCADE_OK : hip_fail(err);
+}
+
+int paged_append(cascade_ctx* ctx, const paged_append_args* a) {
+  if (!ctx || !a) return CASCADE_EINVAL;
+  if (!a->slot_map || !a->k_new || !a->v_new || !a->k_pages || !a->v_pages) return CASCADE_EINVAL;
+  if (a->dtype != CASCADE_F32 && a->dtype != CASCADE_BF16) return CASCADE_EDTYPE;
+  if (a->n_layers < 0 || a->n_tokens < 0 || a->n_source < 0 || a->n_kv_heads <= 0 || a->head_dim <= 0) return CASCADE_EINVAL;
+  if (!a->source && a->n_source < a->n_tokens) return CASCADE_EINVAL;
+  const int st = check_pages(a->n_pages, a->page_size);
+  if (st != CASCADE_OK) return st;
+  const int64_t e = a->dtype == CASCADE_BF16 ? 2 : 4;
+  const int64_t strides[4] = {a->stride_layer, a->stride_page, a->stride_head, a->stride_pos};
+  for (int i = 0; i < 4; ++i)
+    if (strides[i] < 0 || (strides[i] * e) % 16) return CASCADE_ESHAPE;
+  if ((a->head_dim * e) % 16) return CASCADE_ESHAPE;
+  if (((uintptr_t)a->k_new | (uintptr_t)a->v_new | (uintptr_t)a->k_pages | (uintptr_t)a->v_pages) & 15) return CASCADE_EINVAL;
+  if (a->n_layers > 65535 || (int64_t)a->n_tokens * a->n_kv_heads * (a->head_dim * e / 16) > 0x7fffffff) return CASCADE_ESHAPE;
+  if (a->n_layers == 0 || a->n_tokens == 0) return CASCADE_OK;
+  hipError_t err = launch_paged_append(ctx, a);
+  return err == hipSuccess ? CASCADE_OK : hip_fail(err);
+}
+
+static int check_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a) {
+  if (!a->q_off || !a->prefix_len || !a->q || !a->k_new || !a->v_new || !a->out) return CASCADE_EINVAL;
+  if (a->n_rows < 0 || a->n_tokens < 0 || a->max_new < 0 || a->max_prefix_len < 0 || a->window < 0 || a->n_sink < 0 || a->workspace_bytes < 0)
+    return CASCADE_EINVAL;
+  if (a->max_prefix_len > 0 && (!a->k_pages || !a->v_pages || !a->block_table || a->n_pages == 0)) return CASCADE_EINVAL;
+  if (a->dtype != CASCADE_F32 && a->dtype != CASCADE_BF16) return CASCADE_EDTYPE;
+  if (a->n_heads <= 0 || a->n_kv_heads <= 0 || a->head_dim <= 0 || bad_float(a->scale) || a->scale < 0.f) return CASCADE_EINVAL;
+  if (a->n_heads % a->n_kv_heads != 0) return CASCADE_ESHAPE;
+  const int st = check_pages(a->n_pages, a->page_size);
+  if (st != CASCADE_OK) return st;
+  if (a->table_width < 0 || a->table_stride < a->table_width) return CASCADE_EINVAL;
+  if (a->stride_page < 0 || a->stride_head < 0 || a->stride_pos < 0 || a->q_stride < (int64_t)a->n_heads * a->head_dim ||
+      a->kv_stride < (int64_t)a->n_kv_heads * a->head_dim)
+    return CASCADE_ESHAPE;
+  const cascade_limits& L = ctx->lim;
+  if (a->n_rows > L.max_rows || a->n_tokens > L.max_nodes_total || a->max_prefix_len > L.max_prefix || a->n_heads > L.n_heads || a->head_dim > L.head_dim)
+    return CASCADE_ESHAPE;
+  if (a->parent && a->max_new > L.max_nodes_per_tree) return CASCADE_ESHAPE;
+  // positions and what a launch counts stay below 2^30
+  if (a->max_prefix_len > (1 << 30) || a->max_new > (1 << 30) || (int64_t)a->n_tokens * a->n_heads > (1 << 30) || a->n_kv_heads > 65535) return CASCADE_ESHAPE;
+  if (a->dtype == CASCADE_BF16) {
+    if (a->head_dim != 64 && a->head_dim != 128) return CASCADE_ESHAPE;
+    if ((a->stride_page | a->stride_head | a->stride_pos | a->q_stride | a->kv_stride) % 8) return CASCADE_ESHAPE;
+    if (((uintptr_t)a->q | (uintptr_t)a->k_new | (uintptr_t)a->v_new | (uintptr_t)a->k_pages | (uintptr_t)a->v_pages | (uintptr_t)a->out) & 15)
+      return CASCADE_EINVAL;
+  } else if (a->head_dim > 256) {
+    return CASCADE_ESHAPE;
+  }
+  if ((uintptr_t)a->workspace & 15) return CASCADE_EINVAL;
+  return CASCADE_OK;
+}
+
+int paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
+  if (!ctx || !a) return CASCADE_EINVAL;
+  const int st = check_paged_attn(ctx, a);
+  if (st != CASCADE_OK) return st;
+  if (a->n_rows == 0 || a->n_tokens == 0) return CASCADE_OK;
+  if (a->max_new == 0) return CASCADE_ESHAPE;   // the grids are sized by the bound: tokens without one are a contradiction
+  hipError_t err = launch_paged_attn(ctx, a);
+  return err == hipSuccess ? CASCADE_OK : hip_fail(err);
+}
+
+int paged_attn_workspace(const cascade_ctx* ctx, const paged_attn_args* a, int64_t* bytes) {
+  if (!ctx || !a || !bytes) return CASCADE_EINVAL;
+  const int st = check_paged_attn(ctx, a);
+  if (st != CASCADE_OK) return st;
+  *bytes = 0;
+  if (a->n_rows == 0 || a->n_tokens == 0 || a->max_new == 0) return CASCADE_OK;
+  *bytes = plan_paged_attn(ctx, a);
+  return CASCADE_OK;
+}
+
+int sample_tokens(cascade_ctx* ctx, const sample_args* a) {
+  if (!ctx || !a) return CASCADE_EINVAL;
+  if (!a->logits || !a->u || !a->token) return CASCADE_EINVAL;
+  if (a->dtype != CASCADE_F32 && a->dtype != CASCADE_BF16) return CASCADE_EDTYPE;
+  if (a->n_rows < 0 || a->vocab <= 0) return CASCADE_EINVAL;
+  if (a->vocab > ctx->lim.vocab || (a->row_stride < a->vocab && a->n_rows > 1)) return CASCADE_ESHAPE;
+  if (a->n_rows == 0) return CASCADE_OK;
+  hipError_t err = launch_sample(ctx, a);
+  return err == hipSuccess ? CASCADE_OK : hip_fail(err);
+}
+
 }  // extern "C"

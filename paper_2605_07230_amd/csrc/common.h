@@ -75,7 +75,8 @@ enum {
   CASCADE_FLAG_DEPTH = 8,    // path longer than max_depth
   CASCADE_FLAG_CAPACITY = 16, // kv_commit: a row's cache has no room for root + accepted path
   CASCADE_FLAG_PATH = 32,    // kv_commit: a path entry outside the row's tree, or a bad row_prompt
-  CASCADE_FLAG_TREE_SIZE = 64  // a tree with more nodes than the bound the launch was sized for
+  CASCADE_FLAG_TREE_SIZE = 64, // a tree with more nodes than the bound the launch was sized for
+  CASCADE_FLAG_PAGE = 128      // a page or slot outside the pool, or a count of free pages outside its list
 };
 
 // launchers (one translation unit each); all return hipError_t of the launch
@@ -93,6 +94,11 @@ hipError_t launch_select(cascade_ctx* ctx, const select_args* a);
 hipError_t launch_select_residual(cascade_ctx* ctx, const select_args* a);
 hipError_t launch_kv_commit(cascade_ctx* ctx, const kv_commit_args* a);
 hipError_t launch_conv_weights(cascade_ctx* ctx, const conv_weight_args* a);
+hipError_t launch_paged_slots(cascade_ctx* ctx, const paged_slots_args* a);
+hipError_t launch_paged_append(cascade_ctx* ctx, const paged_append_args* a);
+hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a);
+int64_t plan_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a);   // bytes of partial results that the call's cut leaves
+hipError_t launch_sample(cascade_ctx* ctx, const sample_args* a);
 
 // ----------------------------------------------------------------------------------------------
 // device helpers
