@@ -1,17 +1,541 @@
 // paged_attn kernels for gfx950: attention of new tokens (a chain, or a drafted tree) over a cache in pages and over themselves.
+//
+// The query rows of a (row of the batch, kv head) are its tokens times the query heads that share the kv head, token by token, so that a block of rows is a
+// short run of positions: what a chain's mask or a window leaves it is one run of key tiles (two with sinks), and no other tile is touched.
+//
+// Keys come in tiles of 64, first those of the pages, then those of the new tokens.  A page holds a multiple of 16 positions, so 16 keys that begin
+// at a multiple of 16 lie in one page, one stride apart: a wave looks one entry of the table up for them, in scalar registers.
+//
+// Scores are produced transposed, S^T = K Q^T (v_mfma_f32_16x16x32_bf16): a lane owns one query column, so the running maximum and sum are
+// per-lane scalars, a mask is one 64-bit word per lane and tile, made from three comparisons, and the probabilities are already the B operand of
+// O^T = V^T P^T, whose A operand the transposing LDS read (ds_read_b64_tr_b16) takes from row-major values.
+//
+// A masked key has probability 0, but 0 x inf and 0 x NaN are NaN.  Places that no token of the workgroup sees are never taken from memory, or are
+// zeroed on the way; a tile that some tokens see and others do not is looked through for such values, and if it holds any they are taken out of the product
+// and added to the tokens that see them.
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
 #include "common.h"
 
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
+constexpr int KT = 64;   // keys per tile
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned long long u64;
 
 struct PagedParams {
   paged_attn_args a;
   int group;
   float scale_log2e;
   int* dev_status;
+  int page16;            // 16-key groups of a page
+  unsigned page16_inv;   // floor(2^32 / page16) + 1: group / page16 as a high product (groups stay below 2^26, page16 <= 64); 0 for page16 1
+  int parts;             // that the keys of a row are cut into at most; 1: results are written at once
+  int part_tiles;        // tiles of a part (few rows)
+  float* ws_o;           // [parts][n_tokens * n_heads][head_dim]
+  float* ws_ml;          // [parts][n_tokens * n_heads][2]
 };
+
+__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
+  const bf16x2_t v = __builtin_convertvector(f32x2_t{a, b}, bf16x2_t);
+  return *(const uint32_t*)&v;
+}
+union Frag8 {
+  bf16x8 v;
+  uint4 u;
+};
+
+// bits 0 .. n - 1
+__device__ __forceinline__ u64 below(int n) { return n <= 0 ? 0ull : (n >= 64 ? ~0ull : (1ull << n) - 1ull); }
+
+// ---- one row of the batch
+struct RowInfo {
+  int s, lo, T, P;
+  int flag;   // what is wrong with it; then T counts the tokens of it that exist, for zeros
+};
+__device__ __forceinline__ RowInfo check_row(const PagedParams& p, int s, int lo, int hi, int P) {
+  const paged_attn_args& a = p.a;
+  RowInfo r = {s, lo, hi - lo, P, 0};
+  if (lo < 0 || hi > a.n_tokens || lo > hi || hi - lo > a.max_new) {
+    r.flag = CASCADE_FLAG_TREE_SIZE;
+    r.lo = max(lo, 0);
+    r.T = max(min(hi, a.n_tokens) - r.lo, 0);
+  } else if (P < 0 || P > a.max_prefix_len || (long long)P > (long long)a.table_width * a.page_size) {
+    r.flag = CASCADE_FLAG_CAPACITY;
+  }
+  return r;
+}
+
+// The tiles that query tokens i0 .. i1 of a row see: n_p of the pages, then n_n of the new tokens.  A window leaves those of the sinks and those from
+// its beginning on; `skip` tiles between them are left out.
+struct Tiles {
+  int n_p, sinks_p, skip_p;
+  int n_n, sinks_n, skip_n;
+  int first;   // the first position that some of these tokens sees through the window (all: 0)
+  __device__ __forceinline__ int prefix_tile(int t) const { return t < sinks_p ? t : t + skip_p; }
+  __device__ __forceinline__ int new_tile(int t) const { return t < sinks_n ? t : t + skip_n; }
+};
+__device__ __forceinline__ Tiles tiles_of(const PagedParams& p, int P, int i0, int i1, bool tree) {
+  const int W = p.a.window, n_pt = (P + KT - 1) / KT, n_nt = i1 / KT + 1;
+  Tiles t = {n_pt, 0, 0, n_nt, 0, 0, 0};
+  if (W > 0) {
+    if (tree) i0 = 0;   // a node's position is its depth
+    t.first = max(0, P + i0 - W + 1);
+    const int from_p = t.first < P ? t.first / KT : n_pt;
+    t.sinks_p = (min(p.a.n_sink, P) + KT - 1) / KT;
+    t.skip_p = max(0, from_p - t.sinks_p);
+    t.n_p = n_pt - t.skip_p;
+    if (!tree) {
+      t.sinks_n = min((min(max(p.a.n_sink - P, 0), i1 + 1) + KT - 1) / KT, n_nt);
+      t.skip_n = max(0, max(0, i0 - W + 1) / KT - t.sinks_n);
+      t.n_n = n_nt - t.skip_n;
+    }
+  }
+  return t;
+}
+
+// keys kb .. kb + 63 of the pages that a token at position x sees; of a chain's new tokens, that token i sees
+__device__ __forceinline__ u64 sees_prefix(const PagedParams& p, int P, int kb, int x) {
+  u64 v = below(P - kb);
+  if (p.a.window > 0) v &= ~below(x - p.a.window + 1 - kb) | below(p.a.n_sink - kb);
+  return v;
+}
+__device__ __forceinline__ u64 sees_chain(const PagedParams& p, int P, int kb, int i) {
+  u64 v = below(i + 1 - kb);
+  if (p.a.window > 0) v &= ~below(i - p.a.window + 1 - kb) | below(p.a.n_sink - P - kb);
+  return v;
+}
+
+// The group of 16 keys to load for group g: itself, or, where none of its keys exists or is seen, one with such keys.
+__device__ __forceinline__ int needed_group(const PagedParams& p, const Tiles& ti, int P, int g) {
+  g = min(g, (P - 1) >> 4);
+  if (p.a.window > 0 && 16 * g >= p.a.n_sink && 16 * g + 15 < ti.first) g = ti.first < P ? ti.first >> 4 : (min(p.a.n_sink, P) - 1) >> 4;
+  return g;
+}
+__device__ __forceinline__ int page_index(const PagedParams& p, int g) { return p.page16_inv ? (int)__umulhi((unsigned)g, p.page16_inv) : g; }
+
+// an entry of the table; one outside the pool is flagged and stands for the first page
+__device__ __forceinline__ int checked_page(const PagedParams& p, int page) {
+  if ((unsigned)page < (unsigned)p.a.n_pages) return page;
+  if ((threadIdx.x & 63) == 0) atomicOr(p.dev_status, CASCADE_FLAG_PAGE);
+  return 0;
+}
+typedef const __attribute__((address_space(4))) int32_t* ConstTable;   // loads through the scalar cache
+__device__ __forceinline__ int table_entry(const PagedParams& p, int s, int e) {
+  return *((ConstTable)(uintptr_t)p.a.block_table + ((long long)s * p.a.table_stride + e));
+}
+// element offset of the first key of group g in page `page` (e-th of the row), kv head kvh
+__device__ __forceinline__ long long group_offset(const PagedParams& p, int page, int e, int g, int kvh) {
+  return page * p.a.stride_page + kvh * p.a.stride_head + (long long)(16 * (g - e * p.page16)) * p.a.stride_pos;
+}
+
+// infinities and NaN among packed bf16 pairs: adding one to an exponent of ones reaches the sign's place
+__device__ __forceinline__ uint32_t odd_exponent(uint32_t x) { return (x & 0x7f807f80u) + 0x00800080u; }   // & 0x80008000
+__device__ __forceinline__ uint32_t finite_only(uint32_t x) {
+  const uint32_t bad = odd_exponent(x) & 0x80008000u;
+  return x & ~(bad | (bad - (bad >> 15)));
+}
+
+// zeros for the tokens of a row that cannot be computed, query heads of one kv head; empty parts where there are several
+template <typename T>
+__device__ __forceinline__ void write_nothing(const PagedParams& p, const RowInfo& r, int kvh, int part, int tid, int threads) {
+  const int D = p.a.head_dim, G = p.group;
+  if (tid == 0 && part == 0) atomicOr(p.dev_status, r.flag);
+  for (int i = tid; i < r.T * G; i += threads) {
+    const long long row = (long long)(r.lo + i / G) * p.a.n_heads + kvh * G + i % G;
+    if (p.parts > 1) {
+      float* ml = p.ws_ml + ((long long)part * p.a.n_tokens * p.a.n_heads + row) * 2;
+      ml[0] = -INFINITY;
+      ml[1] = 0.f;
+    } else if (part == 0) {
+      for (int d = 0; d < D; ++d) ((T*)p.a.out)[row * D + d] = 0;
+      if (p.a.lse) p.a.lse[row] = -INFINITY;
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------ bf16, few query rows
+// Up to 16 NQ query rows (single tokens, a few of them): bound by the stream of keys and values, so every wave of a workgroup takes its own tiles - w, w + NW, ... of the part
+// - and needs no barrier until their end, where the waves' maxima, sums and outputs meet in LDS.  Keys are loaded in operand order (16 bytes of
+// a key per lane), values through a region of LDS of the wave's own.  A workgroup works through parts (row, kv head, run of part_tiles tiles) until
+// none is left: rows of very different lengths fill the chip evenly, and no workgroup is launched for nothing.
+template <int D, int NQ, int NW, bool TREE>
+__global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedParams p) {
+  constexpr int NT = 64 * NW, KS = D / 32, DB = D / 16, DC = D / 8, VP = D + 16, OP = D + 4, NVC = KT * DC / 64, R = 16 * NQ;
+  extern __shared__ __align__(16) char few_smem[];
+  const paged_attn_args& a = p.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g = lane >> 4, G = p.group;
+  uint16_t* vt = (uint16_t*)few_smem + (size_t)wave * KT * VP;
+
+  for (int item = blockIdx.x;; item += gridDim.x) {
+    const int kvh = item % a.n_kv_heads;
+    int part = item / a.n_kv_heads;
+    // which row this part belongs to
+    RowInfo r = {-1, 0, 0, 0, 0};
+    int n_parts = 0;
+    for (int base = 0; base < a.n_rows && r.s < 0; base += 64) {
+      const int at = base + lane;
+      RowInfo mine = {at, 0, 0, 0, 0};
+      int n = 0;
+      if (at < a.n_rows) {
+        mine = check_row(p, at, a.q_off[at], a.q_off[at + 1], a.prefix_len[at]);
+        if (mine.flag) {
+          n = 1;   // (reported even if it holds no token)
+        } else if (mine.T > 0) {
+          const Tiles ti = tiles_of(p, mine.P, 0, mine.T - 1, TREE);
+          n = (ti.n_p + ti.n_n + p.part_tiles - 1) / p.part_tiles;
+        }
+      }
+      const int incl = wave_scan_incl_i(n);
+      const u64 who = __ballot(part < incl);
+      if (who) {
+        const int l = __ffsll((long long)who) - 1;
+        r.s = base + l;
+        r.lo = __builtin_amdgcn_readlane(mine.lo, l);
+        r.T = __builtin_amdgcn_readlane(mine.T, l);
+        r.P = __builtin_amdgcn_readlane(mine.P, l);
+        r.flag = __builtin_amdgcn_readlane(mine.flag, l);
+        n_parts = __builtin_amdgcn_readlane(n, l);
+        part -= __builtin_amdgcn_readlane(incl - n, l);
+      } else {
+        part -= __builtin_amdgcn_readlane(incl, 63);
+      }
+    }
+    if (r.s < 0) return;
+    if (r.flag) {
+      for (int q = 0; q < p.parts; ++q) write_nothing<uint16_t>(p, r, kvh, q, tid, NT);
+      continue;
+    }
+    const int lo = r.lo, T = r.T, P = r.P, M = T * G;
+    const Tiles ti = tiles_of(p, P, 0, T - 1, TREE);
+    const int nt = ti.n_p + ti.n_n, t_begin = part * p.part_tiles, t_end = min(nt, t_begin + p.part_tiles);
+    if (part == 0 && p.parts > n_parts)   // parts that this row has not
+      for (int i = tid; i < M * (p.parts - n_parts); i += NT) {
+        const int q = i % M;
+        float* ml = p.ws_ml + ((long long)(n_parts + i / M) * a.n_tokens * a.n_heads + (long long)(lo + q / G) * a.n_heads + kvh * G + q % G) * 2;
+        ml[0] = -INFINITY;
+        ml[1] = 0.f;
+      }
+
+    // ---- a tile: kf[kt][ks] = key 16 kt + l16, d 32 ks + 8 g .. + 7; value pieces c = lane + 64 it of the row-major tile
+    u32x4 kf[4][KS], vr[NVC];
+    const uint16_t *kn = (const uint16_t*)a.k_new + lo * a.kv_stride + kvh * D, *vn = (const uint16_t*)a.v_new + lo * a.kv_stride + kvh * D;
+    auto request = [&](int t) {
+      if (t < ti.n_p) {
+        const int kb = ti.prefix_tile(t) * KT;
+        int gq[4];
+        long long off[4];
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+          gq[kt] = needed_group(p, ti, P, (kb >> 4) + kt);
+          const int e = page_index(p, gq[kt]);
+          off[kt] = group_offset(p, checked_page(p, table_entry(p, r.s, e)), e, gq[kt], kvh);
+        }
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+          const uint16_t* kp = (const uint16_t*)a.k_pages + off[kt] + (long long)min(l16, P - 1 - 16 * gq[kt]) * a.stride_pos + 8 * g;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) kf[kt][ks] = *(const u32x4*)(kp + 32 * ks);
+        }
+#pragma unroll
+        for (int it = 0; it < NVC; ++it) {
+          const int c = lane + 64 * it, kt = it / (NVC / 4), in = (c / DC) & 15;
+          vr[it] = *(const u32x4*)((const uint16_t*)a.v_pages + off[kt] + (long long)min(in, P - 1 - 16 * gq[kt]) * a.stride_pos + 8 * (c % DC));
+        }
+      } else {
+        const int kb = ti.new_tile(t - ti.n_p) * KT;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+          const uint16_t* kp = kn + (long long)min(kb + 16 * kt + l16, T - 1) * a.kv_stride + 8 * g;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) kf[kt][ks] = *(const u32x4*)(kp + 32 * ks);
+        }
+#pragma unroll
+        for (int it = 0; it < NVC; ++it) {
+          const int c = lane + 64 * it;
+          vr[it] = *(const u32x4*)(vn + (long long)min(kb + c / DC, T - 1) * a.kv_stride + 8 * (c % DC));
+        }
+      }
+    };
+    // queries (B operand of S^T): rows past the end repeat the last one, masked and never stored
+    Frag8 qf[NQ][KS];
+    int qi[NQ];
+    bool q_ok[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      const int row = min(16 * n + l16, M - 1);
+      q_ok[n] = 16 * n + l16 < M;
+      qi[n] = G == 1 ? row : row / G;
+      const uint16_t* qp = (const uint16_t*)a.q + (long long)(lo + qi[n]) * a.q_stride + (kvh * G + row - qi[n] * G) * D + 8 * g;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) qf[n][ks].u = *(const uint4*)(qp + 32 * ks);
+    }
+    // trees (at most 32 nodes here): parents in the lanes; what a token sees of the new tokens, and its depth
+    u64 path[NQ];
+    int depth[NQ];
+    int pa = -1;
+    if (TREE) pa = a.parent[lo + min(lane, T - 1)];
+    if (t_begin + wave < t_end) request(t_begin + wave);
+    if (TREE) {
+      const bool bad = lane < T && (lane == 0 ? pa != -1 : (pa >= lane || pa < 0));
+      if (bad) { atomicOr(p.dev_status, CASCADE_FLAG_PARENT); pa = lane == 0 ? -1 : 0; }
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        path[n] = 0;
+        int x = qi[n];
+        while (__any(x >= 0)) {
+          if (x >= 0) path[n] |= 1ull << x;
+          const int up = __builtin_amdgcn_ds_bpermute(4 * (x & 63), pa);
+          x = x > 0 ? up : -1;
+        }
+        depth[n] = __popcll(path[n]) - 1;
+        if (a.window > 0) {   // the nearest `window` of them, and the sinks
+          const int keep_sinks = a.n_sink - P;   // depths below this
+          u64 all = path[n];
+          int left = depth[n] + 1 - a.window;   // so many of the path's first are out of reach
+          int d = 0;
+          while (__any(all != 0)) {
+            if (all) {
+              const int b = __ffsll((long long)all) - 1;
+              if (d < left && d >= keep_sinks) path[n] &= ~(1ull << b);
+              all &= all - 1;
+              ++d;
+            }
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) { path[n] = 0; depth[n] = qi[n]; }
+    }
+
+    f32x4 ot[NQ][DB];
+    float m_run[NQ], l_run[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      m_run[n] = -INFINITY;
+      l_run[n] = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) ot[n][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int t = t_begin + wave; t < t_end; t += NW) {
+      const bool fresh = t >= ti.n_p;
+      const int kb = fresh ? ti.new_tile(t - ti.n_p) * KT : ti.prefix_tile(t) * KT;
+      f32x4 st[NQ][4];
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          st[n][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            Frag8 a8;
+            a8.u = make_uint4(kf[kt][ks][0], kf[kt][ks][1], kf[kt][ks][2], kf[kt][ks][3]);
+            st[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a8.v, qf[n][ks].v, st[n][kt], 0, 0, 0);
+          }
+        }
+      __builtin_amdgcn_sched_barrier(0);
+      // what some token sees of this tile, and whether all of them see the same
+      u64 valid[NQ], some = 0, all = ~0ull;
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        valid[n] = fresh ? (TREE ? path[n] : sees_chain(p, P, kb, qi[n])) : sees_prefix(p, P, kb, P + depth[n]);
+        some |= valid[n];
+        all &= valid[n];
+      }
+      // (lanes differ only in l16)
+      if (T > 1 && (fresh || (a.window > 0))) {
+#pragma unroll
+        for (int s = 1; s < 16; s <<= 1) {
+          some |= ((u64)(unsigned)__shfl_xor((int)(some >> 32), s) << 32) | (unsigned)__shfl_xor((int)some, s);
+          all &= ((u64)(unsigned)__shfl_xor((int)(all >> 32), s) << 32) | (unsigned)__shfl_xor((int)all, s);
+        }
+      }
+      bool odd = false;   // wave-uniform: values that must not meet a masked probability
+      if (__any(some != ~0ull || all != ~0ull)) {
+        uint32_t seen_odd = 0;
+#pragma unroll
+        for (int it = 0; it < NVC; ++it) {
+          const int c = lane + 64 * it;
+          const bool keep = (some >> (c / DC)) & 1;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            vr[it][e] = keep ? vr[it][e] : 0u;
+            seen_odd |= odd_exponent(vr[it][e]);
+          }
+        }
+        odd = __any((seen_odd & 0x80008000u) != 0) && __any(some != all);
+      }
+      // values: registers -> this wave's LDS tile (row-major); the previous tile's reads are complete (same wave, in order)
+#pragma unroll
+      for (int it = 0; it < NVC; ++it) {
+        const int c = lane + 64 * it;
+        *(u32x4*)(&vt[(c / DC) * VP + 8 * (c % DC)]) = vr[it];
+      }
+      __builtin_amdgcn_wave_barrier();   // keep the tile's stores ahead of its transposing reads in program order
+      if (t + NW < t_end) request(t + NW);   // the wave's next tile streams in during the softmax
+      Frag8 pf[NQ][2];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const u64 vis = q_ok[n] ? valid[n] : 0ull;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+          const uint32_t nib = (uint32_t)(vis >> (16 * kt + 4 * g));   // this lane's 4 keys of sub-tile kt
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const float z = ((nib >> c) & 1u) ? st[n][kt][c] * p.scale_log2e : -INFINITY;
+            st[n][kt][c] = z;
+            mx = fmaxf(mx, z);
+          }
+        }
+        mx = rows4_max(mx);
+        const float m_new = fmaxf(m_run[n], mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = fast_exp2(m_run[n] - m_use);
+        float ls = 0.f;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const float e = fast_exp2(st[n][kt][c] - m_use);
+            st[n][kt][c] = e;
+            ls += e;
+          }
+        l_run[n] = l_run[n] * alpha + ls;
+        m_run[n] = m_new;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) ot[n][db] *= alpha;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          pf[n][j].u.x = pack_bf16x2(st[n][2 * j][0], st[n][2 * j][1]);
+          pf[n][j].u.y = pack_bf16x2(st[n][2 * j][2], st[n][2 * j][3]);
+          pf[n][j].u.z = pack_bf16x2(st[n][2 * j + 1][0], st[n][2 * j + 1][1]);
+          pf[n][j].u.w = pack_bf16x2(st[n][2 * j + 1][2], st[n][2 * j + 1][3]);
+        }
+      }
+      // O^T += V^T P^T with transposing reads of the wave's tile (LDS operations of one wave complete in order)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint16_t* vp = &vt[(32 * j + 4 * g + (l16 >> 2)) * VP + 16 * db + 4 * (l16 & 3)];
+          union { Frag8 f; s16x4 h[2]; } vf;
+          vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(vp));
+          vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(vp + 16 * VP));
+          if (odd) vf.f.u = make_uint4(finite_only(vf.f.u.x), finite_only(vf.f.u.y), finite_only(vf.f.u.z), finite_only(vf.f.u.w));
+#pragma unroll
+          for (int n = 0; n < NQ; ++n) ot[n][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.f.v, pf[n][j].v, ot[n][db], 0, 0, 0);
+        }
+      if (odd)
+        for (int key = 0; key < KT; ++key)
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const float v = bf16_bits_to_f32(vt[key * VP + 16 * db + 4 * g + c]);
+              const bool is_odd = !(fabsf(v) < INFINITY);
+#pragma unroll
+              for (int n = 0; n < NQ; ++n)
+                if (is_odd && ((valid[n] >> key) & 1)) ot[n][db][c] += v;
+            }
+      __builtin_amdgcn_wave_barrier();   // and the reads ahead of the next tile's stores
+    }
+
+    // ---- the waves' results meet in LDS (the value tiles are reused)
+    __syncthreads();
+    float* mo = (float*)few_smem;          // [NW][R][OP]
+    float* mml = mo + NW * R * OP;         // [NW][R][2]
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      const float l = rows4_sum(l_run[n]);
+      float* orow = mo + (wave * R + 16 * n + l16) * OP;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) *(f32x4*)(orow + 16 * db + 4 * g) = ot[n][db];
+      if (g == 0) {
+        mml[(wave * R + 16 * n + l16) * 2] = m_run[n];
+        mml[(wave * R + 16 * n + l16) * 2 + 1] = l;
+      }
+    }
+    __syncthreads();
+    constexpr int TPR = D / 4;             // threads per row, four elements each
+    for (int row = tid / TPR; row < M; row += NT / TPR) {
+      const int d = 4 * (tid % TPR);
+      float m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) m = fmaxf(m, mml[(w * R + row) * 2]);
+      const float m_use = m == -INFINITY ? 0.f : m;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float f = fast_exp2(mml[(w * R + row) * 2] - m_use);
+        l += f * mml[(w * R + row) * 2 + 1];
+        const f32x4 x = *(const f32x4*)(mo + (w * R + row) * OP + d);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] = fmaf(f, x[c], o[c]);
+      }
+      const long long at = (long long)(lo + row / G) * a.n_heads + kvh * G + row % G;
+      if (p.parts > 1) {
+        const long long w = (long long)part * a.n_tokens * a.n_heads + at;
+        *(f32x4*)(p.ws_o + w * D + d) = o;
+        if (d == 0) { p.ws_ml[w * 2] = m; p.ws_ml[w * 2 + 1] = l; }
+      } else {
+        const float inv = 1.f / l;
+        uint2 x;
+        x.x = pack_bf16x2(o[0] * inv, o[1] * inv);
+        x.y = pack_bf16x2(o[2] * inv, o[3] * inv);
+        *(uint2*)((uint16_t*)a.out + at * D + d) = x;
+        if (d == 0 && a.lse) a.lse[at] = m * LN2 + logf(l);
+      }
+    }
+    __syncthreads();   // the next part's values go where the results were
+  }
+}
+
+// Joins the parts: D / 4 lanes per (token, query head).  Rows that have fewer parts, or that could not be computed, left empty ones (l = 0).
+template <typename T>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedParams p) {
+  const paged_attn_args& a = p.a;
+  const int D = a.head_dim, LPR = (D + 3) / 4;
+  const long long rows = (long long)a.n_tokens * a.n_heads;
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / LPR;
+  const int d = 4 * (int)(at - row * LPR);
+  if (row >= rows) return;
+  const long long first = a.q_off[0], last = a.q_off[a.n_rows];
+  if (row < first * a.n_heads || row >= last * a.n_heads) return;   // tokens of no row
+  float m = -INFINITY, l = 0.f;
+  for (int c = 0; c < p.parts; ++c) m = fmaxf(m, p.ws_ml[(c * rows + row) * 2]);
+  const float m_use = m == -INFINITY ? 0.f : m;
+  float o[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < p.parts; ++c) {
+    const float mc = p.ws_ml[(c * rows + row) * 2], lc = p.ws_ml[(c * rows + row) * 2 + 1];
+    if (lc == 0.f) continue;   // empty: nothing was written but this
+    const float f = fast_exp2(mc - m_use);
+    l += f * lc;
+    const float* x = p.ws_o + (c * rows + row) * D + d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (d + i < D) o[i] = fmaf(f, x[i], o[i]);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* out = (T*)a.out + row * D + d;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (d + i < D) {
+      if constexpr (sizeof(T) == 2) out[i] = f32_to_bf16_bits(o[i] * inv);
+      else out[i] = o[i] * inv;
+    }
+  if (d == 0 && a.lse) a.lse[row] = m * LN2 + logf(l);
+}
 
 // One wave per (token, query head): a lane takes a key of 64, then head elements.
 template <typename T>
@@ -123,6 +647,69 @@ __global__ __launch_bounds__(256) void paged_attn_simple_kernel(PagedParams p) {
   if (lane == 0 && a.lse) a.lse[at] = m * LN2 + logf(l);
 }
 
+// ----------------------------------------------------------------------------------------------------------------------- launches
+// Kernels ask for more LDS than a launch may have by default: said once per kernel and device.
+template <auto KERNEL>
+hipError_t allow_lds(int bytes, int device) {
+  static std::atomic<u64> done{0};
+  const u64 bit = 1ull << (device & 63);
+  if (device < 64 && (done.load(std::memory_order_relaxed) & bit)) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+struct Cut {
+  int kind;         // 0: few query rows
+  int nq;           // query rows of a wave, in sixteens
+  int parts, part_tiles;
+};
+
+int tiles_bound(const paged_attn_args* a) {
+  const int n = (a->max_new + KT - 1) / KT;
+  int t = (a->max_prefix_len + KT - 1) / KT;
+  if (a->window > 0) {
+    const int64_t w = ((int64_t)a->window + KT - 2) / KT + 1 + ((int64_t)a->n_sink + KT - 1) / KT;   // a window's tiles, wherever it begins, and the sinks'
+    if (w < t) t = (int)w;
+  }
+  return t + n;
+}
+
+size_t part_bytes(const paged_attn_args* a) { return (size_t)a->n_tokens * a->n_heads * (a->head_dim + 2) * sizeof(float); }
+
+Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
+  Cut c = {1, 1, 1, 1};
+  if (a->dtype != CASCADE_BF16) return c;
+  const int64_t M = (int64_t)a->max_new * (a->n_heads / a->n_kv_heads);
+  if (M > 32) return c;
+  c.kind = 0;
+  c.nq = M <= 16 ? 1 : 2;
+  const int64_t heads = (int64_t)a->n_rows * a->n_kv_heads;
+  const int tiles = tiles_bound(a), most = (int)std::min<size_t>(ws_bytes / part_bytes(a), 64);
+  int parts = std::max(1, std::min({most, tiles / 8, (int)((2 * n_cu + heads - 1) / heads)}));
+  if (heads >= 2 * n_cu && tiles > 32) parts = std::max(1, std::min(most, tiles / 8));
+  c.part_tiles = (tiles + parts - 1) / parts;
+  c.parts = (tiles + c.part_tiles - 1) / c.part_tiles;
+  return c;
+}
+
+template <int D, int NQ, int NW, bool TREE>
+hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
+  constexpr int v_bytes = NW * KT * (D + 16) * 2, o_bytes = NW * 16 * NQ * (D + 4 + 2) * 4, smem = v_bytes > o_bytes ? v_bytes : o_bytes;
+  constexpr auto kern = paged_few_kernel<D, NQ, NW, TREE>;
+  hipError_t e = allow_lds<kern>(smem, ctx->device);
+  if (e != hipSuccess) return e;
+  const int64_t items = (int64_t)p.a.n_rows * p.a.n_kv_heads * p.parts, slots = (int64_t)ctx->n_cu * (8 / NW);
+  KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
+  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)std::min(items, slots)), dim3(64 * NW), smem, ctx->stream, p);
+  return hipGetLastError();
+}
+template <int D>
+hipError_t launch_few(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
+  if (p.a.parent) return c.nq == 1 ? launch_few_k<D, 1, 4, true>(ctx, p) : launch_few_k<D, 2, 4, true>(ctx, p);
+  return c.nq == 1 ? launch_few_k<D, 1, 4, false>(ctx, p) : launch_few_k<D, 2, 4, false>(ctx, p);
+}
+
 }  // namespace
 
 hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
@@ -131,11 +718,34 @@ hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
   p.group = a->n_heads / a->n_kv_heads;
   p.scale_log2e = (a->scale != 0.f ? a->scale : 1.f / sqrtf((float)a->head_dim)) * LOG2E;
   p.dev_status = ctx->dev_status;
-  const unsigned grid = (unsigned)(((long long)a->n_tokens * a->n_heads + 3) / 4);
-  KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
-  if (a->dtype == CASCADE_BF16) CASCADE_TIMED_LAUNCH(t, paged_attn_simple_kernel<uint16_t>, dim3(grid), dim3(256), 0, ctx->stream, p);
-  else CASCADE_TIMED_LAUNCH(t, paged_attn_simple_kernel<float>, dim3(grid), dim3(256), 0, ctx->stream, p);
+  p.page16 = a->page_size / 16;
+  p.page16_inv = p.page16 == 1 ? 0u : (unsigned)((1ull << 32) / p.page16 + 1);
+  char* ws = a->workspace ? (char*)a->workspace : ctx->attn_ws;
+  size_t ws_bytes = a->workspace ? (size_t)a->workspace_bytes : (recorded(ctx->stream) ? 0 : ctx->attn_ws_bytes);
+  const Cut c = choose(a, ctx->n_cu, ws_bytes);
+  p.parts = c.parts;
+  p.part_tiles = c.part_tiles;
+  p.ws_o = (float*)ws;
+  p.ws_ml = (float*)ws + (size_t)c.parts * a->n_tokens * a->n_heads * a->head_dim;
+  if (c.kind == 0) {
+    hipError_t e = a->head_dim == 128 ? launch_few<128>(ctx, p, c) : launch_few<64>(ctx, p, c);
+    if (e != hipSuccess) return e;
+  } else {
+    const unsigned grid = (unsigned)(((long long)a->n_tokens * a->n_heads + 3) / 4);
+    KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
+    if (a->dtype == CASCADE_BF16) CASCADE_TIMED_LAUNCH(t, paged_attn_simple_kernel<uint16_t>, dim3(grid), dim3(256), 0, ctx->stream, p);
+    else CASCADE_TIMED_LAUNCH(t, paged_attn_simple_kernel<float>, dim3(grid), dim3(256), 0, ctx->stream, p);
+  }
+  if (c.parts > 1) {
+    const long long lanes = (long long)a->n_tokens * a->n_heads * ((a->head_dim + 3) / 4);
+    KernelTimer t(ctx, CASCADE_K_PAGED_MERGE);
+    if (a->dtype == CASCADE_BF16) CASCADE_TIMED_LAUNCH(t, paged_merge_kernel<uint16_t>, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, ctx->stream, p);
+    else CASCADE_TIMED_LAUNCH(t, paged_merge_kernel<float>, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, ctx->stream, p);
+  }
   return hipGetLastError();
 }
 
-int64_t plan_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a) { return 0; }
+int64_t plan_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a) {
+  const Cut c = choose(a, ctx->n_cu, (size_t)1 << 40);
+  return c.parts > 1 ? (int64_t)c.parts * (int64_t)part_bytes(a) : 0;
+}
