@@ -494,6 +494,7 @@ static int check_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a) {
   if (a->dtype == CASCADE_BF16) {
     if (a->head_dim != 64 && a->head_dim != 128) return CASCADE_ESHAPE;
     if ((a->stride_page | a->stride_head | a->stride_pos | a->q_stride | a->kv_stride) % 8) return CASCADE_ESHAPE;
+    if (a->stride_pos > (1 << 25) || a->kv_stride > (1 << 25)) return CASCADE_ESHAPE;   // sixteen keys lie within 32-bit offsets
     if (((uintptr_t)a->q | (uintptr_t)a->k_new | (uintptr_t)a->v_new | (uintptr_t)a->k_pages | (uintptr_t)a->v_pages | (uintptr_t)a->out) & 15)
       return CASCADE_EINVAL;
   } else if (a->head_dim > 256) {

@@ -501,6 +501,511 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedParams p) {
   }
 }
 
+// ------------------------------------------------------------------------------------------------------- bf16, many query rows
+// Workgroup = (16 NQ NW query rows of a row of the batch, kv head, part of their tiles): its waves share every tile of 64 keys.  Tiles never pass through registers on
+// their way in: LDS-direct loads (global_load_lds_dwordx4, M0 = the LDS address of a wave's 1 KiB) write them into two rings of NS tiles, NS - 1 ahead of
+// their use; a wave waits for its own loads of the tile needed next (vmcnt), then one bare barrier per tile makes everybody's visible and
+// the oldest place free.  Such a load puts lane l's 16 bytes at 16 l, so rows cannot be padded; bank conflicts are avoided by WHICH 16-byte piece of a key a lane fetches:
+// slot q of key r holds piece q ^ swz(r).  The products of the next tile's scores stand between the exponentials of this one.  The reference of the exponentials
+// moves when a row's maximum has grown by more than 2^8: the result does not depend on it, and the rescaling becomes a rare branch.
+//
+// A wave's rows of a tile (8 or 16) lie in one group of 16 keys, so their page is one entry of the table.  The workgroup keeps the entries of its part in LDS, as
+// many as fit, and reads the one for the next tile a tile ahead.
+template <int D>
+struct RingGeom {
+  static constexpr int RB = 2 * D;        // bytes per key
+  static constexpr int PPR = RB / 16;     // 16-byte pieces per key
+  static constexpr int RPC = 1024 / RB;   // keys per 1 KiB (one wave-wide load)
+  static constexpr int CPT = KT / RPC;    // such loads per tile
+  static constexpr int TILE = KT * RB;
+  __device__ static constexpr int kswz(int key) { return D == 128 ? (key & 15) : ((key >> 1) & 7); }
+  __device__ static constexpr int vswz(int key) { return D == 128 ? 2 * (key & 7) : 2 * ((key >> 1) & 3); }
+};
+
+constexpr float RESCALE_STEP = 8.f;      // log2 units
+constexpr int STAGED = 2048;             // entries of the table in LDS
+
+// LDS behind the rings: parents and depths (trees), two tiles' ancestor words (trees), entries of the table
+template <int D, int NS, int NQ, int NW, bool TREE>
+constexpr int ring_lds() {
+  return 2 * NS * RingGeom<D>::TILE + (TREE ? CASCADE_MAX_TREE * 6 + 2 * 16 * NQ * NW * 8 : 0) + STAGED * 4;
+}
+
+template <int N>
+__device__ __forceinline__ void wait_and_sync() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// maxima of products' results: an operation that the compiler sees, so that it keeps the distance that the matrix cores ask for
+__device__ __forceinline__ float vmax2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float vmax3(float a, float b, float c) { return vmax2(vmax2(a, b), c); }
+__device__ __forceinline__ float rows4_max_raw(float v) {
+  cascade_u32x2 a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = vmax2(__uint_as_float(a.x), __uint_as_float(a.y));
+  cascade_u32x2 b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return vmax2(__uint_as_float(b.x), __uint_as_float(b.y));
+}
+
+// Block `blk` of the launch: a run of query rows of a row of the batch.  Rows are taken longest first (up to 64 of them), a row's blocks from its end, where a chain sees most.
+__device__ __forceinline__ RowInfo block_row(const PagedParams& p, int blk, int rows_per_block, int lane, int* sb) {
+  const paged_attn_args& a = p.a;
+  RowInfo none = {-1, 0, 0, 0, 0};
+  for (int base = 0; base < a.n_rows; base += 64) {
+    const int at = base + lane;
+    RowInfo mine = {at, 0, 0, 0, 0};
+    int nb = 0;
+    if (at < a.n_rows) {
+      mine = check_row(p, at, a.q_off[at], a.q_off[at + 1], a.prefix_len[at]);
+      nb = mine.flag ? 1 : (mine.T * p.group + rows_per_block - 1) / rows_per_block;
+    }
+    int from = lane;   // the lane whose row stands at this lane's place
+    if (a.n_rows > 1 && a.n_rows <= 64) {
+      const int work = at < a.n_rows ? (mine.flag ? 0 : mine.P + mine.T) : -1;
+      int rank = 0;
+      for (int r = 0; r < 64; ++r) {
+        const int w = __builtin_amdgcn_readlane(work, r);
+        rank += (w > work || (w == work && r < lane)) ? 1 : 0;
+      }
+      from = __builtin_amdgcn_ds_permute(4 * rank, lane);
+      nb = __builtin_amdgcn_ds_bpermute(4 * from, nb);
+    }
+    const int incl = wave_scan_incl_i(nb);
+    const u64 who = __ballot(blk < incl);
+    if (who) {
+      const int l = __ffsll((long long)who) - 1, src = __builtin_amdgcn_readlane(from, l), n = __builtin_amdgcn_readlane(nb, l);
+      blk -= __builtin_amdgcn_readlane(incl, l) - n;
+      *sb = n - 1 - blk;
+      RowInfo r = {base + src, __builtin_amdgcn_readlane(mine.lo, src), __builtin_amdgcn_readlane(mine.T, src), __builtin_amdgcn_readlane(mine.P, src),
+                   __builtin_amdgcn_readlane(mine.flag, src)};
+      return r;
+    }
+    blk -= __builtin_amdgcn_readlane(incl, 63);
+  }
+  return none;
+}
+
+template <int D, int NS, int NQ, int NW, bool TREE>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_ring_kernel(PagedParams p) {
+  using GM = RingGeom<D>;
+  constexpr int NT = 64 * NW, RW = 16 * NQ * NW, KS = D / 32, DB = D / 16;
+  constexpr int CPW = GM::CPT / NW;     // loads of K (and of V) that a wave makes per tile
+  constexpr int LPI = 2 * CPW;
+  static_assert(GM::CPT % NW == 0 && CPW * GM::RPC <= 16 && (NS == 2 || NS == 3), "a wave's keys lie in one group of 16");
+  extern __shared__ __align__(1024) char ring_smem[];
+  char* const smem_raw = ring_smem;
+  int* s_parent = (int*)(smem_raw + 2 * NS * GM::TILE);
+  uint16_t* s_depth = (uint16_t*)(s_parent + CASCADE_MAX_TREE);
+  u64* s_anc = (u64*)(s_depth + CASCADE_MAX_TREE);
+  int* s_page = TREE ? (int*)(s_anc + 2 * RW) : s_parent;
+  const paged_attn_args& a = p.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g = lane >> 4, G = p.group, H = a.n_kv_heads;
+
+  // Workgroups are dealt round-robin to the 8 XCDs, one L2 each: those of a kv head stay on one XCD (or on 8 / H of them), where the blocks of a row meet in its keys.
+  int kvh, b;
+  {
+    const int h = blockIdx.x, x = h & 7, k = h >> 3;
+    if (H % 8 == 0) { const int m = H >> 3; kvh = x + 8 * (k % m); b = k / m; }
+    else if (8 % H == 0 && (gridDim.x & 7) == 0) { kvh = x % H; b = k * (8 / H) + x / H; }
+    else { kvh = h % H; b = h / H; }
+  }
+  const int part = b % p.parts;
+  int sb = 0;
+  const RowInfo ri = block_row(p, b / p.parts, RW, lane, &sb);
+  if (ri.s < 0) return;   // the grid is an upper bound of the number of blocks
+  if (ri.flag) { write_nothing<uint16_t>(p, ri, kvh, part, tid, NT); return; }
+  const int lo = ri.lo, T = ri.T, P = ri.P, M = T * G, row0 = sb * RW;
+  const int i0 = row0 / G, i1 = (min(row0 + RW, M) - 1) / G;
+  const Tiles ti = tiles_of(p, P, i0, i1, TREE);
+  const int nt = ti.n_p + ti.n_n, per = (nt + p.parts - 1) / p.parts, t_begin = part * per, t_end = min(nt, t_begin + per);
+  const long long all_rows = (long long)a.n_tokens * a.n_heads;
+  if (t_begin >= t_end) {   // fewer tiles than parts: an empty one
+    for (int r = row0 + tid; r < min(row0 + RW, M); r += NT) {
+      float* ml = p.ws_ml + (part * all_rows + (long long)(lo + r / G) * a.n_heads + kvh * G + r % G) * 2;
+      ml[0] = -INFINITY;
+      ml[1] = 0.f;
+    }
+    return;
+  }
+
+  // ---- loader: load i of a wave is 1 KiB c = CPW wave + i of a tile; lane -> key c RPC + lane / PPR, LDS slot lane % PPR
+  const unsigned pitch_p = (unsigned)(a.stride_pos * 2), pitch_n = (unsigned)(a.kv_stride * 2);
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(size_t)smem_raw);
+  const int wave_group = CPW * GM::RPC * wave / 16;   // the group of 16 keys of a tile that the wave's keys lie in
+  int ld_row[CPW];                                    // key in that group
+  unsigned ld_kpiece[CPW], ld_vpiece[CPW], ld_kfull[CPW], ld_vfull[CPW];
+#pragma unroll
+  for (int i = 0; i < CPW; ++i) {
+    const int r = (CPW * wave + i) * GM::RPC + lane / GM::PPR, q = lane % GM::PPR;
+    ld_row[i] = r & 15;
+    ld_kpiece[i] = 16u * (unsigned)(q ^ GM::kswz(r));
+    ld_vpiece[i] = 16u * (unsigned)(q ^ GM::vswz(r));
+    ld_kfull[i] = (unsigned)(r & 15) * pitch_p + ld_kpiece[i];
+    ld_vfull[i] = (unsigned)(r & 15) * pitch_p + ld_vpiece[i];
+  }
+  // Where the wave's keys of a tile come from: the first key of their group, and how many keys are behind it.  Tiles past the part's end are its
+  // last one again (the number of loads stays fixed; what they bring is not used), keys past the end are the last one again, masked.
+  struct Source {
+    long long off;   // bytes from k_pages / v_pages, or from the row's new keys / values
+    int last;        // keys of the group behind the first
+    bool fresh;
+  };
+  const int e0 = ti.n_p > 0 ? page_index(p, 4 * min(ti.prefix_tile(max(min(t_begin, ti.n_p - 1), ti.sinks_p)), (P - 1) / KT)) : 0;
+  const int n_staged = ti.n_p > 0 ? min(STAGED, page_index(p, (P - 1) >> 4) + 1 - e0) : 0;
+  auto group_of = [&](int t) { return needed_group(p, ti, P, 4 * ti.prefix_tile(t) + wave_group); };   // t < n_p
+  auto source_of = [&](int t, int page) {
+    Source s;
+    s.fresh = t >= ti.n_p;
+    if (!s.fresh) {
+      const int gq = group_of(t);
+      s.off = 2 * group_offset(p, checked_page(p, page), page_index(p, gq), gq, kvh);
+      s.last = P - 1 - 16 * gq;
+    } else {
+      const int gq = min(4 * ti.new_tile(t - ti.n_p) + wave_group, (T - 1) >> 4);
+      s.off = (long long)(16 * gq) * pitch_n;
+      s.last = T - 1 - 16 * gq;
+    }
+    return s;
+  };
+  auto entry_now = [&](int t) { return t < ti.n_p ? table_entry(p, ri.s, page_index(p, group_of(t))) : 0; };
+  auto entry_staged = [&](int t) {
+    if (t >= ti.n_p) return 0;
+    const int e = page_index(p, group_of(t)), at = e - e0;
+    return at >= 0 && at < n_staged ? s_page[at] : table_entry(p, ri.s, e);
+  };
+  const char *kc = (const char*)a.k_pages, *vc = (const char*)a.v_pages;
+  const char* kn = (const char*)((const uint16_t*)a.k_new + lo * a.kv_stride + kvh * D);
+  const char* vn = (const char*)((const uint16_t*)a.v_new + lo * a.kv_stride + kvh * D);
+  auto request = [&](const Source& s, int stage, bool is_v) {
+    const unsigned ldst = lds0 + (is_v ? NS * GM::TILE : 0) + stage * GM::TILE + CPW * wave * 1024;
+    const uintptr_t at = (uintptr_t)((s.fresh ? (is_v ? vn : kn) : (is_v ? vc : kc)) + s.off);
+    const char* src = (const char*)(((u64)(unsigned)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)at));
+    if (!s.fresh && s.last >= 15) {   // whole: the lanes' offsets are constants
+#pragma unroll
+      for (int i = 0; i < CPW; ++i) {
+        const unsigned l = ldst + i * 1024;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(l), "v"(is_v ? ld_vfull[i] : ld_kfull[i]), "s"(src) : "memory");
+      }
+    } else {
+      const unsigned pitch = s.fresh ? pitch_n : pitch_p;
+#pragma unroll
+      for (int i = 0; i < CPW; ++i) {
+        const unsigned l = ldst + i * 1024, off = (unsigned)min(ld_row[i], s.last) * pitch + (is_v ? ld_vpiece[i] : ld_kpiece[i]);
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(l), "v"(off), "s"(src) : "memory");
+      }
+    }
+  };
+
+  // ---- prologue: K of the first tile, then the steady order K(t + NS), V(t + NS - 1)
+  auto clamped = [&](int t) { return min(t, t_end - 1); };
+  Source before;   // the tile whose V is requested next
+  before = source_of(t_begin, entry_now(t_begin));
+  request(before, 0, false);
+#pragma unroll
+  for (int i = 1; i < NS; ++i) {
+    const int t = clamped(t_begin + i);
+    const Source s = source_of(t, entry_now(t));
+    request(s, i, false);
+    request(before, i - 1, true);
+    before = s;
+  }
+  // what else the loop needs in LDS
+  for (int i = tid; i < n_staged; i += NT) s_page[i] = a.block_table[ri.s * a.table_stride + e0 + i];
+  if (TREE) {
+    for (int i = tid; i < T; i += NT) {
+      int pi = a.parent[lo + i];
+      if (i == 0 ? pi != -1 : (pi >= i || pi < 0)) {
+        atomicOr(p.dev_status, CASCADE_FLAG_PARENT);
+        pi = i == 0 ? -1 : 0;   // keeps the climb finite
+      }
+      s_parent[i] = pi;
+    }
+  }
+  // query fragments (B operand of S^T): lane = (query l16, d group g)
+  Frag8 qf[NQ][KS];
+  int qi[NQ];            // the token, -1 behind the last
+  long long out_row[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int r = row0 + 16 * (wave + NW * n) + l16;
+    const bool ok = r < M;
+    const int i = ok ? r / G : 0, hg = ok ? r - i * G : 0;
+    qi[n] = ok ? i : -1;
+    out_row[n] = (long long)(lo + i) * a.n_heads + kvh * G + hg;
+    const uint16_t* qp = (const uint16_t*)a.q + (lo + i) * a.q_stride + (kvh * G + hg) * D + 8 * g;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if (ok) qf[n][ks].u = *(const uint4*)(qp + 32 * ks);
+      else qf[n][ks].u = make_uint4(0, 0, 0, 0);
+    }
+  }
+  f32x4 ot[NQ][DB];
+  f32x4 lsum[NQ];        // row sums of the (bf16) probabilities, from the matrix cores: every entry holds the sum
+  float m_ref[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    m_ref[n] = -INFINITY;
+    lsum[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int db = 0; db < DB; ++db) ot[n][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  Frag8 ones;
+  ones.u = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+
+  // ---- LDS addresses (see the comment on slots): K fragment (kt, ks): key 16 kt + l16, piece 4 ks + g; V operand (db, j): keys 32 j + 4 g + (l16 >> 2)
+  // (+ 16), four d at 16 db + 4 (l16 & 3).  ks and db enter by XOR, the stage, kt and j are constants.
+  const unsigned k_lane = (unsigned)(l16 * GM::RB) + 16u * (unsigned)(g ^ GM::kswz(l16));
+  const int vkey = 4 * g + (l16 >> 2);
+  const unsigned v_lane = (unsigned)(vkey * GM::RB) + ((16u * (unsigned)((l16 & 3) >> 1)) ^ (16u * (unsigned)GM::vswz(vkey))) + 8u * (unsigned)(l16 & 1);
+  const char* k_addr[KS];
+  const char* v_addr[DB];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) k_addr[ks] = smem_raw + (k_lane ^ (unsigned)(64 * ks));
+#pragma unroll
+  for (int db = 0; db < DB; ++db) v_addr[db] = smem_raw + NS * GM::TILE + (v_lane ^ (unsigned)(32 * db));
+
+  f32x4 st[NQ][4];   // scores: st[n][kt] holds keys 16 kt + 4 g + c for query l16
+  auto load_kfrags = [&](Frag8 (&kf)[KS], int stage, int kt) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kf[ks].u = *(const uint4*)(k_addr[ks] + stage * GM::TILE + 16 * kt * GM::RB);
+  };
+  auto score_kt = [&](const Frag8 (&kf)[KS], int kt) {
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) st[n][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) st[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks].v, qf[n][ks].v, st[n][kt], 0, 0, 0);
+  };
+  union VFrag { Frag8 f; s16x4 h[2]; };
+  auto load_vfrag = [&](VFrag& vf, int stage, int i) {   // step i = (db, j) = (i / 2, i % 2)
+    const char* vp = v_addr[i >> 1] + stage * GM::TILE + 32 * (i & 1) * GM::RB;
+    vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(vp));
+    vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(vp + 16 * GM::RB));
+  };
+  auto lane_max = [&](int n) {
+    float x = vmax3(st[n][0][0], st[n][0][1], st[n][0][2]);
+    x = vmax3(x, st[n][0][3], st[n][1][0]);
+    x = vmax3(x, st[n][1][1], st[n][1][2]);
+    x = vmax3(x, st[n][1][3], st[n][2][0]);
+    x = vmax3(x, st[n][2][1], st[n][2][2]);
+    x = vmax3(x, st[n][2][3], st[n][3][0]);
+    x = vmax3(x, st[n][3][1], st[n][3][2]);
+    return vmax2(x, st[n][3][3]);
+  };
+
+  __syncthreads();                    // parents and entries complete
+  int q_depth[NQ];                    // position of the query behind the prefix
+  if (TREE) {
+    if (a.window > 0) {
+      for (int i = tid; i < T; i += NT) {
+        int d = 0;
+        for (int x = s_parent[i]; x >= 0; x = s_parent[x]) ++d;
+        s_depth[i] = (uint16_t)d;
+      }
+      __syncthreads();
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) q_depth[n] = TREE ? (a.window > 0 ? s_depth[max(qi[n], 0)] : 0) : qi[n];
+  // trees: which nodes of new tile t each of the workgroup's query rows sees
+  auto build_mask = [&](int t) {
+    if (tid < RW) {
+      const int kb = (t - ti.n_p) * KT, r = row0 + tid;
+      u64 bits = 0;
+      if (r < M) {
+        int x = r / G;
+        const int reach = a.window > 0 ? s_depth[x] - a.window + 1 : 0, sinks = a.n_sink - P;   // depths seen: from `reach` on, and below `sinks`
+        while (x >= kb) {   // kb >= 0; ancestors only get smaller
+          if (x - kb < 64 && (a.window == 0 || s_depth[x] >= reach || (int)s_depth[x] < sinks)) bits |= 1ull << (x - kb);
+          x = s_parent[x];
+        }
+      }
+      s_anc[(t & 1) * RW + tid] = bits;
+    }
+  };
+  if (TREE && t_begin >= ti.n_p) build_mask(t_begin);
+  int entry = entry_staged(clamped(t_begin + NS));
+  wait_and_sync<LPI * (NS - 1)>();    // K of the first tile everywhere (and the first mask)
+  float lmax[NQ];                     // lane_max of the scores in st
+  {
+    Frag8 kf[2][KS];
+    load_kfrags(kf[0], 0, 0);
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+      if (kt < 3) load_kfrags(kf[(kt + 1) & 1], 0, kt + 1);
+      score_kt(kf[kt & 1], kt);
+    }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) lmax[n] = lane_max(n);
+  }
+
+  auto tile_step = [&](int t, auto st_const) {
+    constexpr int ST = decltype(st_const)::value;
+    constexpr int ST_K = (ST + 1) % NS;             // stage of K(t+1)
+    constexpr int ST_VNEW = (ST + NS - 1) % NS;     // V(t + NS - 1) goes where V(t - 1) was
+    wait_and_sync<LPI * (NS - 2)>();   // K(t+1), V(t) landed everywhere; K(t), V(t-1) free
+    {
+      const Source s = source_of(clamped(t + NS), __builtin_amdgcn_readfirstlane(entry));
+      request(s, ST, false);
+      request(before, ST_VNEW, true);
+      before = s;
+    }
+    Frag8 kf[2][KS];
+    load_kfrags(kf[0], ST_K, 0);       // in flight during the reference check
+    entry = entry_staged(clamped(t + NS + 1));
+    if (TREE && t + 1 < t_end && t + 1 >= ti.n_p) build_mask(t + 1);   // read behind the next barrier
+
+    // ---- masks
+    const bool fresh = t >= ti.n_p;
+    const int kb = fresh ? ti.new_tile(t - ti.n_p) * KT : ti.prefix_tile(t) * KT;
+    const int far = fresh ? i1 : P + i1;             // no query's position is behind this one
+    const bool cut = a.window > 0 && kb < far - a.window + 1 && kb + KT > a.n_sink - (fresh ? P : 0);
+    const bool mixed = (fresh && (TREE || kb + KT - 1 > i0)) || cut;   // some queries see less of it than others
+    if (mixed || (!fresh && kb + KT > P)) {
+      u64 valid[NQ];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        if (fresh) valid[n] = TREE ? s_anc[(t & 1) * RW + 16 * (wave + NW * n) + l16] : sees_chain(p, P, kb, qi[n]);
+        else valid[n] = sees_prefix(p, P, kb, P + q_depth[n]);
+        if (qi[n] < 0) valid[n] = 0;
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+          const uint32_t nib = (uint32_t)(valid[n] >> (16 * kt + 4 * g));   // this lane's 4 keys of sub-tile kt
+#pragma unroll
+          for (int c = 0; c < 4; ++c) st[n][kt][c] = ((nib >> c) & 1u) ? st[n][kt][c] : -INFINITY;
+        }
+        lmax[n] = lane_max(n);
+      }
+      if (mixed) {
+        // infinities and NaN among values that not every query sees (every wave looks through the whole tile, so all agree)
+        uint32_t odd = 0;
+        char* const vt = smem_raw + NS * GM::TILE + ST * GM::TILE;
+#pragma unroll
+        for (int c = 0; c < GM::CPT; ++c) {
+          const uint4 x = *(const uint4*)(vt + 1024 * c + 16 * lane);
+          odd |= odd_exponent(x.x) | odd_exponent(x.y) | odd_exponent(x.z) | odd_exponent(x.w);
+        }
+        if (__any((odd & 0x80008000u) != 0)) {   // they go to the queries that see them, and out of the tile
+          for (int key = 0; key < KT; ++key)
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const float v = bf16_bits_to_f32(*(const uint16_t*)(vt + key * GM::RB + 16 * ((2 * db + (g >> 1)) ^ GM::vswz(key)) + 8 * (g & 1) + 2 * c));
+                const bool is_odd = !(fabsf(v) < INFINITY);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+                  if (is_odd && ((valid[n] >> key) & 1)) ot[n][db][c] += v;
+              }
+          __syncthreads();
+          for (int c = tid; c < GM::TILE / 16; c += NT) {
+            uint4* at = (uint4*)(vt + 16 * c);
+            *at = make_uint4(finite_only(at->x), finite_only(at->y), finite_only(at->z), finite_only(at->w));
+          }
+          __syncthreads();
+        }
+      }
+    }
+    // ---- the reference of the exponentials: a lane sees 16 of its row's 64 scores; if none of the wave's lanes exceeds its row's by more than the step, no row does
+    bool moved = false;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) moved |= lmax[n] * p.scale_log2e > m_ref[n] + RESCALE_STEP;   // -inf + 8 = -inf: a first finite score always moves it
+    if (__ballot(moved) != 0ull) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const float mx = rows4_max_raw(lmax[n]) * p.scale_log2e;
+        const float m_new = (mx > m_ref[n] + RESCALE_STEP) ? mx : m_ref[n];
+        const float use_new = (m_new == -INFINITY) ? 0.f : m_new;
+        const float alpha = fast_exp2(m_ref[n] - use_new);   // -inf - finite = -inf -> 0 ; equal -> 1
+        lsum[n] *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) ot[n][db] *= alpha;
+        m_ref[n] = m_new;
+      }
+    }
+    float m_neg[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) m_neg[n] = (m_ref[n] == -INFINITY) ? 0.f : -m_ref[n];
+
+    // ---- probabilities of tile t (B operand of the second product), between them the scores of tile t+1 over the same registers
+    Frag8 pf[NQ][2];
+    auto probs_kt = [&](int kt) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        float e[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) e[c] = fast_exp2(fmaf(st[n][kt][c], p.scale_log2e, m_neg[n]));   // -inf stays -inf -> 0
+        const uint32_t lo2 = pack_bf16x2(e[0], e[1]), hi2 = pack_bf16x2(e[2], e[3]);
+        if (kt & 1) { pf[n][kt >> 1].u.z = lo2; pf[n][kt >> 1].u.w = hi2; }
+        else { pf[n][kt >> 1].u.x = lo2; pf[n][kt >> 1].u.y = hi2; }
+      }
+    };
+    constexpr int NVS = 2 * DB, VW = 4;   // V steps per tile, steps whose fragments are requested ahead
+    VFrag vf[VW];
+    probs_kt(0);
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+      if (kt < 3) load_kfrags(kf[(kt + 1) & 1], ST_K, kt + 1);
+      else {
+#pragma unroll
+        for (int i = 0; i < VW; ++i) load_vfrag(vf[i], ST, i);
+        __builtin_amdgcn_sched_barrier(0);   // left alone, every V read sinks to its product
+      }
+      score_kt(kf[kt & 1], kt);
+      if (kt < 3) probs_kt(kt + 1);
+    }
+    // ---- O^T += V^T P^T, row sums += ones P^T; the vector ALU meanwhile looks at the next tile's scores
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) lsum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones.v, pf[n][j].v, lsum[n], 0, 0, 0);
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) lmax[n] = lane_max(n);
+#pragma unroll
+    for (int i = 0; i < NVS; ++i) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) ot[n][i >> 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i % VW].f.v, pf[n][i & 1].v, ot[n][i >> 1], 0, 0, 0);
+      if (i + VW < NVS) load_vfrag(vf[i % VW], ST, i + VW);
+      __builtin_amdgcn_sched_barrier(0);   // keeps the read of step i + VW here, VW steps ahead of its use
+    }
+  };
+  for (int t = t_begin; t < t_end; t += NS) {
+    tile_step(t, std::integral_constant<int, 0>{});
+    if (t + 1 >= t_end) break;
+    tile_step(t + 1, std::integral_constant<int, 1>{});
+    if constexpr (NS > 2) {
+      if (t + 2 >= t_end) break;
+      tile_step(t + 2, std::integral_constant<int, 2>{});
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the loads that nothing uses must not outlive the workgroup's LDS
+
+  // epilogue: lane (query l16, g) owns d = 16 db + 4 g + c
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    if (qi[n] < 0) continue;
+    const float l = lsum[n][0];
+    if (p.parts > 1) {
+      const long long w = part * all_rows + out_row[n];
+#pragma unroll
+      for (int db = 0; db < DB; ++db) *(f32x4*)(p.ws_o + w * D + 16 * db + 4 * g) = ot[n][db];
+      if (g == 0) { p.ws_ml[w * 2] = m_ref[n]; p.ws_ml[w * 2 + 1] = l; }
+      continue;
+    }
+    const float inv = 1.f / l;
+    uint16_t* o = (uint16_t*)a.out + out_row[n] * D;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      uint2 w;
+      w.x = pack_bf16x2(ot[n][db][0] * inv, ot[n][db][1] * inv);
+      w.y = pack_bf16x2(ot[n][db][2] * inv, ot[n][db][3] * inv);
+      *(uint2*)(o + 16 * db + 4 * g) = w;
+    }
+    if (g == 0 && a.lse) a.lse[out_row[n]] = m_ref[n] * LN2 + logf(l);
+  }
+}
+
 // Joins the parts: D / 4 lanes per (token, query head).  Rows that have fewer parts, or that could not be computed, left empty ones (l = 0).
 template <typename T>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedParams p) {
@@ -659,11 +1164,13 @@ hipError_t allow_lds(int bytes, int device) {
   return e;
 }
 
+// How a call is cut.  Shapes 0 and 1: few query rows, 16 or 32 of them; 2, 3, 4: workgroups of 64, 128, 256 query rows.
 struct Cut {
-  int kind;         // 0: few query rows
-  int nq;           // query rows of a wave, in sixteens
+  int shape;
   int parts, part_tiles;
 };
+constexpr int FEW_16 = 0, FEW_32 = 1, RING_64 = 2, RING_128 = 3, RING_256 = 4, OTHER = 5;
+constexpr int SHAPE_ROWS[] = {16, 32, 64, 128, 256};
 
 int tiles_bound(const paged_attn_args* a) {
   const int n = (a->max_new + KT - 1) / KT;
@@ -677,15 +1184,37 @@ int tiles_bound(const paged_attn_args* a) {
 
 size_t part_bytes(const paged_attn_args* a) { return (size_t)a->n_tokens * a->n_heads * (a->head_dim + 2) * sizeof(float); }
 
+// Estimated time of a cut of many query rows, us
+float ring_estimate_us(int shape, const paged_attn_args* a, int parts, int n_cu) {
+  constexpr struct { float c0, c1, c2, c2_hbm; } COST[] = {{1.0f, 1.0f, 1.5f, 3.0f}, {1.2f, 1.45f, 2.5f, 2.5f}, {1.7f, 2.3f, 2.3f, 2.3f}};
+  const auto& c = COST[shape - RING_64];
+  const int G = a->n_heads / a->n_kv_heads, rows = SHAPE_ROWS[shape];
+  const int n_sb = (int)(((int64_t)a->max_new * G + rows - 1) / rows);
+  float blocks = (float)a->n_rows * n_sb;
+  if (n_sb > 1) blocks = fminf(blocks, (float)a->n_tokens * G / rows + 0.5f * a->n_rows);
+  const float x = blocks * a->n_kv_heads * parts / n_cu, c2 = c.c2_hbm + (c.c2 - c.c2_hbm) * fminf(blocks / a->n_rows - 1.f, 1.f);
+  const float per_tile = x <= 1.f ? c.c0 + (c.c1 - c.c0) * x : (shape == RING_256 ? c.c1 * ceilf(x) : (x <= 2.f ? c.c1 + (c2 - c.c1) * (x - 1.f) : c2 * 0.5f * x));
+  float us = 7.4f + (float)((tiles_bound(a) + parts - 1) / parts) * per_tile * (a->head_dim == 64 ? 0.7f : 1.f);
+  if (parts > 1) us += 3.8f + 0.3f * parts + (float)parts * a->n_tokens * a->n_heads * (a->head_dim + 2) * 4.f / 7e6f;
+  return us;
+}
+
 Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
-  Cut c = {1, 1, 1, 1};
+  Cut c = {OTHER, 1, 1};
   if (a->dtype != CASCADE_BF16) return c;
   const int64_t M = (int64_t)a->max_new * (a->n_heads / a->n_kv_heads);
-  if (M > 32) return c;
-  c.kind = 0;
-  c.nq = M <= 16 ? 1 : 2;
-  const int64_t heads = (int64_t)a->n_rows * a->n_kv_heads;
   const int tiles = tiles_bound(a), most = (int)std::min<size_t>(ws_bytes / part_bytes(a), 64);
+  if (M > 32) {
+    float best = INFINITY;
+    for (int shape = RING_64; shape <= RING_256; ++shape)
+      for (int parts = 1; parts <= 16 && parts <= std::max(most, 1) && parts <= tiles; parts = parts < 4 ? parts + 1 : parts * 2) {
+        const float us = ring_estimate_us(shape, a, parts, n_cu);
+        if (us < best) { best = us; c.shape = shape; c.parts = parts; }
+      }
+    return c;
+  }
+  c.shape = M <= 16 ? FEW_16 : FEW_32;
+  const int64_t heads = (int64_t)a->n_rows * a->n_kv_heads;
   int parts = std::max(1, std::min({most, tiles / 8, (int)((2 * n_cu + heads - 1) / heads)}));
   if (heads >= 2 * n_cu && tiles > 32) parts = std::max(1, std::min(most, tiles / 8));
   c.part_tiles = (tiles + parts - 1) / parts;
@@ -706,8 +1235,36 @@ hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
 }
 template <int D>
 hipError_t launch_few(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
-  if (p.a.parent) return c.nq == 1 ? launch_few_k<D, 1, 4, true>(ctx, p) : launch_few_k<D, 2, 4, true>(ctx, p);
-  return c.nq == 1 ? launch_few_k<D, 1, 4, false>(ctx, p) : launch_few_k<D, 2, 4, false>(ctx, p);
+  if (p.a.parent) return c.shape == FEW_16 ? launch_few_k<D, 1, 4, true>(ctx, p) : launch_few_k<D, 2, 4, true>(ctx, p);
+  return c.shape == FEW_16 ? launch_few_k<D, 1, 4, false>(ctx, p) : launch_few_k<D, 2, 4, false>(ctx, p);
+}
+
+template <int D, int NS, int NQ, int NW, bool TREE>
+hipError_t launch_ring_k(cascade_ctx* ctx, const PagedParams& p) {
+  constexpr int smem = ring_lds<D, NS, NQ, NW, TREE>(), rows = 16 * NQ * NW;
+  constexpr auto kern = paged_ring_kernel<D, NS, NQ, NW, TREE>;
+  hipError_t e = allow_lds<kern>(smem, ctx->device);
+  if (e != hipSuccess) return e;
+  const paged_attn_args& a = p.a;
+  // no more blocks than this, whatever the rows' lengths are; a row out of order is one
+  const int64_t each = ((int64_t)a.max_new * p.group + rows - 1) / rows;
+  const int64_t blocks = std::min((int64_t)a.n_tokens * p.group / rows + a.n_rows, each * a.n_rows) * p.parts;
+  // (8 / n_kv_heads XCDs share a kv head: every one gets as many)
+  const int64_t share = 8 % a.n_kv_heads == 0 ? 8 / a.n_kv_heads : 1;
+  KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
+  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)((blocks + share - 1) / share * share * a.n_kv_heads)), dim3(64 * NW), smem, ctx->stream, p);
+  return hipGetLastError();
+}
+template <int D, bool TREE>
+hipError_t launch_ring(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
+  if (c.shape == RING_64) return launch_ring_k<D, 2, 1, 4, TREE>(ctx, p);
+  if (c.shape == RING_128) return launch_ring_k<D, 2, 2, 4, TREE>(ctx, p);
+  return launch_ring_k<D, 3, 2, 8, TREE>(ctx, p);
+}
+template <int D>
+hipError_t launch_bf16(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
+  if (c.shape <= FEW_32) return launch_few<D>(ctx, p, c);
+  return p.a.parent ? launch_ring<D, true>(ctx, p, c) : launch_ring<D, false>(ctx, p, c);
 }
 
 }  // namespace
@@ -727,14 +1284,13 @@ hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
   p.part_tiles = c.part_tiles;
   p.ws_o = (float*)ws;
   p.ws_ml = (float*)ws + (size_t)c.parts * a->n_tokens * a->n_heads * a->head_dim;
-  if (c.kind == 0) {
-    hipError_t e = a->head_dim == 128 ? launch_few<128>(ctx, p, c) : launch_few<64>(ctx, p, c);
+  if (c.shape != OTHER) {
+    hipError_t e = a->head_dim == 128 ? launch_bf16<128>(ctx, p, c) : launch_bf16<64>(ctx, p, c);
     if (e != hipSuccess) return e;
   } else {
     const unsigned grid = (unsigned)(((long long)a->n_tokens * a->n_heads + 3) / 4);
     KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
-    if (a->dtype == CASCADE_BF16) CASCADE_TIMED_LAUNCH(t, paged_attn_simple_kernel<uint16_t>, dim3(grid), dim3(256), 0, ctx->stream, p);
-    else CASCADE_TIMED_LAUNCH(t, paged_attn_simple_kernel<float>, dim3(grid), dim3(256), 0, ctx->stream, p);
+    CASCADE_TIMED_LAUNCH(t, paged_attn_simple_kernel<float>, dim3(grid), dim3(256), 0, ctx->stream, p);
   }
   if (c.parts > 1) {
     const long long lanes = (long long)a->n_tokens * a->n_heads * ((a->head_dim + 3) / 4);
