@@ -84,19 +84,20 @@ struct Tiles {
   __device__ __forceinline__ int prefix_tile(int t) const { return t < sinks_p ? t : t + skip_p; }
   __device__ __forceinline__ int new_tile(int t) const { return t < sinks_n ? t : t + skip_n; }
 };
+template <int TS = KT>   // keys per tile
 __device__ __forceinline__ Tiles tiles_of(const PagedParams& p, int P, int i0, int i1, bool tree) {
-  const int W = p.a.window, n_pt = (P + KT - 1) / KT, n_nt = i1 / KT + 1;
+  const int W = p.a.window, n_pt = (P + TS - 1) / TS, n_nt = i1 / TS + 1;
   Tiles t = {n_pt, 0, 0, n_nt, 0, 0, 0};
   if (W > 0) {
     if (tree) i0 = 0;   // a node's position is its depth
     t.first = max(0, P + i0 - W + 1);
-    const int from_p = t.first < P ? t.first / KT : n_pt;
-    t.sinks_p = (min(p.a.n_sink, P) + KT - 1) / KT;
+    const int from_p = t.first < P ? t.first / TS : n_pt;
+    t.sinks_p = (min(p.a.n_sink, P) + TS - 1) / TS;
     t.skip_p = max(0, from_p - t.sinks_p);
     t.n_p = n_pt - t.skip_p;
     if (!tree) {
-      t.sinks_n = min((min(max(p.a.n_sink - P, 0), i1 + 1) + KT - 1) / KT, n_nt);
-      t.skip_n = max(0, max(0, i0 - W + 1) / KT - t.sinks_n);
+      t.sinks_n = min((min(max(p.a.n_sink - P, 0), i1 + 1) + TS - 1) / TS, n_nt);
+      t.skip_n = max(0, max(0, i0 - W + 1) / TS - t.sinks_n);
       t.n_n = n_nt - t.skip_n;
     }
   }
@@ -1006,6 +1007,219 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_ring_kernel(Pa
   }
 }
 
+// ------------------------------------------------------------------------------------------------------------------------- f32
+// Workgroup = (16 query rows, kv head, part); its NW waves take every NW-th tile of 16 keys - one group, one page - and meet in LDS.  Both products run on
+// v_mfma_f32_16x16x4_f32 (one value per lane and operand, k = lane / 16 = g):
+//   S^T = K Q^T   lane (l16, g) loads 16 bytes at d = 16 db + 4 g of key / query l16 and feeds element c of both to the c-th product; the result holds
+//                 keys 4 g + r of query l16;
+//   O^T = V^T P^T product r takes P^T straight from register r of that result, and element c of the 16 bytes at d = 64 h + 4 l16 of key 4 g + r's value: its row l16
+//                 stands for that d + c (element loads: d = 16 db + l16).
+// Nothing passes through LDS before the waves meet.  Bound by the trips to memory, one after the other: the row's place, the table's entry, the first tile.
+template <int DB, int NW, bool VEC, bool TREE>
+__global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
+  extern __shared__ __align__(16) float f32_smem[];   // [NW][16 queries][16 DB + 4] outputs, [NW][16][2] maxima and sums
+  __shared__ int s_parent[TREE ? CASCADE_MAX_TREE : 1];
+  constexpr int OP = 16 * DB + 4, TS = 16;
+  const paged_attn_args& a = p.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g = lane >> 4, G = p.group, D = a.head_dim;
+  const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads, part = b % p.parts;
+  int sb = 0;
+  const RowInfo ri = block_row(p, b / p.parts, 16, lane, &sb);
+  if (ri.s < 0) return;   // the grid is an upper bound of the number of blocks
+  if (ri.flag) { write_nothing<float>(p, ri, kvh, part, tid, 64 * NW); return; }
+  const int lo = ri.lo, T = ri.T, P = ri.P, M = T * G, row0 = 16 * sb, rows = min(16, M - row0);
+  const Tiles ti = tiles_of<TS>(p, P, row0 / G, (row0 + rows - 1) / G, TREE);
+  const int nt = ti.n_p + ti.n_n, per = (nt + p.parts - 1) / p.parts, t_begin = part * per, t_end = min(nt, t_begin + per);
+  const int qr = row0 + min(l16, rows - 1);   // rows past the end repeat the last one, never stored
+  const int qi = qr / G;
+  const float* qrow = (const float*)a.q + (lo + qi) * a.q_stride + (kvh * G + qr - qi * G) * D;
+  const float *kn = (const float*)a.k_new + lo * a.kv_stride + kvh * D, *vn = (const float*)a.v_new + lo * a.kv_stride + kvh * D;
+  auto load4 = [&](const float* row, int d) {
+    if (VEC) return d < D ? *(const f32x4*)(row + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 x;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) x[c] = d + c < D ? row[d + c] : 0.f;
+    return x;
+  };
+  f32x4 q[DB], ot[DB], k[DB], v[4][DB / 4];
+  // keys past the end of the tile's source: the last one again, masked
+  struct Source {
+    long long off, pitch;
+    int last;
+    bool fresh;
+  };
+  auto source_of = [&](int t) {
+    Source s;
+    s.fresh = t >= ti.n_p;
+    if (!s.fresh) {
+      const int gq = needed_group(p, ti, P, ti.prefix_tile(t)), e = page_index(p, gq);
+      s.off = group_offset(p, checked_page(p, table_entry(p, ri.s, e)), e, gq, kvh);
+      s.last = P - 1 - 16 * gq;
+      s.pitch = a.stride_pos;
+    } else {
+      const int j = ti.new_tile(t - ti.n_p);
+      s.off = (long long)(16 * j) * a.kv_stride;
+      s.last = T - 1 - 16 * j;
+      s.pitch = a.kv_stride;
+    }
+    return s;
+  };
+  auto request_k = [&](const Source& s) {
+    const float* row = (s.fresh ? kn : (const float*)a.k_pages) + s.off + min(l16, s.last) * s.pitch;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) k[db] = load4(row, 16 * db + 4 * g);
+  };
+  auto request_v = [&](const Source& s) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float* row = (s.fresh ? vn : (const float*)a.v_pages) + s.off + min(4 * g + r, s.last) * s.pitch;
+#pragma unroll
+      for (int h = 0; h < DB / 4; ++h)
+        if (VEC) v[r][h] = load4(row, 64 * h + 4 * l16);
+        else
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[r][h][c] = row[min(64 * h + 16 * c + l16, D - 1)];
+    }
+  };
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    q[db] = load4(qrow, 16 * db + 4 * g);
+    ot[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  if (t_begin + wave < t_end) {
+    const Source s = source_of(t_begin + wave);
+    request_k(s);
+    request_v(s);
+  }
+  int depth = qi;
+  if (TREE) {
+    for (int i = tid; i < T; i += 64 * NW) {
+      int pi = a.parent[lo + i];
+      if (i == 0 ? pi != -1 : (pi >= i || pi < 0)) { atomicOr(p.dev_status, CASCADE_FLAG_PARENT); pi = i == 0 ? -1 : 0; }
+      s_parent[i] = pi;
+    }
+    __syncthreads();
+    if (a.window > 0) {
+      depth = 0;
+      for (int x = s_parent[qi]; x >= 0; x = s_parent[x]) ++depth;
+    }
+  }
+  // keys of tile t that query l16 sees
+  auto seen = [&](int t) -> unsigned {
+    if (t < ti.n_p) return (unsigned)sees_prefix(p, P, 16 * ti.prefix_tile(t), P + depth) & 0xffffu;
+    const int kb = 16 * ti.new_tile(t - ti.n_p);
+    if (!TREE) return (unsigned)sees_chain(p, P, kb, qi) & 0xffffu;
+    unsigned bits = 0;
+    const int reach = depth - a.window + 1, sinks = a.n_sink - P;
+    int d = depth;
+    for (int x = qi; x >= kb; x = s_parent[x], --d)   // kb >= 0; ancestors only get smaller
+      if (x - kb < 16 && (a.window == 0 || d >= reach || d < sinks)) bits |= 1u << (x - kb);
+    return bits;
+  };
+  float m = -INFINITY, l = 0.f;
+  auto step = [&](int t, auto more) {   // more: another tile of the wave follows
+    constexpr bool MORE = decltype(more)::value;
+    const unsigned bits = seen(t);
+    f32x4 st = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) st = __builtin_amdgcn_mfma_f32_16x16x4f32(k[db][c], q[db][c], st, 0, 0, 0);
+    Source next;
+    if constexpr (MORE) {
+      next = source_of(t + NW);
+      request_k(next);
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      st[r] = ((bits >> (4 * g + r)) & 1u) ? st[r] * p.scale_log2e : -INFINITY;
+      mx = fmaxf(mx, st[r]);
+    }
+    const float m_new = fmaxf(m, rows4_max(mx)), m_use = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = fast_exp2(m - m_use);
+    float ls = 0.f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      st[r] = fast_exp2(st[r] - m_use);
+      ls += st[r];
+    }
+    l = l * alpha + ls;
+    m = m_new;
+    // a tile that some query does not see whole is looked through for infinities and NaN; if it holds any its keys are added one at a time, to the queries that see them
+    bool whole_keys = true;
+    if (__any(bits != 0xffffu)) {
+      float z = 0.f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) z = fmaf(v[r][db / 4][db % 4], 0.f, z);
+      whole_keys = !__any(z != 0.f);
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db) ot[db] *= alpha;
+    if (whole_keys) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) ot[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][db / 4][db % 4], st[r], ot[db], 0, 0, 0);
+    } else {
+      for (int kg = 0; kg < 4; ++kg)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const bool sees = (bits >> (4 * kg + r)) & 1u;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            const f32x4 o = __builtin_amdgcn_mfma_f32_16x16x4f32(g == kg ? v[r][db / 4][db % 4] : 0.f, st[r], ot[db], 0, 0, 0);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) ot[db][c] = sees ? o[c] : ot[db][c];
+          }
+        }
+    }
+    if constexpr (MORE) request_v(next);
+  };
+  int t = t_begin + wave;
+  for (; t + NW < t_end; t += NW) step(t, std::true_type{});
+  if (t < t_end) step(t, std::false_type{});
+  // the waves meet: lane (l16, g) holds d = 64 (db / 4) + 16 g + 4 c + db % 4 of query l16 (element loads: d = 16 db + 4 g + c)
+  l = rows4_sum(l);
+  float* mo = f32_smem + (wave * 16 + l16) * OP;
+  float* ml = f32_smem + NW * 16 * OP;
+#pragma unroll
+  for (int h = 0; h < DB / 4; ++h)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      if (VEC) *(f32x4*)(mo + 64 * h + 16 * g + 4 * c) = f32x4{ot[4 * h][c], ot[4 * h + 1][c], ot[4 * h + 2][c], ot[4 * h + 3][c]};
+      else *(f32x4*)(mo + 64 * h + 16 * c + 4 * g) = ot[4 * h + c];
+    }
+  if (g == 0) {
+    ml[(wave * 16 + l16) * 2] = m;
+    ml[(wave * 16 + l16) * 2 + 1] = l;
+  }
+  __syncthreads();
+  // a wave finishes whole rows: lane w holds the factor of wave w's part
+  const long long all_rows = (long long)a.n_tokens * a.n_heads;
+  for (int r = wave; r < rows; r += NW) {
+    const int row = row0 + r, w = lane & 15;
+    const float mw = w < NW ? ml[(w * 16 + r) * 2] : -INFINITY, lw = w < NW ? ml[(w * 16 + r) * 2 + 1] : 0.f;
+    const float mm = wave_max(mw), f = fast_exp2(mw - (mm == -INFINITY ? 0.f : mm));   // a wave without visible keys: 0
+    const float ll = wave_sum(lane < NW ? f * lw : 0.f);
+    const long long at = (long long)(lo + row / G) * a.n_heads + kvh * G + row % G;
+    float* out = p.parts > 1 ? p.ws_o + (part * all_rows + at) * D : (float*)a.out + at * D;
+    for (int d = lane; d < D; d += 64) {
+      float o = 0.f;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) o = fmaf(__int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i)), f32_smem[(i * 16 + r) * OP + d], o);
+      out[d] = p.parts > 1 ? o : o / ll;
+    }
+    if (lane == 0) {
+      if (p.parts > 1) { p.ws_ml[(part * all_rows + at) * 2] = mm; p.ws_ml[(part * all_rows + at) * 2 + 1] = ll; }
+      else if (a.lse) a.lse[at] = mm * LN2 + logf(ll);
+    }
+  }
+}
+
 // Joins the parts: D / 4 lanes per (token, query head).  Rows that have fewer parts, or that could not be computed, left empty ones (l = 0).
 template <typename T>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedParams p) {
@@ -1042,116 +1256,6 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedParams p) {
   if (d == 0 && a.lse) a.lse[row] = m * LN2 + logf(l);
 }
 
-// One wave per (token, query head): a lane takes a key of 64, then head elements.
-template <typename T>
-__global__ __launch_bounds__(256) void paged_attn_simple_kernel(PagedParams p) {
-  const paged_attn_args& a = p.a;
-  __shared__ float s_q[4][256];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long at = (long long)blockIdx.x * 4 + wave;
-  if (at >= (long long)a.n_tokens * a.n_heads) return;
-  const int t = (int)(at / a.n_heads), h = (int)(at % a.n_heads), kvh = h / p.group, D = a.head_dim;
-  int s = -1;
-  for (int base = 0; base < a.n_rows && s < 0; base += 64) {
-    const int r = base + lane;
-    const bool hit = r < a.n_rows && a.q_off[r] <= t && t < a.q_off[r + 1];
-    const unsigned long long who = __ballot(hit);
-    if (who) s = base + __ffsll((long long)who) - 1;
-  }
-  if (s < 0) return;
-  const int lo = a.q_off[s], n = a.q_off[s + 1] - lo, P = a.prefix_len[s];
-  T* out = (T*)a.out + at * D;
-  auto put = [&](int d, float v) {
-    if constexpr (sizeof(T) == 2) out[d] = f32_to_bf16_bits(v);
-    else out[d] = v;
-  };
-  int flag = 0;
-  if (lo < 0 || a.q_off[s + 1] > a.n_tokens || n > a.max_new) flag = CASCADE_FLAG_TREE_SIZE;
-  else if (P < 0 || P > a.max_prefix_len || P > (long long)a.table_width * a.page_size) flag = CASCADE_FLAG_CAPACITY;
-  if (flag) {
-    if (lane == 0) atomicOr(p.dev_status, flag);
-    for (int d = lane; d < D; d += 64) put(d, 0.f);
-    if (lane == 0 && a.lse) a.lse[at] = -INFINITY;
-    return;
-  }
-  const T* q = (const T*)a.q + (long long)t * a.q_stride + (long long)h * D;
-  for (int d = lane; d < D; d += 64) s_q[wave][d] = load_f32(q + d);
-  const int i = t - lo;
-  // the node's depth (a chain: its index)
-  int depth = i;
-  if (a.parent) {
-    depth = 0;
-    for (int x = i; x > 0; ++depth) {
-      const int up = a.parent[lo + x];
-      if (up >= x || up < 0) { if (lane == 0) atomicOr(p.dev_status, CASCADE_FLAG_PARENT); x = 0; }
-      else x = up;
-    }
-  }
-  const int qpos = P + depth;
-  auto near = [&](int kpos) { return a.window == 0 || qpos - kpos < a.window || kpos < a.n_sink; };
-  float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  const int n_pt = (P + 63) / 64, n_nt = i / 64 + 1;
-  for (int c = 0; c < n_pt + n_nt; ++c) {
-    const bool fresh = c >= n_pt;
-    const int key = 64 * (fresh ? c - n_pt : c) + lane;
-    bool sees = false;
-    const T *k = nullptr, *v = nullptr;
-    if (!fresh) {
-      if (key < P && near(key)) {
-        int g = a.block_table[s * a.table_stride + key / a.page_size];
-        if (g < 0 || g >= a.n_pages) { atomicOr(p.dev_status, CASCADE_FLAG_PAGE); g = 0; }
-        const long long off = g * a.stride_page + kvh * a.stride_head + (key % a.page_size) * a.stride_pos;
-        k = (const T*)a.k_pages + off;
-        v = (const T*)a.v_pages + off;
-        sees = true;
-      }
-    } else if (key <= i) {
-      int kdepth = key;
-      sees = true;
-      if (a.parent) {
-        sees = false;
-        int x = i;
-        kdepth = depth;
-        while (x > key) {
-          const int up = a.parent[lo + x];
-          x = up >= x || up < 0 ? 0 : up;
-          --kdepth;
-        }
-        sees = x == key;
-      }
-      sees = sees && near(P + kdepth);
-      if (sees) {
-        const long long off = (lo + key) * a.kv_stride + (long long)kvh * D;
-        k = (const T*)a.k_new + off;
-        v = (const T*)a.v_new + off;
-      }
-    }
-    float z = -INFINITY;
-    if (sees) {
-      float dot = 0.f;
-      for (int d = 0; d < D; ++d) dot = fmaf(s_q[wave][d], load_f32(k + d), dot);
-      z = dot * p.scale_log2e;
-    }
-    const float m_new = fmaxf(m, wave_max(z)), use = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = exp2f(m - use), e = sees ? exp2f(z - use) : 0.f;
-    l = l * alpha + wave_sum(e);
-    m = m_new;
-    for (int x = 0; x < 4; ++x) o[x] *= alpha;
-    unsigned long long who = __ballot(sees);
-    while (who) {
-      const int j = __ffsll((long long)who) - 1;
-      who &= who - 1;
-      const float w = __shfl(e, j);
-      const T* vj = (const T*)__shfl((unsigned long long)v, j);
-      for (int x = 0; x < 4; ++x)
-        if (lane + 64 * x < D) o[x] = fmaf(w, load_f32(vj + lane + 64 * x), o[x]);
-    }
-  }
-  for (int x = 0; x < 4; ++x)
-    if (lane + 64 * x < D) put(lane + 64 * x, l == 0.f ? 0.f : o[x] / l);
-  if (lane == 0 && a.lse) a.lse[at] = m * LN2 + logf(l);
-}
-
 // ----------------------------------------------------------------------------------------------------------------------- launches
 // Kernels ask for more LDS than a launch may have by default: said once per kernel and device.
 template <auto KERNEL>
@@ -1164,19 +1268,19 @@ hipError_t allow_lds(int bytes, int device) {
   return e;
 }
 
-// How a call is cut.  Shapes 0 and 1: few query rows, 16 or 32 of them; 2, 3, 4: workgroups of 64, 128, 256 query rows.
+// How a call is cut.  Shapes 0 and 1: few query rows, 16 or 32 of them; 2, 3, 4: workgroups of 64, 128, 256 query rows; 5: f32.
 struct Cut {
   int shape;
   int parts, part_tiles;
 };
-constexpr int FEW_16 = 0, FEW_32 = 1, RING_64 = 2, RING_128 = 3, RING_256 = 4, OTHER = 5;
-constexpr int SHAPE_ROWS[] = {16, 32, 64, 128, 256};
+constexpr int FEW_16 = 0, FEW_32 = 1, RING_64 = 2, RING_128 = 3, RING_256 = 4, F32 = 5;
+constexpr int SHAPE_ROWS[] = {16, 32, 64, 128, 256, 16};
 
-int tiles_bound(const paged_attn_args* a) {
-  const int n = (a->max_new + KT - 1) / KT;
-  int t = (a->max_prefix_len + KT - 1) / KT;
+int tiles_bound(const paged_attn_args* a, int ts = KT) {
+  const int n = (a->max_new + ts - 1) / ts;
+  int t = (a->max_prefix_len + ts - 1) / ts;
   if (a->window > 0) {
-    const int64_t w = ((int64_t)a->window + KT - 2) / KT + 1 + ((int64_t)a->n_sink + KT - 1) / KT;   // a window's tiles, wherever it begins, and the sinks'
+    const int64_t w = ((int64_t)a->window + ts - 2) / ts + 1 + ((int64_t)a->n_sink + ts - 1) / ts;   // a window's tiles, wherever it begins, and the sinks'
     if (w < t) t = (int)w;
   }
   return t + n;
@@ -1200,10 +1304,17 @@ float ring_estimate_us(int shape, const paged_attn_args* a, int parts, int n_cu)
 }
 
 Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
-  Cut c = {OTHER, 1, 1};
-  if (a->dtype != CASCADE_BF16) return c;
+  Cut c = {F32, 1, 1};
   const int64_t M = (int64_t)a->max_new * (a->n_heads / a->n_kv_heads);
-  const int tiles = tiles_bound(a), most = (int)std::min<size_t>(ws_bytes / part_bytes(a), 64);
+  const int most = (int)std::min<size_t>(ws_bytes / part_bytes(a), 64);
+  if (a->dtype == CASCADE_F32) {
+    // few blocks share the keys, four tiles to a wave at least
+    const int waves = a->head_dim <= 64 ? 16 : (a->head_dim <= 128 ? 8 : 4);
+    const int64_t blocks = a->n_rows * ((M + 15) / 16) * a->n_kv_heads;
+    c.parts = (int)std::max<int64_t>(1, std::min<int64_t>({most, n_cu / blocks, tiles_bound(a, 16) / (4 * waves)}));
+    return c;
+  }
+  const int tiles = tiles_bound(a);
   if (M > 32) {
     float best = INFINITY;
     for (int shape = RING_64; shape <= RING_256; ++shape)
@@ -1239,16 +1350,20 @@ hipError_t launch_few(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
   return c.shape == FEW_16 ? launch_few_k<D, 1, 4, false>(ctx, p) : launch_few_k<D, 2, 4, false>(ctx, p);
 }
 
+// no more blocks of so many query rows than this, whatever the rows' lengths are; a row out of order is one
+int64_t most_blocks(const PagedParams& p, int rows) {
+  const int64_t each = ((int64_t)p.a.max_new * p.group + rows - 1) / rows;
+  return std::min((int64_t)p.a.n_tokens * p.group / rows + p.a.n_rows, each * p.a.n_rows) * p.parts;
+}
+
 template <int D, int NS, int NQ, int NW, bool TREE>
 hipError_t launch_ring_k(cascade_ctx* ctx, const PagedParams& p) {
-  constexpr int smem = ring_lds<D, NS, NQ, NW, TREE>(), rows = 16 * NQ * NW;
+  constexpr int smem = ring_lds<D, NS, NQ, NW, TREE>();
   constexpr auto kern = paged_ring_kernel<D, NS, NQ, NW, TREE>;
   hipError_t e = allow_lds<kern>(smem, ctx->device);
   if (e != hipSuccess) return e;
   const paged_attn_args& a = p.a;
-  // no more blocks than this, whatever the rows' lengths are; a row out of order is one
-  const int64_t each = ((int64_t)a.max_new * p.group + rows - 1) / rows;
-  const int64_t blocks = std::min((int64_t)a.n_tokens * p.group / rows + a.n_rows, each * a.n_rows) * p.parts;
+  const int64_t blocks = most_blocks(p, 16 * NQ * NW);
   // (8 / n_kv_heads XCDs share a kv head: every one gets as many)
   const int64_t share = 8 % a.n_kv_heads == 0 ? 8 / a.n_kv_heads : 1;
   KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
@@ -1260,6 +1375,29 @@ hipError_t launch_ring(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
   if (c.shape == RING_64) return launch_ring_k<D, 2, 1, 4, TREE>(ctx, p);
   if (c.shape == RING_128) return launch_ring_k<D, 2, 2, 4, TREE>(ctx, p);
   return launch_ring_k<D, 3, 2, 8, TREE>(ctx, p);
+}
+template <int DB, int NW, bool VEC, bool TREE>
+hipError_t launch_f32_k(cascade_ctx* ctx, const PagedParams& p) {
+  constexpr int smem = (NW * 16 * (16 * DB + 4) + NW * 32) * 4;
+  constexpr auto kern = paged_f32_kernel<DB, NW, VEC, TREE>;
+  hipError_t e = allow_lds<kern>(smem, ctx->device);
+  if (e != hipSuccess) return e;
+  KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
+  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)(most_blocks(p, 16) * p.a.n_kv_heads)), dim3(64 * NW), smem, ctx->stream, p);
+  return hipGetLastError();
+}
+template <int DB, int NW>
+hipError_t launch_f32_t(cascade_ctx* ctx, const PagedParams& p) {
+  const paged_attn_args& a = p.a;
+  // keys, values and queries 16 bytes at a time where everything lies on such boundaries, otherwise element by element
+  const bool vec = ((a.head_dim | a.q_stride | a.kv_stride | a.stride_page | a.stride_head | a.stride_pos) % 4) == 0 &&
+                   (((uintptr_t)a.q | (uintptr_t)a.k_new | (uintptr_t)a.v_new | (uintptr_t)a.k_pages | (uintptr_t)a.v_pages) & 15) == 0;
+  if (a.parent) return vec ? launch_f32_k<DB, NW, true, true>(ctx, p) : launch_f32_k<DB, NW, false, true>(ctx, p);
+  return vec ? launch_f32_k<DB, NW, true, false>(ctx, p) : launch_f32_k<DB, NW, false, false>(ctx, p);
+}
+hipError_t launch_f32(cascade_ctx* ctx, const PagedParams& p) {
+  if (p.a.head_dim <= 64) return launch_f32_t<4, 16>(ctx, p);
+  return p.a.head_dim <= 128 ? launch_f32_t<8, 8>(ctx, p) : launch_f32_t<16, 4>(ctx, p);
 }
 template <int D>
 hipError_t launch_bf16(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
@@ -1284,14 +1422,8 @@ hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
   p.part_tiles = c.part_tiles;
   p.ws_o = (float*)ws;
   p.ws_ml = (float*)ws + (size_t)c.parts * a->n_tokens * a->n_heads * a->head_dim;
-  if (c.shape != OTHER) {
-    hipError_t e = a->head_dim == 128 ? launch_bf16<128>(ctx, p, c) : launch_bf16<64>(ctx, p, c);
-    if (e != hipSuccess) return e;
-  } else {
-    const unsigned grid = (unsigned)(((long long)a->n_tokens * a->n_heads + 3) / 4);
-    KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
-    CASCADE_TIMED_LAUNCH(t, paged_attn_simple_kernel<float>, dim3(grid), dim3(256), 0, ctx->stream, p);
-  }
+  hipError_t e = c.shape == F32 ? launch_f32(ctx, p) : (a->head_dim == 128 ? launch_bf16<128>(ctx, p, c) : launch_bf16<64>(ctx, p, c));
+  if (e != hipSuccess) return e;
   if (c.parts > 1) {
     const long long lanes = (long long)a->n_tokens * a->n_heads * ((a->head_dim + 3) / 4);
     KernelTimer t(ctx, CASCADE_K_PAGED_MERGE);
