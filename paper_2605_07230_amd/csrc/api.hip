@@ -490,7 +490,9 @@ static int check_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a) {
     return CASCADE_ESHAPE;
   if (a->parent && a->max_new > L.max_nodes_per_tree) return CASCADE_ESHAPE;
   // positions and what a launch counts stay below 2^30
-  if (a->max_prefix_len > (1 << 30) || a->max_new > (1 << 30) || (int64_t)a->n_tokens * a->n_heads > (1 << 30) || a->n_kv_heads > 65535) return CASCADE_ESHAPE;
+  if (a->max_prefix_len > (1 << 30) || a->max_new > (1 << 30) || (int64_t)a->n_tokens * a->n_heads > (1 << 30) || a->n_kv_heads > 65535 ||
+      (double)a->max_new * (a->n_heads / a->n_kv_heads) * (a->n_heads / a->n_kv_heads) >= 4294967296.0)
+    return CASCADE_ESHAPE;
   if (a->dtype == CASCADE_BF16) {
     if (a->head_dim != 64 && a->head_dim != 128) return CASCADE_ESHAPE;
     if ((a->stride_page | a->stride_head | a->stride_pos | a->q_stride | a->kv_stride) % 8) return CASCADE_ESHAPE;

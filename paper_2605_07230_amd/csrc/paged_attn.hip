@@ -34,6 +34,8 @@ typedef unsigned long long u64;
 struct PagedParams {
   paged_attn_args a;
   int group;
+  unsigned group_inv;    // floor(2^32 / group) + 1: a query row's token as a high product (rows times group stay below 2^32); 0 for one head
+  int most_prefix;       // the longest prefix that the bound and the table allow
   float scale_log2e;
   int* dev_status;
   int page16;            // 16-key groups of a page
@@ -69,7 +71,7 @@ __device__ __forceinline__ RowInfo check_row(const PagedParams& p, int s, int lo
     r.flag = CASCADE_FLAG_TREE_SIZE;
     r.lo = max(lo, 0);
     r.T = max(min(hi, a.n_tokens) - r.lo, 0);
-  } else if (P < 0 || P > a.max_prefix_len || (long long)P > (long long)a.table_width * a.page_size) {
+  } else if (P < 0 || P > p.most_prefix) {
     r.flag = CASCADE_FLAG_CAPACITY;
   }
   return r;
@@ -122,6 +124,7 @@ __device__ __forceinline__ int needed_group(const PagedParams& p, const Tiles& t
   if (p.a.window > 0 && 16 * g >= p.a.n_sink && 16 * g + 15 < ti.first) g = ti.first < P ? ti.first >> 4 : (min(p.a.n_sink, P) - 1) >> 4;
   return g;
 }
+__device__ __forceinline__ int token_of(const PagedParams& p, int row) { return p.group_inv ? (int)__umulhi((unsigned)row, p.group_inv) : row; }
 __device__ __forceinline__ int page_index(const PagedParams& p, int g) { return p.page16_inv ? (int)__umulhi((unsigned)g, p.page16_inv) : g; }
 
 // an entry of the table; one outside the pool is flagged and stands for the first page
@@ -170,7 +173,7 @@ __device__ __forceinline__ void write_nothing(const PagedParams& p, const RowInf
 // a key per lane), values through a region of LDS of the wave's own.  A workgroup works through parts (row, kv head, run of part_tiles tiles) until
 // none is left: rows of very different lengths fill the chip evenly, and no workgroup is launched for nothing.
 template <int D, int NQ, int NW, bool TREE>
-__global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedParams p) {
+__global__ __launch_bounds__(64 * NW, 8 / NW) void paged_few_kernel(PagedParams p) {
   constexpr int NT = 64 * NW, KS = D / 32, DB = D / 16, DC = D / 8, VP = D + 16, OP = D + 4, NVC = KT * DC / 64, R = 16 * NQ;
   extern __shared__ __align__(16) char few_smem[];
   const paged_attn_args& a = p.a;
@@ -228,44 +231,41 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedParams p) {
         ml[1] = 0.f;
       }
 
-    // ---- a tile: kf[kt][ks] = key 16 kt + l16, d 32 ks + 8 g .. + 7; value pieces c = lane + 64 it of the row-major tile
+    // ---- a tile: kf[kt][ks] = key 16 kt + l16, d 32 ks + 8 g .. + 7; value pieces c = lane + 64 it of the row-major tile.  Groups of 16 keys begin
+    // anywhere; inside one, 32-bit offsets do.  Keys past the end are the last one again.
     u32x4 kf[4][KS], vr[NVC];
-    const uint16_t *kn = (const uint16_t*)a.k_new + lo * a.kv_stride + kvh * D, *vn = (const uint16_t*)a.v_new + lo * a.kv_stride + kvh * D;
+    const char *kn = (const char*)((const uint16_t*)a.k_new + lo * a.kv_stride + kvh * D), *vn = (const char*)((const uint16_t*)a.v_new + lo * a.kv_stride + kvh * D);
     auto request = [&](int t) {
-      if (t < ti.n_p) {
-        const int kb = ti.prefix_tile(t) * KT;
-        int gq[4];
-        long long off[4];
+      const bool fresh = t >= ti.n_p;
+      const int g0 = 4 * (fresh ? ti.new_tile(t - ti.n_p) : ti.prefix_tile(t)), end = (fresh ? T : P) - 1;
+      const unsigned pitch = 2u * (unsigned)(fresh ? a.kv_stride : a.stride_pos);
+      const char *kb = fresh ? kn : (const char*)a.k_pages, *vb = fresh ? vn : (const char*)a.v_pages;
+      long long off[4];
+      int last[4];
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-          gq[kt] = needed_group(p, ti, P, (kb >> 4) + kt);
-          const int e = page_index(p, gq[kt]);
-          off[kt] = group_offset(p, checked_page(p, table_entry(p, r.s, e)), e, gq[kt], kvh);
+      for (int kt = 0; kt < 4; ++kt) {
+        int gq;
+        if (fresh) {
+          gq = min(g0 + kt, end >> 4);
+          off[kt] = (long long)(16 * gq) * pitch;
+        } else {
+          gq = needed_group(p, ti, P, g0 + kt);
+          const int e = page_index(p, gq);
+          off[kt] = 2 * group_offset(p, checked_page(p, table_entry(p, r.s, e)), e, gq, kvh);
         }
+        last[kt] = end - 16 * gq;
+      }
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-          const uint16_t* kp = (const uint16_t*)a.k_pages + off[kt] + (long long)min(l16, P - 1 - 16 * gq[kt]) * a.stride_pos + 8 * g;
+      for (int kt = 0; kt < 4; ++kt) {
+        const char* kp = kb + off[kt];
+        const unsigned at = (unsigned)min(l16, last[kt]) * pitch + 16u * g;
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) kf[kt][ks] = *(const u32x4*)(kp + 32 * ks);
-        }
+        for (int ks = 0; ks < KS; ++ks) kf[kt][ks] = *(const u32x4*)(kp + (at + 64u * ks));
+      }
 #pragma unroll
-        for (int it = 0; it < NVC; ++it) {
-          const int c = lane + 64 * it, kt = it / (NVC / 4), in = (c / DC) & 15;
-          vr[it] = *(const u32x4*)((const uint16_t*)a.v_pages + off[kt] + (long long)min(in, P - 1 - 16 * gq[kt]) * a.stride_pos + 8 * (c % DC));
-        }
-      } else {
-        const int kb = ti.new_tile(t - ti.n_p) * KT;
-#pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-          const uint16_t* kp = kn + (long long)min(kb + 16 * kt + l16, T - 1) * a.kv_stride + 8 * g;
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) kf[kt][ks] = *(const u32x4*)(kp + 32 * ks);
-        }
-#pragma unroll
-        for (int it = 0; it < NVC; ++it) {
-          const int c = lane + 64 * it;
-          vr[it] = *(const u32x4*)(vn + (long long)min(kb + c / DC, T - 1) * a.kv_stride + 8 * (c % DC));
-        }
+      for (int it = 0; it < NVC; ++it) {
+        const int c = lane + 64 * it, kt = it / (NVC / 4);
+        vr[it] = *(const u32x4*)(vb + off[kt] + ((unsigned)min((c / DC) & 15, last[kt]) * pitch + 16u * (unsigned)(c % DC)));
       }
     };
     // queries (B operand of S^T): rows past the end repeat the last one, masked and never stored
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedParams p) {
     for (int n = 0; n < NQ; ++n) {
       const int row = min(16 * n + l16, M - 1);
       q_ok[n] = 16 * n + l16 < M;
-      qi[n] = G == 1 ? row : row / G;
+      qi[n] = token_of(p, row);
       const uint16_t* qp = (const uint16_t*)a.q + (long long)(lo + qi[n]) * a.q_stride + (kvh * G + row - qi[n] * G) * D + 8 * g;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) qf[n][ks].u = *(const uint4*)(qp + 32 * ks);
@@ -363,7 +363,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedParams p) {
         }
       }
       bool odd = false;   // wave-uniform: values that must not meet a masked probability
-      if (__any(some != ~0ull || all != ~0ull)) {
+      // (a single token without a window sees every key that exists, and those past the end are the last one of them)
+      if ((T > 1 || a.window > 0) && __any(some != ~0ull || all != ~0ull)) {
         uint32_t seen_odd = 0;
 #pragma unroll
         for (int it = 0; it < NVC; ++it) {
@@ -484,7 +485,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_few_kernel(PagedParams p) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) o[c] = fmaf(f, x[c], o[c]);
       }
-      const long long at = (long long)(lo + row / G) * a.n_heads + kvh * G + row % G;
+      const int tok = token_of(p, row);
+      const long long at = (long long)(lo + tok) * a.n_heads + kvh * G + row - tok * G;
       if (p.parts > 1) {
         const long long w = (long long)part * a.n_tokens * a.n_heads + at;
         *(f32x4*)(p.ws_o + w * D + d) = o;
@@ -616,7 +618,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_ring_kernel(Pa
   if (ri.s < 0) return;   // the grid is an upper bound of the number of blocks
   if (ri.flag) { write_nothing<uint16_t>(p, ri, kvh, part, tid, NT); return; }
   const int lo = ri.lo, T = ri.T, P = ri.P, M = T * G, row0 = sb * RW;
-  const int i0 = row0 / G, i1 = (min(row0 + RW, M) - 1) / G;
+  const int i0 = token_of(p, row0), i1 = token_of(p, min(row0 + RW, M) - 1);
   const Tiles ti = tiles_of(p, P, i0, i1, TREE);
   const int nt = ti.n_p + ti.n_n, per = (nt + p.parts - 1) / p.parts, t_begin = part * per, t_end = min(nt, t_begin + per);
   const long long all_rows = (long long)a.n_tokens * a.n_heads;
@@ -730,7 +732,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_ring_kernel(Pa
   for (int n = 0; n < NQ; ++n) {
     const int r = row0 + 16 * (wave + NW * n) + l16;
     const bool ok = r < M;
-    const int i = ok ? r / G : 0, hg = ok ? r - i * G : 0;
+    const int i = ok ? token_of(p, r) : 0, hg = ok ? r - i * G : 0;
     qi[n] = ok ? i : -1;
     out_row[n] = (long long)(lo + i) * a.n_heads + kvh * G + hg;
     const uint16_t* qp = (const uint16_t*)a.q + (lo + i) * a.q_stride + (kvh * G + hg) * D + 8 * g;
@@ -815,7 +817,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_ring_kernel(Pa
       const int kb = (t - ti.n_p) * KT, r = row0 + tid;
       u64 bits = 0;
       if (r < M) {
-        int x = r / G;
+        int x = token_of(p, r);
         const int reach = a.window > 0 ? s_depth[x] - a.window + 1 : 0, sinks = a.n_sink - P;   // depths seen: from `reach` on, and below `sinks`
         while (x >= kb) {   // kb >= 0; ancestors only get smaller
           if (x - kb < 64 && (a.window == 0 || s_depth[x] >= reach || (int)s_depth[x] < sinks)) bits |= 1ull << (x - kb);
@@ -1029,10 +1031,10 @@ __global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
   if (ri.s < 0) return;   // the grid is an upper bound of the number of blocks
   if (ri.flag) { write_nothing<float>(p, ri, kvh, part, tid, 64 * NW); return; }
   const int lo = ri.lo, T = ri.T, P = ri.P, M = T * G, row0 = 16 * sb, rows = min(16, M - row0);
-  const Tiles ti = tiles_of<TS>(p, P, row0 / G, (row0 + rows - 1) / G, TREE);
+  const Tiles ti = tiles_of<TS>(p, P, token_of(p, row0), token_of(p, row0 + rows - 1), TREE);
   const int nt = ti.n_p + ti.n_n, per = (nt + p.parts - 1) / p.parts, t_begin = part * per, t_end = min(nt, t_begin + per);
   const int qr = row0 + min(l16, rows - 1);   // rows past the end repeat the last one, never stored
-  const int qi = qr / G;
+  const int qi = token_of(p, qr);
   const float* qrow = (const float*)a.q + (lo + qi) * a.q_stride + (kvh * G + qr - qi * G) * D;
   const float *kn = (const float*)a.k_new + lo * a.kv_stride + kvh * D, *vn = (const float*)a.v_new + lo * a.kv_stride + kvh * D;
   auto load4 = [&](const float* row, int d) {
@@ -1205,7 +1207,8 @@ __global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
     const float mw = w < NW ? ml[(w * 16 + r) * 2] : -INFINITY, lw = w < NW ? ml[(w * 16 + r) * 2 + 1] : 0.f;
     const float mm = wave_max(mw), f = fast_exp2(mw - (mm == -INFINITY ? 0.f : mm));   // a wave without visible keys: 0
     const float ll = wave_sum(lane < NW ? f * lw : 0.f);
-    const long long at = (long long)(lo + row / G) * a.n_heads + kvh * G + row % G;
+    const int tok = token_of(p, row);
+    const long long at = (long long)(lo + tok) * a.n_heads + kvh * G + row - tok * G;
     float* out = p.parts > 1 ? p.ws_o + (part * all_rows + at) * D : (float*)a.out + at * D;
     for (int d = lane; d < D; d += 64) {
       float o = 0.f;
@@ -1220,40 +1223,56 @@ __global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
   }
 }
 
-// Joins the parts: D / 4 lanes per (token, query head).  Rows that have fewer parts, or that could not be computed, left empty ones (l = 0).
-template <typename T>
+// Joins the parts, a wave to a (token, query head): the parts' factors come from its lanes, so two trips to memory follow each other whatever their number.  Rows
+// that have fewer parts, or that could not be computed, left empty ones (l = 0), of which nothing else was written.
+constexpr int MOST_PARTS = 64;
+template <typename T, int DL>   // DL: elements of the head to a lane
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedParams p) {
   const paged_attn_args& a = p.a;
-  const int D = a.head_dim, LPR = (D + 3) / 4;
-  const long long rows = (long long)a.n_tokens * a.n_heads;
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / LPR;
-  const int d = 4 * (int)(at - row * LPR);
+  const int D = a.head_dim, lane = threadIdx.x & 63;
+  const int rows = a.n_tokens * a.n_heads, row = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
   if (row >= rows) return;
-  const long long first = a.q_off[0], last = a.q_off[a.n_rows];
-  if (row < first * a.n_heads || row >= last * a.n_heads) return;   // tokens of no row
   float m = -INFINITY, l = 0.f;
-  for (int c = 0; c < p.parts; ++c) m = fmaxf(m, p.ws_ml[(c * rows + row) * 2]);
-  const float m_use = m == -INFINITY ? 0.f : m;
-  float o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int c = 0; c < p.parts; ++c) {
-    const float mc = p.ws_ml[(c * rows + row) * 2], lc = p.ws_ml[(c * rows + row) * 2 + 1];
-    if (lc == 0.f) continue;   // empty: nothing was written but this
-    const float f = fast_exp2(mc - m_use);
-    l += f * lc;
-    const float* x = p.ws_o + (c * rows + row) * D + d;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (d + i < D) o[i] = fmaf(f, x[i], o[i]);
+  if (lane < p.parts) {
+    const float2 ml = *(const float2*)(p.ws_ml + ((long long)lane * rows + row) * 2);
+    m = ml.x;
+    l = ml.y;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  T* out = (T*)a.out + row * D + d;
+  const int first = a.q_off[0], last = a.q_off[a.n_rows];
+  if (row < (long long)first * a.n_heads || row >= (long long)last * a.n_heads) return;   // a token of no row
+  const float mm = wave_max(m);
+  float f = l == 0.f ? 0.f : fast_exp2(m - (mm == -INFINITY ? 0.f : mm));
+  const float ll = wave_sum(f * l);
+  f = ll == 0.f ? 0.f : f / ll;
+  float o[DL];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (d + i < D) {
-      if constexpr (sizeof(T) == 2) out[i] = f32_to_bf16_bits(o[i] * inv);
-      else out[i] = o[i] * inv;
+  for (int i = 0; i < DL; ++i) o[i] = 0.f;
+  const u64 used = __ballot(l != 0.f);
+  for (int c0 = 0; c0 < p.parts; c0 += 4) {
+    float x[4][DL];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = c0 + j;
+      const bool there = c < p.parts && ((used >> c) & 1);
+      const float* src = p.ws_o + ((long long)(there ? c : 0) * rows + row) * D;
+#pragma unroll
+      for (int i = 0; i < DL; ++i) x[j][i] = there && DL * lane + i < D ? src[DL * lane + i] : 0.f;
     }
-  if (d == 0 && a.lse) a.lse[row] = m * LN2 + logf(l);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), (c0 + j) & 63));
+#pragma unroll
+      for (int i = 0; i < DL; ++i) o[i] = fmaf(w, x[j][i], o[i]);
+    }
+  }
+  T* out = (T*)a.out + (long long)row * D;
+#pragma unroll
+  for (int i = 0; i < DL; ++i)
+    if (DL * lane + i < D) {
+      if constexpr (sizeof(T) == 2) out[DL * lane + i] = f32_to_bf16_bits(o[i]);
+      else out[DL * lane + i] = o[i];
+    }
+  if (lane == 0 && a.lse) a.lse[row] = mm * LN2 + logf(ll);
 }
 
 // ----------------------------------------------------------------------------------------------------------------------- launches
@@ -1306,7 +1325,7 @@ float ring_estimate_us(int shape, const paged_attn_args* a, int parts, int n_cu)
 Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
   Cut c = {F32, 1, 1};
   const int64_t M = (int64_t)a->max_new * (a->n_heads / a->n_kv_heads);
-  const int most = (int)std::min<size_t>(ws_bytes / part_bytes(a), 64);
+  const int most = (int)std::min<size_t>(ws_bytes / part_bytes(a), MOST_PARTS);
   if (a->dtype == CASCADE_F32) {
     // few blocks share the keys, four tiles to a wave at least
     const int waves = a->head_dim <= 64 ? 16 : (a->head_dim <= 128 ? 8 : 4);
@@ -1347,7 +1366,8 @@ hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
 template <int D>
 hipError_t launch_few(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
   if (p.a.parent) return c.shape == FEW_16 ? launch_few_k<D, 1, 4, true>(ctx, p) : launch_few_k<D, 2, 4, true>(ctx, p);
-  return c.shape == FEW_16 ? launch_few_k<D, 1, 4, false>(ctx, p) : launch_few_k<D, 2, 4, false>(ctx, p);
+  if (c.shape == FEW_32) return launch_few_k<D, 2, 4, false>(ctx, p);
+  return (int64_t)p.a.n_rows * p.a.n_kv_heads * c.parts <= ctx->n_cu ? launch_few_k<D, 1, 8, false>(ctx, p) : launch_few_k<D, 1, 4, false>(ctx, p);
 }
 
 // no more blocks of so many query rows than this, whatever the rows' lengths are; a row out of order is one
@@ -1411,6 +1431,8 @@ hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
   PagedParams p;
   p.a = *a;
   p.group = a->n_heads / a->n_kv_heads;
+  p.group_inv = p.group == 1 ? 0u : (unsigned)((1ull << 32) / p.group + 1);
+  p.most_prefix = (int)std::min<int64_t>(a->max_prefix_len, (int64_t)a->table_width * a->page_size);
   p.scale_log2e = (a->scale != 0.f ? a->scale : 1.f / sqrtf((float)a->head_dim)) * LOG2E;
   p.dev_status = ctx->dev_status;
   p.page16 = a->page_size / 16;
@@ -1425,10 +1447,11 @@ hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
   hipError_t e = c.shape == F32 ? launch_f32(ctx, p) : (a->head_dim == 128 ? launch_bf16<128>(ctx, p, c) : launch_bf16<64>(ctx, p, c));
   if (e != hipSuccess) return e;
   if (c.parts > 1) {
-    const long long lanes = (long long)a->n_tokens * a->n_heads * ((a->head_dim + 3) / 4);
+    const dim3 grid((unsigned)((a->n_tokens * a->n_heads + 3) / 4));
     KernelTimer t(ctx, CASCADE_K_PAGED_MERGE);
-    if (a->dtype == CASCADE_BF16) CASCADE_TIMED_LAUNCH(t, paged_merge_kernel<uint16_t>, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, ctx->stream, p);
-    else CASCADE_TIMED_LAUNCH(t, paged_merge_kernel<float>, dim3((unsigned)((lanes + 255) / 256)), dim3(256), 0, ctx->stream, p);
+    if (a->dtype == CASCADE_F32) CASCADE_TIMED_LAUNCH(t, (paged_merge_kernel<float, 4>), grid, dim3(256), 0, ctx->stream, p);
+    else if (a->head_dim == 128) CASCADE_TIMED_LAUNCH(t, (paged_merge_kernel<uint16_t, 2>), grid, dim3(256), 0, ctx->stream, p);
+    else CASCADE_TIMED_LAUNCH(t, (paged_merge_kernel<uint16_t, 1>), grid, dim3(256), 0, ctx->stream, p);
   }
   return hipGetLastError();
 }
