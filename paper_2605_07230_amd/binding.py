@@ -400,12 +400,14 @@ def paged_slots(ctx: Context, *, seq_len, block_table, free_pages, free_count, p
                 new_len=None, position=None, source=None, node_off=None, row_prompt=None, accept_len=None, path_nodes=None, n_nodes_total: int = 0) -> None:
     """block_table [S, width] int32 (last dim contiguous), extended in place; seq_len / seq_len_out / new_len [S]; free_pages [any], free_count /
     free_count_out [1]; q_off [S+1]; slot_map / position / source [max_tokens].  Without new_len the rows keep select_path's paths."""
-    assert block_table.stride(1) == 1
+    table_stride, one = block_table.stride()
+    assert one == 1
+    at = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
     _check(ctx.lib.paged_slots_record(ctx.handle, _SLOTS(
-        seq_len.numel(), page_size, n_pages, block_table.shape[1], block_table.stride(0), slot_map.numel(), free_pages.numel(), seq_len.data_ptr(),
-        *_ptrs(new_len, node_off, row_prompt, accept_len, path_nodes), accept_len.numel() if accept_len is not None else 0,
-        path_nodes.shape[1] if path_nodes is not None else 0, n_nodes_total,
-        *_ptrs(block_table, free_pages, free_count, free_count_out, q_off, slot_map, position, source, seq_len_out))))
+        seq_len.numel(), page_size, n_pages, block_table.shape[1], table_stride, slot_map.numel(), free_pages.numel(), seq_len.data_ptr(), at(new_len), at(node_off),
+        at(row_prompt), at(accept_len), at(path_nodes), accept_len.numel() if accept_len is not None else 0,
+        path_nodes.shape[1] if path_nodes is not None else 0, n_nodes_total, block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+        free_count_out.data_ptr(), q_off.data_ptr(), slot_map.data_ptr(), at(position), at(source), seq_len_out.data_ptr())))
 
 
 def paged_append(ctx: Context, *, k_new, v_new, slot_map, k_pages, v_pages, source=None) -> None:
@@ -420,20 +422,27 @@ def paged_append(ctx: Context, *, k_new, v_new, slot_map, k_pages, v_pages, sour
 
 def _paged_attn_record(q_off, prefix_len, block_table, q, k_new, v_new, k_pages, v_pages, out, lse, parent, scale, window, n_sink, max_new,
                        max_prefix_len, workspace) -> bytes:
-    shape, q_stride, kv_stride = q.shape, q.stride(), k_new.stride()
-    D = shape[2]
-    assert out.is_contiguous() and out.shape == shape and out.dtype == q.dtype == k_new.dtype == v_new.dtype and k_new.shape == v_new.shape
-    assert q_stride[1:] == (D, 1) and kv_stride == v_new.stride() and kv_stride[1:] == (D, 1) and k_new.shape[2] == D and k_new.shape[0] == shape[0]
+    # every look at a tensor costs 0.1 to 0.2 us of a call that takes 10: each is taken once
+    shape, kv_shape, dtype = q.shape, k_new.shape, q.dtype
+    n, heads, D = shape
+    n_kv, kv_heads, D_kv = kv_shape
+    q_stride, q_head, q_one = q.stride()
+    kv_strides = k_new.stride()
+    assert (D_kv == D == q_head == kv_strides[1] and q_one == 1 == kv_strides[2] and n_kv == n and kv_strides == v_new.stride() and kv_shape == v_new.shape
+            and out.shape == shape and out.is_contiguous() and dtype is k_new.dtype and dtype is v_new.dtype and dtype is out.dtype)
     if k_pages is not None:
-        pages, page_size, stride = k_pages.shape[0], k_pages.shape[2], k_pages.stride()
-        assert stride == v_pages.stride() and k_pages.shape == v_pages.shape and stride[3] == 1 and k_pages.shape[1::2] == k_new.shape[1:]
-        assert k_pages.dtype == v_pages.dtype == q.dtype and block_table.stride(1) == 1
-        width, table_stride = block_table.shape[1], block_table.stride(0)
+        pool, (page_stride, head_stride, pos_stride, one) = k_pages.shape, k_pages.stride()
+        pages, pool_heads, page_size, pool_D = pool
+        table_stride, table_one = block_table.stride()
+        assert (pool_heads == kv_heads and pool_D == D and one == 1 == table_one and (page_stride, head_stride, pos_stride, 1) == v_pages.stride()
+                and pool == v_pages.shape and dtype is k_pages.dtype and dtype is v_pages.dtype)
+        width, kp, vp, table = block_table.shape[1], k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr()
     else:
-        pages, page_size, stride, width, table_stride = 0, 16, (0, 0, 0, 1), 0, 0
-    return _PAGED_ATTN(_dtype_code(q), prefix_len.numel(), *_ptrs(q_off, parent, prefix_len), shape[0], max_new, max_prefix_len, shape[1], k_new.shape[1], D,
-                       scale, window, n_sink, *_ptrs(q, k_new, v_new), q_stride[0], kv_stride[0], *_ptrs(k_pages, v_pages), *stride[:3], pages, page_size,
-                       _ptr(block_table), table_stride, width, *_ptrs(out, lse, workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0)
+        pages, page_size, page_stride, head_stride, pos_stride, table_stride, width, kp, vp, table = 0, 16, 0, 0, 0, 0, 0, 0, 0, 0
+    return _PAGED_ATTN(_dtype_code(q), prefix_len.numel(), q_off.data_ptr(), 0 if parent is None else parent.data_ptr(), prefix_len.data_ptr(), n, max_new,
+                       max_prefix_len, heads, kv_heads, D, scale, window, n_sink, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), q_stride, kv_strides[0], kp, vp,
+                       page_stride, head_stride, pos_stride, pages, page_size, table, table_stride, width, out.data_ptr(), 0 if lse is None else lse.data_ptr(),
+                       *((0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())))
 
 
 def paged_attn(ctx: Context, *, q_off, prefix_len, block_table, q, k_new, v_new, k_pages, v_pages, out, lse=None, parent=None, scale: float = 0.0,

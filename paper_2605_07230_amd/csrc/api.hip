@@ -23,6 +23,24 @@ size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 bool bad_float(float x) { return isnan(x); }
 
+// The calls on pages and samples run on the device that their context was made on, whichever one is current.
+struct OnDevice {
+  int before = -1;
+  hipError_t error;
+  explicit OnDevice(int device) {
+    error = hipGetDevice(&before);
+    if (error == hipSuccess && before != device) error = hipSetDevice(device);
+    else before = -1;
+  }
+  ~OnDevice() { if (before >= 0) (void)hipSetDevice(before); }
+};
+template <typename Launch>
+int on_device(const cascade_ctx* ctx, Launch launch) {
+  OnDevice on(ctx->device);
+  const hipError_t e = on.error == hipSuccess ? launch() : on.error;
+  return e == hipSuccess ? CASCADE_OK : hip_fail(e);
+}
+
 }  // namespace
 
 extern "C" {
@@ -447,8 +465,7 @@ int paged_slots(cascade_ctx* ctx, const paged_slots_args* a) {
   if (st != CASCADE_OK) return st;
   if (a->n_rows > ctx->lim.max_rows || (int64_t)a->table_width * a->page_size > 0x7fffffff) return CASCADE_ESHAPE;
   if (a->n_rows == 0) return CASCADE_OK;
-  hipError_t err = launch_paged_slots(ctx, a);
-  return err == hipSuccess ? CASCADE_OK : hip_fail(err);
+  return on_device(ctx, [&] { return launch_paged_slots(ctx, a); });
 }
 
 int paged_append(cascade_ctx* ctx, const paged_append_args* a) {
@@ -467,8 +484,7 @@ int paged_append(cascade_ctx* ctx, const paged_append_args* a) {
   if (((uintptr_t)a->k_new | (uintptr_t)a->v_new | (uintptr_t)a->k_pages | (uintptr_t)a->v_pages) & 15) return CASCADE_EINVAL;
   if (a->n_layers > 65535 || (int64_t)a->n_tokens * a->n_kv_heads * (a->head_dim * e / 16) > 0x7fffffff) return CASCADE_ESHAPE;
   if (a->n_layers == 0 || a->n_tokens == 0) return CASCADE_OK;
-  hipError_t err = launch_paged_append(ctx, a);
-  return err == hipSuccess ? CASCADE_OK : hip_fail(err);
+  return on_device(ctx, [&] { return launch_paged_append(ctx, a); });
 }
 
 static int check_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a) {
@@ -512,8 +528,7 @@ int paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
   if (st != CASCADE_OK) return st;
   if (a->n_rows == 0 || a->n_tokens == 0) return CASCADE_OK;
   if (a->max_new == 0) return CASCADE_ESHAPE;   // the grids are sized by the bound: tokens without one are a contradiction
-  hipError_t err = launch_paged_attn(ctx, a);
-  return err == hipSuccess ? CASCADE_OK : hip_fail(err);
+  return on_device(ctx, [&] { return launch_paged_attn(ctx, a); });
 }
 
 int paged_attn_workspace(const cascade_ctx* ctx, const paged_attn_args* a, int64_t* bytes) {
@@ -533,8 +548,7 @@ int sample_tokens(cascade_ctx* ctx, const sample_args* a) {
   if (a->n_rows < 0 || a->vocab <= 0) return CASCADE_EINVAL;
   if (a->vocab > ctx->lim.vocab || (a->row_stride < a->vocab && a->n_rows > 1)) return CASCADE_ESHAPE;
   if (a->n_rows == 0) return CASCADE_OK;
-  hipError_t err = launch_sample(ctx, a);
-  return err == hipSuccess ? CASCADE_OK : hip_fail(err);
+  return on_device(ctx, [&] { return launch_sample(ctx, a); });
 }
 
 }  // extern "C"

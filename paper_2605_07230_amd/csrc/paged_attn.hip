@@ -565,10 +565,11 @@ __device__ __forceinline__ RowInfo block_row(const PagedParams& p, int blk, int 
     if (a.n_rows > 1 && a.n_rows <= 64) {
       const int work = at < a.n_rows ? (mine.flag ? 0 : mine.P + mine.T) : -1;
       int rank = 0;
-      for (int r = 0; r < 64; ++r) {
+      for (int r = 0; r < a.n_rows; ++r) {
         const int w = __builtin_amdgcn_readlane(work, r);
         rank += (w > work || (w == work && r < lane)) ? 1 : 0;
       }
+      if (lane >= a.n_rows) rank = lane;
       from = __builtin_amdgcn_ds_permute(4 * rank, lane);
       nb = __builtin_amdgcn_ds_bpermute(4 * from, nb);
     }
@@ -588,7 +589,7 @@ __device__ __forceinline__ RowInfo block_row(const PagedParams& p, int blk, int 
 }
 
 template <int D, int NS, int NQ, int NW, bool TREE>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_ring_kernel(PagedParams p) {
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3) : 2)) void paged_ring_kernel(PagedParams p) {
   using GM = RingGeom<D>;
   constexpr int NT = 64 * NW, RW = 16 * NQ * NW, KS = D / 32, DB = D / 16;
   constexpr int CPW = GM::CPT / NW;     // loads of K (and of V) that a wave makes per tile
@@ -617,8 +618,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_ring_kernel(Pa
   const RowInfo ri = block_row(p, b / p.parts, RW, lane, &sb);
   if (ri.s < 0) return;   // the grid is an upper bound of the number of blocks
   if (ri.flag) { write_nothing<uint16_t>(p, ri, kvh, part, tid, NT); return; }
-  const int lo = ri.lo, T = ri.T, P = ri.P, M = T * G, row0 = sb * RW;
-  const int i0 = token_of(p, row0), i1 = token_of(p, min(row0 + RW, M) - 1);
+  auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const int lo = uniform(ri.lo), T = uniform(ri.T), P = uniform(ri.P), M = T * G, row0 = uniform(sb) * RW;
+  const int i0 = uniform(token_of(p, row0)), i1 = uniform(token_of(p, min(row0 + RW, M) - 1));
   const Tiles ti = tiles_of(p, P, i0, i1, TREE);
   const int nt = ti.n_p + ti.n_n, per = (nt + p.parts - 1) / p.parts, t_begin = part * per, t_end = min(nt, t_begin + per);
   const long long all_rows = (long long)a.n_tokens * a.n_heads;
@@ -649,34 +651,39 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_ring_kernel(Pa
   // Where the wave's keys of a tile come from: the first key of their group, and how many keys are behind it.  Tiles past the part's end are its
   // last one again (the number of loads stays fixed; what they bring is not used), keys past the end are the last one again, masked.
   struct Source {
-    long long off;   // bytes from k_pages / v_pages, or from the row's new keys / values
+    long long off;   // bytes from the first page's or the row's first new key
     int last;        // keys of the group behind the first
     bool fresh;
   };
   const int e0 = ti.n_p > 0 ? page_index(p, 4 * min(ti.prefix_tile(max(min(t_begin, ti.n_p - 1), ti.sinks_p)), (P - 1) / KT)) : 0;
   const int n_staged = ti.n_p > 0 ? min(STAGED, page_index(p, (P - 1) >> 4) + 1 - e0) : 0;
-  auto group_of = [&](int t) { return needed_group(p, ti, P, 4 * ti.prefix_tile(t) + wave_group); };   // t < n_p
+  const ConstTable table = (ConstTable)(uintptr_t)a.block_table + (long long)ri.s * a.table_stride;
+  const long long page_bytes = 2 * a.stride_page;
+  const unsigned group_bytes = 16u * pitch_p;   // (stride_pos is at most 2^25)
+  // (without a branch: it stands among the products of a step)
+  const int first = ti.first, seen_group = first < P ? first >> 4 : (min(a.n_sink, P) - 1) >> 4, sinks = a.window > 0 ? a.n_sink : P;
+  auto group_of = [&](int t) {   // as needed_group; t < n_p
+    const int g = min(4 * ti.prefix_tile(t) + wave_group, (P - 1) >> 4);
+    return 16 * g >= sinks && 16 * g + 15 < first ? seen_group : g;
+  };
+  const unsigned inv = p.page16_inv, whole = inv ? 0u : 1u;
+  auto entry_of = [&](int g) { return (int)(__umulhi((unsigned)g, inv) + whole * (unsigned)g); };
   auto source_of = [&](int t, int page) {
     Source s;
     s.fresh = t >= ti.n_p;
-    if (!s.fresh) {
-      const int gq = group_of(t);
-      s.off = 2 * group_offset(p, checked_page(p, page), page_index(p, gq), gq, kvh);
-      s.last = P - 1 - 16 * gq;
-    } else {
-      const int gq = min(4 * ti.new_tile(t - ti.n_p) + wave_group, (T - 1) >> 4);
-      s.off = (long long)(16 * gq) * pitch_n;
-      s.last = T - 1 - 16 * gq;
-    }
+    const int gp = group_of(min(t, ti.n_p - 1)), gn = min(4 * ti.new_tile(t - ti.n_p) + wave_group, (T - 1) >> 4), gq = s.fresh ? gn : gp;
+    const long long in_pages = (long long)(s.fresh ? 0 : checked_page(p, page)) * page_bytes + (long long)(gp - entry_of(gp) * p.page16) * group_bytes;
+    s.off = s.fresh ? (long long)(16 * gn) * pitch_n : in_pages;
+    s.last = (s.fresh ? T : P) - 1 - 16 * gq;
     return s;
   };
-  auto entry_now = [&](int t) { return t < ti.n_p ? table_entry(p, ri.s, page_index(p, group_of(t))) : 0; };
+  auto entry_now = [&](int t) { return t < ti.n_p ? table[entry_of(group_of(t))] : 0; };
   auto entry_staged = [&](int t) {
     if (t >= ti.n_p) return 0;
-    const int e = page_index(p, group_of(t)), at = e - e0;
-    return at >= 0 && at < n_staged ? s_page[at] : table_entry(p, ri.s, e);
+    const int e = entry_of(group_of(t)), at = e - e0;
+    return at >= 0 && at < n_staged ? s_page[at] : table[e];
   };
-  const char *kc = (const char*)a.k_pages, *vc = (const char*)a.v_pages;
+  const char *kc = (const char*)((const uint16_t*)a.k_pages + kvh * a.stride_head), *vc = (const char*)((const uint16_t*)a.v_pages + kvh * a.stride_head);
   const char* kn = (const char*)((const uint16_t*)a.k_new + lo * a.kv_stride + kvh * D);
   const char* vn = (const char*)((const uint16_t*)a.v_new + lo * a.kv_stride + kvh * D);
   auto request = [&](const Source& s, int stage, bool is_v) {
@@ -828,7 +835,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_ring_kernel(Pa
     }
   };
   if (TREE && t_begin >= ti.n_p) build_mask(t_begin);
+  // the source of the K requested next is worked out a step ahead, among the products
   int entry = entry_staged(clamped(t_begin + NS));
+  Source next;
   wait_and_sync<LPI * (NS - 1)>();    // K of the first tile everywhere (and the first mask)
   float lmax[NQ];                     // lane_max of the scores in st
   {
@@ -848,15 +857,14 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void paged_ring_kernel(Pa
     constexpr int ST_K = (ST + 1) % NS;             // stage of K(t+1)
     constexpr int ST_VNEW = (ST + NS - 1) % NS;     // V(t + NS - 1) goes where V(t - 1) was
     wait_and_sync<LPI * (NS - 2)>();   // K(t+1), V(t) landed everywhere; K(t), V(t-1) free
-    {
-      const Source s = source_of(clamped(t + NS), __builtin_amdgcn_readfirstlane(entry));
-      request(s, ST, false);
-      request(before, ST_VNEW, true);
-      before = s;
-    }
+    next = source_of(clamped(t + NS), __builtin_amdgcn_readfirstlane(entry));
+    request(next, ST, false);
+    request(before, ST_VNEW, true);
+    before = next;
+    entry = entry_staged(clamped(t + NS + 1));
+    __builtin_amdgcn_sched_barrier(0);
     Frag8 kf[2][KS];
     load_kfrags(kf[0], ST_K, 0);       // in flight during the reference check
-    entry = entry_staged(clamped(t + NS + 1));
     if (TREE && t + 1 < t_end && t + 1 >= ti.n_p) build_mask(t + 1);   // read behind the next barrier
 
     // ---- masks
@@ -1345,8 +1353,14 @@ Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
   }
   c.shape = M <= 16 ? FEW_16 : FEW_32;
   const int64_t heads = (int64_t)a->n_rows * a->n_kv_heads;
-  int parts = std::max(1, std::min({most, tiles / 8, (int)((2 * n_cu + heads - 1) / heads)}));
-  if (heads >= 2 * n_cu && tiles > 32) parts = std::max(1, std::min(most, tiles / 8));
+  // A wave takes 4-5 us to a tile whose keys come from memory, so few (row, kv head) pairs are cut until there is a part for every compute unit (up to 16: joining
+  // more takes longer than they save), unless that saves less than the join's 4 us.  Pairs that fill the chip by themselves are cut in two, for rows of different lengths:
+  // 64 rows of 90-4200 keys, 8 kv heads 140.7 -> 136.4 us, 40 of 100-1500 45.8 -> 39.8 (all of them 4200 keys: 199 -> 211).
+  int parts = (int)std::min<int64_t>(n_cu / heads, 16);
+  const int alone = (tiles + 7) / 8, cut = parts > 1 ? (tiles + 8 * parts - 1) / (8 * parts) : alone;
+  if (alone - cut < (parts >= 4 ? 1 : 2)) parts = 1;
+  if (heads > n_cu && tiles >= 16) parts = 2;
+  parts = std::max(1, std::min(parts, most));
   c.part_tiles = (tiles + parts - 1) / parts;
   c.parts = (tiles + c.part_tiles - 1) / c.part_tiles;
   return c;
