@@ -8,6 +8,9 @@ synthetic step inputs (``workloads.make_config``) that is cycled through, which 
 stochastic drafter and the target's forward pass.  What is real is the chain: the prefix grows by
 what the walk accepted, so attention reads what earlier steps committed.
 
+``PagedLoop`` is the same chain for a batch of prompts whose prefixes lie in pages: prompts arrive in chunks, steps verify trees or draw
+one token per prompt, and rows take pages as they grow.
+
 Host logic only; every computation runs in the library's kernels.
 """
 from __future__ import annotations
@@ -179,3 +182,73 @@ class DecodeLoop:
             raise binding.CascadeError(binding.ETREE)
         return LoopResult(steps=n, tokens=tokens, accept_lens=accept_lens, tvd_used=tvds, emitted=emitted, seconds=seconds,
                           records=records)
+
+
+class PagedLoop:
+    """A batch of prompts (with their guidance rows, if any) over a cache in pages.
+
+    The step inputs are one synthetic record, as in ``DecodeLoop``; ``prompt_k`` / ``prompt_v`` of ``admit`` stand for what a model makes of
+    the prompts' tokens.  Lengths, tables and free pages live on the device: a step needs nothing from the host but a bound of the prefix lengths."""
+
+    def __init__(self, inp, page_size: int = 64, n_pages: Optional[int] = None, max_len: int = 4096, max_chunk: int = 1024, device: str = "cuda:0"):
+        self.inp, self.page_size, self.max_len, self.max_chunk = inp, page_size, max_len, max_chunk
+        self.dev = torch.device(device)
+        self.step_in = binding.DeviceStep(inp, device)
+        S, width = inp.n_rows, -(-max_len // page_size)
+        self.n_pages = S * width if n_pages is None else n_pages
+        self.ctx = binding.Context(max_rows=max(S, inp.n_prompts), max_nodes_total=max(inp.q.shape[0], S * max_chunk), max_nodes_per_tree=self.step_in.max_tree,
+                                   max_prefix=max_len, n_heads=inp.n_heads, head_dim=inp.head_dim, hidden=inp.hidden, vocab=inp.vocab)
+        self.step_in.ctx = self.ctx
+        i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=self.dev)  # noqa: E731
+        dt = self.step_in.q.dtype
+        self.k_pages = torch.zeros((1, self.n_pages, inp.n_kv_heads, page_size, inp.head_dim), dtype=dt, device=self.dev)
+        self.v_pages = torch.zeros_like(self.k_pages)
+        self.block_table = i32(S, width)
+        self.free_pages = torch.arange(self.n_pages - 1, -1, -1, dtype=torch.int32, device=self.dev)
+        self.free_count, self.free_next = torch.full((1,), self.n_pages, dtype=torch.int32, device=self.dev), i32(1)
+        self.seq_len, self.seq_next = i32(S), i32(S)
+        self.row_prompt = torch.tensor([s * inp.n_prompts // S if S == inp.n_prompts else s // 2 for s in range(S)], dtype=torch.int32, device=self.dev)
+        self.q_off = i32(S + 1)
+        self.longest = 0                       # host bound on the rows' lengths
+        self.rows = inp.n_rows
+
+    def _place(self, tokens: int, **lengths):
+        """Pages and slots for new tokens; the rows' lengths become those behind them."""
+        slot_map, source = (torch.empty(tokens, dtype=torch.int32, device=self.dev) for _ in range(2))
+        binding.paged_slots(self.ctx, seq_len=self.seq_len, block_table=self.block_table, free_pages=self.free_pages, free_count=self.free_count,
+                            page_size=self.page_size, n_pages=self.n_pages, q_off=self.q_off, slot_map=slot_map, source=source, seq_len_out=self.seq_next,
+                            free_count_out=self.free_next, **lengths)
+        self.seq_len, self.seq_next = self.seq_next, self.seq_len
+        self.free_count, self.free_next = self.free_next, self.free_count
+        return slot_map, source
+
+    def admit(self, q, k_new, v_new, new_len, out, lse=None):
+        """A chunk of every row's prompt, packed row by row: its attention over what is there and over itself, then its keys and values go to
+        the pages.  new_len: host lengths."""
+        lens = torch.tensor(new_len, dtype=torch.int32, device=self.dev)
+        before = self.seq_len.clone()
+        slot_map, _ = self._place(q.shape[0], new_len=lens)
+        binding.paged_attn(self.ctx, q_off=self.q_off, prefix_len=before, block_table=self.block_table, q=q, k_new=k_new, v_new=v_new, k_pages=self.k_pages[0],
+                           v_pages=self.v_pages[0], out=out, lse=lse, max_new=max(new_len), max_prefix_len=self.longest)
+        binding.paged_append(self.ctx, k_new=k_new.unsqueeze(0), v_new=v_new.unsqueeze(0), slot_map=slot_map, k_pages=self.k_pages, v_pages=self.v_pages)
+        self.longest = min(self.longest + max(new_len), self.max_len)
+
+    def step(self, mode: int = binding.WALK_SEQUENTIAL) -> None:
+        """One verification step of every prompt's tree over the pages, and the commit of what it accepts to them."""
+        st = self.step_in
+        binding.paged_attn(self.ctx, q_off=st.row_node_off, parent=st.row_parent, prefix_len=self.seq_len, block_table=self.block_table, q=st.q, k_new=st.k_tree,
+                           v_new=st.v_tree, k_pages=self.k_pages[0], v_pages=self.v_pages[0], out=st.attn_out, lse=st.attn_lse, max_new=st.max_tree,
+                           max_prefix_len=self.longest)
+        st.lmhead()
+        st.accept()
+        st.select(mode)
+        slot_map, source = self._place(self.rows * (st.max_depth + 1), node_off=st.row_node_off, row_prompt=self.row_prompt, accept_len=st.accept_len,
+                                       path_nodes=st.path_nodes, n_nodes_total=st.q.shape[0])
+        binding.paged_append(self.ctx, k_new=st.k_tree.unsqueeze(0), v_new=st.v_tree.unsqueeze(0), slot_map=slot_map, source=source, k_pages=self.k_pages,
+                             v_pages=self.v_pages)
+        self.longest = min(self.longest + st.max_depth + 1, self.max_len)
+
+    def draw(self, u, token, prob=None, **parameters) -> None:
+        """Plain decoding: one token of every prompt from the logits of its tree's root (of the last ``step``), with each prompt's own sampling parameters."""
+        roots = self.step_in.node_off[:-1].long()
+        binding.sample_tokens(self.ctx, logits=self.step_in.logits.index_select(0, roots), u=u, token=token, prob=prob, **parameters)
