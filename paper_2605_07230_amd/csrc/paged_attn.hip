@@ -750,17 +750,15 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
     }
   }
   f32x4 ot[NQ][DB];
-  f32x4 lsum[NQ];        // row sums of the (bf16) probabilities, from the matrix cores: every entry holds the sum
+  float lsum[NQ];        // this lane's part of the row sums, of the probabilities before they are rounded
   float m_ref[NQ];
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     m_ref[n] = -INFINITY;
-    lsum[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    lsum[n] = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db) ot[n][db] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  Frag8 ones;
-  ones.u = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
 
   // ---- LDS addresses (see the comment on slots): K fragment (kt, ks): key 16 kt + l16, piece 4 ks + g; V operand (db, j): keys 32 j + 4 g + (l16 >> 2)
   // (+ 16), four d at 16 db + 4 (l16 & 3).  ks and db enter by XOR, the stage, kt and j are constants.
@@ -947,6 +945,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
         float e[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) e[c] = fast_exp2(fmaf(st[n][kt][c], p.scale_log2e, m_neg[n]));   // -inf stays -inf -> 0
+        lsum[n] += (e[0] + e[1]) + (e[2] + e[3]);
         const uint32_t lo2 = pack_bf16x2(e[0], e[1]), hi2 = pack_bf16x2(e[2], e[3]);
         if (kt & 1) { pf[n][kt >> 1].u.z = lo2; pf[n][kt >> 1].u.w = hi2; }
         else { pf[n][kt >> 1].u.x = lo2; pf[n][kt >> 1].u.y = hi2; }
@@ -966,11 +965,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
       score_kt(kf[kt & 1], kt);
       if (kt < 3) probs_kt(kt + 1);
     }
-    // ---- O^T += V^T P^T, row sums += ones P^T; the vector ALU meanwhile looks at the next tile's scores
-#pragma unroll
-    for (int n = 0; n < NQ; ++n)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) lsum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones.v, pf[n][j].v, lsum[n], 0, 0, 0);
+    // ---- O^T += V^T P^T; the vector ALU meanwhile looks at the next tile's scores
 #pragma unroll
     for (int n = 0; n < NQ; ++n) lmax[n] = lane_max(n);
 #pragma unroll
@@ -995,8 +990,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
   // epilogue: lane (query l16, g) owns d = 16 db + 4 g + c
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
+    const float l = rows4_sum(lsum[n]);
     if (qi[n] < 0) continue;
-    const float l = lsum[n][0];
     if (p.parts > 1) {
       const long long w = part * all_rows + out_row[n];
 #pragma unroll

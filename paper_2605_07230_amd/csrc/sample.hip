@@ -120,7 +120,7 @@ struct Shared {
 // What a row's weights are measured in.
 struct Row {
   double m, c;        // where a weight is 1, log2(e) / T
-  float m32, scale;   // the former again, bins per unit below it
+  float m32, scale;   // where the bins begin, bins per unit below it
   __device__ __forceinline__ void at(float top, float temp) {
     m = top;
     m32 = top;
@@ -412,9 +412,10 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleParams p) {
   near_max = all_max(near_max);
   const bool sampled = near_max > -INFINITY && near_max < INFINITY;
   Row row;
-  // the row's maximum is mostly a little above the sample's: weights and bins are measured from five temperatures above that
-  const float above = near_max + 5.f * temp;
-  row.at(!sampled ? 0.f : (above < INFINITY ? above : near_max), temp);
+  // The row's maximum is mostly above the sample's: bins begin fifteen temperatures above that (five left a third of the rows of a normal distribution of 6.7
+  // temperatures above the bins).  A weight of exactly 1 at the sample's maximum keeps the sums of rows of one value whole numbers.
+  row.at(sampled ? near_max : 0.f, temp);
+  if (sampled && near_max + 15.f * temp < INFINITY) row.m32 = near_max + 15.f * temp;
   auto row_bin = [&](float x) { return row.bin(x); };
   auto row_mass = [&](float x) { return mass_of(row.weight(x)); };
   const bool top_k = k > 0 && k < V;
@@ -425,19 +426,25 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleParams p) {
     if (!(cut >= LOWEST)) cut = LOWEST;
   }
   if (sampled && !list_all && ((top_k && k <= MOST_SAMPLED) || cut > LOWEST)) {
-    clear_bins(sh);
-    if (tid == 0) sh.at_bin = BINS - 1;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (sample[i] >= cut) atomicAdd((unsigned*)&sh.bin[row.bin(sample[i])], 1u);
-    __syncthreads();
-    // some more than k entries, as a share of the sample
+    // some more than k entries, as a share of the sample; bins sixteen times as wide where these lie too far below the maximum
     const float share = top_k && k <= MOST_SAMPLED ? (float)max(k + k / 4 + 300, 1500) * (4.f * NT) / (float)V : 4.f * NT;
     u64 hits = 0;
-    crossing(sh, [&](u64 total) { hits = total; return (u64)share + 1; });
-    if ((float)hits > share) { cut = fmaxf(cut, row.m32 - (float)(sh.at_bin + 1) / row.scale); cut_by_k = true; }
-    list_all = fminf((float)hits, share) * (float)V < 3900.f * 4.f * NT;   // (the estimate of what is above the cut)
+    float scale = row.scale;
+#pragma unroll 1
+    for (int wide = 0; wide < 3; ++wide, scale *= 1.f / 16) {
+      clear_bins(sh);
+      if (tid == 0) sh.at_bin = BINS - 1;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (sample[i] >= cut) atomicAdd((unsigned*)&sh.bin[(int)__builtin_amdgcn_fmed3f((row.m32 - sample[i]) * scale, 0.f, (float)(BINS - 1))], 1u);
+      __syncthreads();
+      crossing(sh, [&](u64 total) { hits = total; return (u64)share + 1; });
+      if (!((float)hits > share) || sh.at_bin < BINS - 1) break;
+      __syncthreads();
+    }
+    if ((float)hits > share && sh.at_bin < BINS - 1) { cut = fmaxf(cut, row.m32 - (float)(sh.at_bin + 1) / scale); cut_by_k = true; }
+    list_all = (cut_by_k || !((float)hits > share)) && fminf((float)hits, share) * (float)V < 3900.f * 4.f * NT;   // (the estimate of what is above the cut)
   } else if (!list_all) {
     cut = LOWEST;
   }
