@@ -498,8 +498,8 @@ int paged_append(cascade_ctx* ctx, const paged_append_args* args);
  * its output.  Tokens behind q_off[n_rows] are not written.  A row whose q_off is not in order or in n_tokens, that has more than
  * max_new tokens, or whose prefix is negative or longer than max_prefix_len or its table, gets zeros and lse = -inf and sets the flag; an
  * entry of the table outside the pool sets it too, and what the tokens that need it get is then not defined (the pool's first page is read).
- * bf16: head_dim 64 or 128; strides multiples of 8 elements, stride_pos and kv_stride at most 2^25, buffers on 16-byte boundaries.  f32: any
- * head_dim up to 256.
+ * bf16: head_dim 64 or 128; strides multiples of 8 elements, stride_pos and kv_stride at most 2^25, buffers on 16-byte boundaries,
+ * n_tokens * n_heads at most 2^30.  f32: any head_dim up to 256, n_tokens * n_heads at most 2^25.
  *
  * Keys may be cut into parts whose results are joined by a second kernel.  Those partial results lie in `workspace` if it is given,
  * else in the context's.  A call that is recorded into a graph without a workspace of its own takes its keys whole, so

@@ -505,7 +505,7 @@ static int check_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a) {
   if (a->n_rows > L.max_rows || a->n_tokens > L.max_nodes_total || a->max_prefix_len > L.max_prefix || a->n_heads > L.n_heads || a->head_dim > L.head_dim)
     return CASCADE_ESHAPE;
   if (a->parent && a->max_new > L.max_nodes_per_tree) return CASCADE_ESHAPE;
-  // positions and what a launch counts stay below 2^30
+  // positions and what a launch counts stay below 2^30 (f32: up to 1024 threads to 16 query rows)
   if (a->max_prefix_len > (1 << 30) || a->max_new > (1 << 30) || (int64_t)a->n_tokens * a->n_heads > (1 << 30) || a->n_kv_heads > 65535 ||
       (double)a->max_new * (a->n_heads / a->n_kv_heads) * (a->n_heads / a->n_kv_heads) >= 4294967296.0)
     return CASCADE_ESHAPE;
@@ -515,7 +515,7 @@ static int check_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a) {
     if (a->stride_pos > (1 << 25) || a->kv_stride > (1 << 25)) return CASCADE_ESHAPE;   // sixteen keys lie within 32-bit offsets
     if (((uintptr_t)a->q | (uintptr_t)a->k_new | (uintptr_t)a->v_new | (uintptr_t)a->k_pages | (uintptr_t)a->v_pages | (uintptr_t)a->out) & 15)
       return CASCADE_EINVAL;
-  } else if (a->head_dim > 256) {
+  } else if (a->head_dim > 256 || (int64_t)a->n_tokens * a->n_heads > (1 << 25)) {
     return CASCADE_ESHAPE;
   }
   if ((uintptr_t)a->workspace & 15) return CASCADE_EINVAL;

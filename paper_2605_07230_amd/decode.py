@@ -188,11 +188,16 @@ class PagedLoop:
     """A batch of prompts (with their guidance rows, if any) over a cache in pages.
 
     The step inputs are one synthetic record, as in ``DecodeLoop``; ``prompt_k`` / ``prompt_v`` of ``admit`` stand for what a model makes of
-    the prompts' tokens.  Lengths, tables and free pages live on the device: a step needs nothing from the host but a bound of the prefix lengths."""
+    the prompts' tokens.  Lengths, tables and free pages live on the device: a step needs nothing from the host but a bound of the prefix lengths.
+    Calls run on the stream that was current when the loop was made; inputs have to be ready for it."""
 
     def __init__(self, inp, page_size: int = 64, n_pages: Optional[int] = None, max_len: int = 4096, max_chunk: int = 1024, device: str = "cuda:0"):
         self.inp, self.page_size, self.max_len, self.max_chunk = inp, page_size, max_len, max_chunk
         self.dev = torch.device(device)
+        with torch.cuda.device(self.dev):
+            self._allocate(inp, page_size, n_pages, max_len, max_chunk, device)
+
+    def _allocate(self, inp, page_size, n_pages, max_len, max_chunk, device) -> None:
         self.step_in = binding.DeviceStep(inp, device)
         S, width = inp.n_rows, -(-max_len // page_size)
         self.n_pages = S * width if n_pages is None else n_pages
@@ -225,12 +230,17 @@ class PagedLoop:
     def admit(self, q, k_new, v_new, new_len, out, lse=None):
         """A chunk of every row's prompt, packed row by row: its attention over what is there and over itself, then its keys and values go to
         the pages.  new_len: host lengths."""
-        lens = torch.tensor(new_len, dtype=torch.int32, device=self.dev)
-        before = self.seq_len.clone()
-        slot_map, _ = self._place(q.shape[0], new_len=lens)
-        binding.paged_attn(self.ctx, q_off=self.q_off, prefix_len=before, block_table=self.block_table, q=q, k_new=k_new, v_new=v_new, k_pages=self.k_pages[0],
-                           v_pages=self.v_pages[0], out=out, lse=lse, max_new=max(new_len), max_prefix_len=self.longest)
-        binding.paged_append(self.ctx, k_new=k_new.unsqueeze(0), v_new=v_new.unsqueeze(0), slot_map=slot_map, k_pages=self.k_pages, v_pages=self.v_pages)
+        if len(new_len) != self.rows or min(new_len) < 0 or sum(new_len) > q.shape[0] or q.shape[0] > self.ctx.limits.max_nodes_total:
+            raise ValueError(f"chunks of {list(new_len)} tokens, {q.shape[0]} given: one chunk for each of {self.rows} rows, {self.ctx.limits.max_nodes_total} tokens together")
+        if max(new_len) == 0:
+            return
+        with torch.cuda.stream(self.ctx.stream):
+            lens = torch.tensor(new_len, dtype=torch.int32, device=self.dev)
+            before = self.seq_len.clone()
+            slot_map, _ = self._place(q.shape[0], new_len=lens)
+            binding.paged_attn(self.ctx, q_off=self.q_off, prefix_len=before, block_table=self.block_table, q=q, k_new=k_new, v_new=v_new, k_pages=self.k_pages[0],
+                               v_pages=self.v_pages[0], out=out, lse=lse, max_new=max(new_len), max_prefix_len=self.longest)
+            binding.paged_append(self.ctx, k_new=k_new.unsqueeze(0), v_new=v_new.unsqueeze(0), slot_map=slot_map, k_pages=self.k_pages, v_pages=self.v_pages)
         self.longest = min(self.longest + max(new_len), self.max_len)
 
     def step(self, mode: int = binding.WALK_SEQUENTIAL) -> None:
@@ -242,13 +252,15 @@ class PagedLoop:
         st.lmhead()
         st.accept()
         st.select(mode)
-        slot_map, source = self._place(self.rows * (st.max_depth + 1), node_off=st.row_node_off, row_prompt=self.row_prompt, accept_len=st.accept_len,
-                                       path_nodes=st.path_nodes, n_nodes_total=st.q.shape[0])
-        binding.paged_append(self.ctx, k_new=st.k_tree.unsqueeze(0), v_new=st.v_tree.unsqueeze(0), slot_map=slot_map, source=source, k_pages=self.k_pages,
-                             v_pages=self.v_pages)
+        with torch.cuda.stream(self.ctx.stream):
+            slot_map, source = self._place(self.rows * (st.max_depth + 1), node_off=st.row_node_off, row_prompt=self.row_prompt, accept_len=st.accept_len,
+                                           path_nodes=st.path_nodes, n_nodes_total=st.q.shape[0])
+            binding.paged_append(self.ctx, k_new=st.k_tree.unsqueeze(0), v_new=st.v_tree.unsqueeze(0), slot_map=slot_map, source=source, k_pages=self.k_pages,
+                                 v_pages=self.v_pages)
         self.longest = min(self.longest + st.max_depth + 1, self.max_len)
 
     def draw(self, u, token, prob=None, **parameters) -> None:
         """Plain decoding: one token of every prompt from the logits of its tree's root (of the last ``step``), with each prompt's own sampling parameters."""
-        roots = self.step_in.node_off[:-1].long()
-        binding.sample_tokens(self.ctx, logits=self.step_in.logits.index_select(0, roots), u=u, token=token, prob=prob, **parameters)
+        with torch.cuda.stream(self.ctx.stream):
+            roots = self.step_in.node_off[:-1].long()
+            binding.sample_tokens(self.ctx, logits=self.step_in.logits.index_select(0, roots), u=u, token=token, prob=prob, **parameters)

@@ -76,3 +76,11 @@ def test_draws(lib, ctx):
     r = B.sample_args(B.F32, 3, 4096, 64, 4096, 64, 64, 64, 64, 64, 64, 64)
     _refused(lib.sample_tokens, ctx, r, [(E, {k: None}) for k in ("logits", "u", "token")]
              + [(E, dict(n_rows=-1)), (E, dict(vocab=0)), (D, dict(dtype=2)), (S, dict(vocab=4097)), (S, dict(row_stride=4095)), (B.OK, dict(n_rows=0))])
+
+
+def test_attention_that_a_launch_cannot_count(lib):
+    buf = C.create_string_buffer(4096)
+    C.memmove(C.addressof(buf) + 8, C.byref(B.cascade_limits(4, 1 << 30, 32, 1 << 30, 128, 128, 256, 4096)), C.sizeof(B.cascade_limits))
+    r = B.paged_attn_args(B.BF16, 4, 64, 0, 64, 1, 1, 1000, 128, 128, 128, 0.0, 0, 0, 64, 64, 64, 16384, 16384, 64, 64, 4096, 2048, 128, 10, 16, 64, 63, 63, 64, 0, 0, 0)
+    _refused(lib.paged_attn, buf, r, [(S, dict(n_tokens=(1 << 23) + 1)), (S, dict(dtype=B.F32, n_tokens=(1 << 18) + 1)), (S, dict(max_new=(1 << 30) + 1)),
+                                      (S, dict(n_kv_heads=1, max_new=1 << 18)), (B.OK, dict(n_rows=0)), (B.OK, dict(n_tokens=0))])
