@@ -168,15 +168,15 @@ __device__ __forceinline__ void write_nothing(const PagedParams& p, const RowInf
 }
 
 // ------------------------------------------------------------------------------------------------------------ bf16, few query rows
-// Up to 16 NQ query rows (single tokens, a few of them): bound by the stream of keys and values, so every wave of a workgroup takes its own tiles - w, w + NW, ... of the part
+// Up to 16 query rows (single tokens, a few of them): bound by the stream of keys and values, so every wave of a workgroup takes its own tiles - w, w + NW, ... of the part
 // - and needs no barrier until their end, where the waves' maxima, sums and outputs meet in LDS.  Keys are loaded in operand order (16 bytes of
 // a key per lane), values through a region of LDS of the wave's own.  A workgroup works through parts (row, kv head, run of part_tiles tiles) until
 // none is left: rows of very different lengths share the chip, and no workgroup is launched for nothing.
 // One token of 64 rows x 4200 keys, 8 kv heads of 4, head_dim 128 (1.1 GB): 199 us = 5.5 TB/s; of 90 to 4200 keys (602 MB) 131 us and the join's 4; two rows x 312 keys, 32 kv heads: 11 us, of
 // which the chain row -> table -> tile -> join of the waves is all.  Sixty-four rows dealt longest first, every second round backwards: no faster (131 -> 146).
-template <int D, int NQ, int NW, bool TREE>
+template <int D, int NW, bool TREE>
 __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_few_kernel(PagedParams p) {
-  constexpr int NT = 64 * NW, KS = D / 32, DB = D / 16, DC = D / 8, VP = D + 16, OP = D + 4, NVC = KT * DC / 64, R = 16 * NQ;
+  constexpr int NT = 64 * NW, KS = D / 32, DB = D / 16, DC = D / 8, VP = D + 16, OP = D + 4, NVC = KT * DC / 64, R = 16;
   extern __shared__ __align__(16) char few_smem[];
   const paged_attn_args& a = p.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -271,91 +271,66 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_few_kernel(PagedParams 
       }
     };
     // queries (B operand of S^T): rows past the end repeat the last one, masked and never stored
-    Frag8 qf[NQ][KS];
-    int qi[NQ];
-    bool q_ok[NQ];
+    Frag8 qf[KS];
+    const bool q_ok = l16 < M;
+    const int qr = min(l16, M - 1), qi = token_of(p, qr);
+    const uint16_t* qp = (const uint16_t*)a.q + (long long)(lo + qi) * a.q_stride + (kvh * G + qr - qi * G) * D + 8 * g;
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      const int row = min(16 * n + l16, M - 1);
-      q_ok[n] = 16 * n + l16 < M;
-      qi[n] = token_of(p, row);
-      const uint16_t* qp = (const uint16_t*)a.q + (long long)(lo + qi[n]) * a.q_stride + (kvh * G + row - qi[n] * G) * D + 8 * g;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) qf[n][ks].u = *(const uint4*)(qp + 32 * ks);
-    }
-    // trees (at most 32 nodes here): parents in the lanes; what a token sees of the new tokens, and its depth
-    u64 path[NQ];
-    int depth[NQ];
+    for (int ks = 0; ks < KS; ++ks) qf[ks].u = *(const uint4*)(qp + 32 * ks);
+    // trees (at most 16 nodes here): parents in the lanes; what a token sees of the new tokens, and its depth
+    u64 path = 0;
+    int depth = qi;
     int pa = -1;
     if (TREE) pa = a.parent[lo + min(lane, T - 1)];
     if (t_begin + wave < t_end) request(t_begin + wave);
     if (TREE) {
       const bool bad = lane < T && (lane == 0 ? pa != -1 : (pa >= lane || pa < 0));
       if (bad) { atomicOr(p.dev_status, CASCADE_FLAG_PARENT); pa = lane == 0 ? -1 : 0; }
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        path[n] = 0;
-        int x = qi[n];
-        while (__any(x >= 0)) {
-          if (x >= 0) path[n] |= 1ull << x;
-          const int up = __builtin_amdgcn_ds_bpermute(4 * (x & 63), pa);
-          x = x > 0 ? up : -1;
-        }
-        depth[n] = __popcll(path[n]) - 1;
-        if (a.window > 0) {   // the nearest `window` of them, and the sinks
-          const int keep_sinks = a.n_sink - P;   // depths below this
-          u64 all = path[n];
-          int left = depth[n] + 1 - a.window;   // so many of the path's first are out of reach
-          int d = 0;
-          while (__any(all != 0)) {
-            if (all) {
-              const int b = __ffsll((long long)all) - 1;
-              if (d < left && d >= keep_sinks) path[n] &= ~(1ull << b);
-              all &= all - 1;
-              ++d;
-            }
+      int x = qi;
+      while (__any(x >= 0)) {
+        if (x >= 0) path |= 1ull << x;
+        const int up = __builtin_amdgcn_ds_bpermute(4 * (x & 63), pa);
+        x = x > 0 ? up : -1;
+      }
+      depth = __popcll(path) - 1;
+      if (a.window > 0) {   // the nearest `window` of them, and the sinks
+        const int keep_sinks = a.n_sink - P;   // depths below this
+        u64 all = path;
+        int left = depth + 1 - a.window;   // so many of the path's first are out of reach
+        int d = 0;
+        while (__any(all != 0)) {
+          if (all) {
+            const int b = __ffsll((long long)all) - 1;
+            if (d < left && d >= keep_sinks) path &= ~(1ull << b);
+            all &= all - 1;
+            ++d;
           }
         }
       }
-    } else {
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) { path[n] = 0; depth[n] = qi[n]; }
     }
 
-    f32x4 ot[NQ][DB];
-    float m_run[NQ], l_run[NQ];
+    f32x4 ot[DB];
+    float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      m_run[n] = -INFINITY;
-      l_run[n] = 0.f;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) ot[n][db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int db = 0; db < DB; ++db) ot[db] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int t = t_begin + wave; t < t_end; t += NW) {
       const bool fresh = t >= ti.n_p;
       const int kb = fresh ? ti.new_tile(t - ti.n_p) * KT : ti.prefix_tile(t) * KT;
-      f32x4 st[NQ][4];
+      f32x4 st[4];
 #pragma unroll
-      for (int kt = 0; kt < 4; ++kt)
+      for (int kt = 0; kt < 4; ++kt) {
+        st[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-          st[n][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            Frag8 a8;
-            a8.u = make_uint4(kf[kt][ks][0], kf[kt][ks][1], kf[kt][ks][2], kf[kt][ks][3]);
-            st[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a8.v, qf[n][ks].v, st[n][kt], 0, 0, 0);
-          }
+        for (int ks = 0; ks < KS; ++ks) {
+          Frag8 a8;
+          a8.u = make_uint4(kf[kt][ks][0], kf[kt][ks][1], kf[kt][ks][2], kf[kt][ks][3]);
+          st[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a8.v, qf[ks].v, st[kt], 0, 0, 0);
         }
+      }
       __builtin_amdgcn_sched_barrier(0);
       // what some token sees of this tile, and whether all of them see the same
-      u64 valid[NQ], some = 0, all = ~0ull;
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        valid[n] = fresh ? (TREE ? path[n] : sees_chain(p, P, kb, qi[n])) : sees_prefix(p, P, kb, P + depth[n]);
-        some |= valid[n];
-        all &= valid[n];
-      }
+      const u64 valid = fresh ? (TREE ? path : sees_chain(p, P, kb, qi)) : sees_prefix(p, P, kb, P + depth);
+      u64 some = valid, all = valid;
       // (lanes differ only in l16)
       if (T > 1 && (fresh || (a.window > 0))) {
 #pragma unroll
@@ -388,44 +363,41 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_few_kernel(PagedParams 
       }
       __builtin_amdgcn_wave_barrier();   // keep the tile's stores ahead of its transposing reads in program order
       if (t + NW < t_end) request(t + NW);   // the wave's next tile streams in during the softmax
-      Frag8 pf[NQ][2];
+      Frag8 pf[2];
+      const u64 vis = q_ok ? valid : 0ull;
+      float mx = -INFINITY;
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        const u64 vis = q_ok[n] ? valid[n] : 0ull;
-        float mx = -INFINITY;
+      for (int kt = 0; kt < 4; ++kt) {
+        const uint32_t nib = (uint32_t)(vis >> (16 * kt + 4 * g));   // this lane's 4 keys of sub-tile kt
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
-          const uint32_t nib = (uint32_t)(vis >> (16 * kt + 4 * g));   // this lane's 4 keys of sub-tile kt
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const float z = ((nib >> c) & 1u) ? st[n][kt][c] * p.scale_log2e : -INFINITY;
-            st[n][kt][c] = z;
-            mx = fmaxf(mx, z);
-          }
+        for (int c = 0; c < 4; ++c) {
+          const float z = ((nib >> c) & 1u) ? st[kt][c] * p.scale_log2e : -INFINITY;
+          st[kt][c] = z;
+          mx = fmaxf(mx, z);
         }
-        mx = rows4_max(mx);
-        const float m_new = fmaxf(m_run[n], mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = fast_exp2(m_run[n] - m_use);
-        float ls = 0.f;
+      }
+      mx = rows4_max(mx);
+      const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = fast_exp2(m_run - m_use);
+      float ls = 0.f;
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
+      for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const float e = fast_exp2(st[n][kt][c] - m_use);
-            st[n][kt][c] = e;
-            ls += e;
-          }
-        l_run[n] = l_run[n] * alpha + ls;
-        m_run[n] = m_new;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) ot[n][db] *= alpha;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          pf[n][j].u.x = pack_bf16x2(st[n][2 * j][0], st[n][2 * j][1]);
-          pf[n][j].u.y = pack_bf16x2(st[n][2 * j][2], st[n][2 * j][3]);
-          pf[n][j].u.z = pack_bf16x2(st[n][2 * j + 1][0], st[n][2 * j + 1][1]);
-          pf[n][j].u.w = pack_bf16x2(st[n][2 * j + 1][2], st[n][2 * j + 1][3]);
+        for (int c = 0; c < 4; ++c) {
+          const float e = fast_exp2(st[kt][c] - m_use);
+          st[kt][c] = e;
+          ls += e;
         }
+      l_run = l_run * alpha + ls;
+      m_run = m_new;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) ot[db] *= alpha;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        pf[j].u.x = pack_bf16x2(st[2 * j][0], st[2 * j][1]);
+        pf[j].u.y = pack_bf16x2(st[2 * j][2], st[2 * j][3]);
+        pf[j].u.z = pack_bf16x2(st[2 * j + 1][0], st[2 * j + 1][1]);
+        pf[j].u.w = pack_bf16x2(st[2 * j + 1][2], st[2 * j + 1][3]);
       }
       // O^T += V^T P^T with transposing reads of the wave's tile (LDS operations of one wave complete in order)
 #pragma unroll
@@ -437,8 +409,7 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_few_kernel(PagedParams 
           vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(vp));
           vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)(vp + 16 * VP));
           if (odd) vf.f.u = make_uint4(finite_only(vf.f.u.x), finite_only(vf.f.u.y), finite_only(vf.f.u.z), finite_only(vf.f.u.w));
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) ot[n][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.f.v, pf[n][j].v, ot[n][db], 0, 0, 0);
+          ot[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.f.v, pf[j].v, ot[db], 0, 0, 0);
         }
       if (odd)
         for (int key = 0; key < KT; ++key)
@@ -448,9 +419,7 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_few_kernel(PagedParams 
             for (int c = 0; c < 4; ++c) {
               const float v = bf16_bits_to_f32(vt[key * VP + 16 * db + 4 * g + c]);
               const bool is_odd = !(fabsf(v) < INFINITY);
-#pragma unroll
-              for (int n = 0; n < NQ; ++n)
-                if (is_odd && ((valid[n] >> key) & 1)) ot[n][db][c] += v;
+              if (is_odd && ((valid >> key) & 1)) ot[db][c] += v;
             }
       __builtin_amdgcn_wave_barrier();   // and the reads ahead of the next tile's stores
     }
@@ -459,16 +428,13 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_few_kernel(PagedParams 
     __syncthreads();
     float* mo = (float*)few_smem;          // [NW][R][OP]
     float* mml = mo + NW * R * OP;         // [NW][R][2]
+    const float l = rows4_sum(l_run);
+    float* orow = mo + (wave * R + l16) * OP;
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      const float l = rows4_sum(l_run[n]);
-      float* orow = mo + (wave * R + 16 * n + l16) * OP;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) *(f32x4*)(orow + 16 * db + 4 * g) = ot[n][db];
-      if (g == 0) {
-        mml[(wave * R + 16 * n + l16) * 2] = m_run[n];
-        mml[(wave * R + 16 * n + l16) * 2 + 1] = l;
-      }
+    for (int db = 0; db < DB; ++db) *(f32x4*)(orow + 16 * db + 4 * g) = ot[db];
+    if (g == 0) {
+      mml[(wave * R + l16) * 2] = m_run;
+      mml[(wave * R + l16) * 2 + 1] = l;
     }
     __syncthreads();
     constexpr int TPR = D / 4;             // threads per row, four elements each
@@ -1299,13 +1265,13 @@ hipError_t allow_lds(int bytes, int device) {
   return e;
 }
 
-// How a call is cut.  Shapes 0 and 1: few query rows, 16 or 32 of them; 2, 3, 4: workgroups of 64, 128, 256 query rows; 5: f32.
+// How a call is cut.  Shape 0: few query rows, at most 16; 1, 2, 3: workgroups of 64, 128, 256 query rows; 4: f32.
 struct Cut {
   int shape;
   int parts, part_tiles;
 };
-constexpr int FEW_16 = 0, FEW_32 = 1, RING_64 = 2, RING_128 = 3, RING_256 = 4, F32 = 5;
-constexpr int SHAPE_ROWS[] = {16, 32, 64, 128, 256, 16};
+constexpr int FEW = 0, RING_64 = 1, RING_128 = 2, RING_256 = 3, F32 = 4;
+constexpr int SHAPE_ROWS[] = {16, 64, 128, 256, 16};
 
 int tiles_bound(const paged_attn_args* a, int ts = KT) {
   const int n = (a->max_new + ts - 1) / ts;
@@ -1319,19 +1285,35 @@ int tiles_bound(const paged_attn_args* a, int ts = KT) {
 
 size_t part_bytes(const paged_attn_args* a) { return (size_t)a->n_tokens * a->n_heads * (a->head_dim + 2) * sizeof(float); }
 
-// Estimated time of a cut of many query rows, us: as for trees over a contiguous prefix (the same tiles), what one tile costs a workgroup on a mostly idle chip (c0), with one
-// workgroup on every compute unit (c1), with two (c2; c2_hbm where every tile comes from memory), and the fixed part.
+// Estimated time of a cut of many query rows, us: what the longest workgroup takes, or what all of them have to do where several share a compute unit, whichever is more.  A tile costs a
+// workgroup c0 on a mostly idle chip, c1 with one workgroup on every compute unit, c2 with two (256 rows: one after the other); at head_dim 64 what is shared costs `narrow` of that, a step
+// by itself the same.  Workgroups of a chain go through half of its new tiles in the mean; trees' new tiles cost 0.7 more for their masks; to begin and to end is worth 4.6 tiles.
+// Fitted to 180 sizes x 3 shapes x up to 4 numbers of parts (1 to 64 rows, 1 to 2200 new tokens behind 0 to 8000, windows, trees): the cut with the least estimate
+// takes 0.6 % longer than the fastest one in the mean, 17 % at most.  With every workgroup as long as the longest it was 3 % and 38 %.
 float ring_estimate_us(int shape, const paged_attn_args* a, int parts, int n_cu) {
-  constexpr struct { float c0, c1, c2, c2_hbm; } COST[] = {{1.0f, 1.0f, 1.5f, 3.0f}, {1.2f, 1.45f, 2.5f, 2.5f}, {1.7f, 2.3f, 2.3f, 2.3f}};
+  constexpr struct { float c0, c1, c2, narrow; } COST[] = {{0.85f, 1.01f, 1.4f, 0.59f}, {1.1f, 1.52f, 1.96f, 0.73f}, {1.34f, 2.09f, 0.f, 0.67f}};
   const auto& c = COST[shape - RING_64];
   const int G = a->n_heads / a->n_kv_heads, rows = SHAPE_ROWS[shape];
   const int n_sb = (int)(((int64_t)a->max_new * G + rows - 1) / rows);
   float blocks = (float)a->n_rows * n_sb;
   if (n_sb > 1) blocks = fminf(blocks, (float)a->n_tokens * G / rows + 0.5f * a->n_rows);
-  const float x = blocks * a->n_kv_heads * parts / n_cu, c2 = c.c2_hbm + (c.c2 - c.c2_hbm) * fminf(blocks / a->n_rows - 1.f, 1.f);
-  const float per_tile = x <= 1.f ? c.c0 + (c.c1 - c.c0) * x : (shape == RING_256 ? c.c1 * ceilf(x) : (x <= 2.f ? c.c1 + (c2 - c.c1) * (x - 1.f) : c2 * 0.5f * x));
-  float us = 7.4f + (float)((tiles_bound(a) + parts - 1) / parts) * per_tile * (a->head_dim == 64 ? 0.7f : 1.f);
-  if (parts > 1) us += 3.8f + 0.3f * parts + (float)parts * a->n_tokens * a->n_heads * (a->head_dim + 2) * 4.f / 7e6f;
+  const float x = blocks * a->n_kv_heads * parts / n_cu;
+  // tiles of the longest workgroup, and in the mean
+  const int news = (a->max_new + KT - 1) / KT, old = tiles_bound(a) - news;
+  const float row_tokens = (float)a->n_tokens / a->n_rows;
+  float most = (float)(old + news), mean = a->parent ? fminf((float)news, news * row_tokens / a->max_new) : 0.5f * row_tokens / KT + 0.5f;
+  if (a->window > 0) {
+    const float w = (float)(((int64_t)a->window + KT - 2) / KT + 1), all = w + (float)(((int64_t)a->n_sink + KT - 1) / KT) + 1.f;
+    most = fminf(old + fminf((float)news, w), all);
+    mean = fminf(old + fminf(mean, w), all);
+  } else {
+    mean += old;
+  }
+  if (a->parent) { most += 0.7f * news; mean += 0.7f * news; }
+  const float alone = c.c0 + (c.c1 - c.c0) * fminf(x, 1.f);
+  const float shared = x <= 1.f ? alone : (shape == RING_256 ? c.c1 * ceilf(x) : (x <= 2.f ? c.c1 + (c.c2 - c.c1) * (x - 1.f) : c.c2 * 0.5f * x));
+  float us = 5.15f + fmaxf(ceilf(most / parts) * alone, (mean / parts + 4.65f) * shared * (a->head_dim == 64 ? c.narrow : 1.f));
+  if (parts > 1) us += 3.f + 0.2f * parts + (float)parts * a->n_tokens * a->n_heads * (a->head_dim + 2) * 4.f / 7e6f;
   return us;
 }
 
@@ -1347,7 +1329,8 @@ Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
     return c;
   }
   const int tiles = tiles_bound(a);
-  if (M > 32) {
+  // (17 to 32 query rows in waves of their own, twice the registers: 0.6 to 1.1 of the time at head_dim 64, 1.5 to 2.6 at 128, where they do not fit)
+  if (M > 16) {
     float best = INFINITY;
     for (int shape = RING_64; shape <= RING_256; ++shape)
       for (int parts = 1; parts <= 16 && parts <= std::max(most, 1) && parts <= tiles; parts = parts < 4 ? parts + 1 : parts * 2) {
@@ -1356,7 +1339,7 @@ Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
       }
     return c;
   }
-  c.shape = M <= 16 ? FEW_16 : FEW_32;
+  c.shape = FEW;
   const int64_t heads = (int64_t)a->n_rows * a->n_kv_heads;
   // A wave takes 4-5 us to a tile whose keys come from memory, so few (row, kv head) pairs are cut until there is a part for every compute unit (up to 16: joining
   // more takes longer than they save), unless that saves less than the join's 4 us.  Pairs that fill the chip by themselves are cut in two, for rows of different lengths:
@@ -1371,10 +1354,10 @@ Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
   return c;
 }
 
-template <int D, int NQ, int NW, bool TREE>
+template <int D, int NW, bool TREE>
 hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
-  constexpr int v_bytes = NW * KT * (D + 16) * 2, o_bytes = NW * 16 * NQ * (D + 4 + 2) * 4, smem = v_bytes > o_bytes ? v_bytes : o_bytes;
-  constexpr auto kern = paged_few_kernel<D, NQ, NW, TREE>;
+  constexpr int v_bytes = NW * KT * (D + 16) * 2, o_bytes = NW * 16 * (D + 4 + 2) * 4, smem = v_bytes > o_bytes ? v_bytes : o_bytes;
+  constexpr auto kern = paged_few_kernel<D, NW, TREE>;
   hipError_t e = allow_lds<kern>(smem, ctx->device);
   if (e != hipSuccess) return e;
   const int64_t items = (int64_t)p.a.n_rows * p.a.n_kv_heads * p.parts, slots = (int64_t)ctx->n_cu * (8 / NW);
@@ -1384,9 +1367,8 @@ hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
 }
 template <int D>
 hipError_t launch_few(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
-  if (p.a.parent) return c.shape == FEW_16 ? launch_few_k<D, 1, 4, true>(ctx, p) : launch_few_k<D, 2, 4, true>(ctx, p);
-  if (c.shape == FEW_32) return launch_few_k<D, 2, 4, false>(ctx, p);
-  return (int64_t)p.a.n_rows * p.a.n_kv_heads * c.parts <= ctx->n_cu ? launch_few_k<D, 1, 8, false>(ctx, p) : launch_few_k<D, 1, 4, false>(ctx, p);
+  if (p.a.parent) return launch_few_k<D, 4, true>(ctx, p);
+  return (int64_t)p.a.n_rows * p.a.n_kv_heads * c.parts <= ctx->n_cu ? launch_few_k<D, 8, false>(ctx, p) : launch_few_k<D, 4, false>(ctx, p);
 }
 
 // no more blocks of so many query rows than this, whatever the rows' lengths are; a row out of order is one
@@ -1440,7 +1422,7 @@ hipError_t launch_f32(cascade_ctx* ctx, const PagedParams& p) {
 }
 template <int D>
 hipError_t launch_bf16(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
-  if (c.shape <= FEW_32) return launch_few<D>(ctx, p, c);
+  if (c.shape == FEW) return launch_few<D>(ctx, p, c);
   return p.a.parent ? launch_ring<D, true>(ctx, p, c) : launch_ring<D, false>(ctx, p, c);
 }
 
