@@ -42,6 +42,7 @@ struct PagedParams {
   unsigned page16_inv;   // floor(2^32 / page16) + 1: group / page16 as a high product (groups stay below 2^26, page16 <= 64); 0 for page16 1
   int parts;             // that the keys of a row are cut into at most; 1: results are written at once
   int part_tiles;        // tiles of a part (few rows)
+  bool in_order;         // (other kernels) rows of the batch are taken in order, not longest first
   float* ws_o;           // [parts][n_tokens * n_heads][head_dim]
   float* ws_ml;          // [parts][n_tokens * n_heads][2]
 };
@@ -484,8 +485,8 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_few_kernel(PagedParams 
 // many as fit, and reads the one for the next tile a tile ahead.
 //
 // Bound by the matrix cores and the vector ALU taking turns: products keep the former busy 41 % of the cycles (clock 2.0 GHz under this load), the table costs nothing that can be
-// measured.  Eight rows of 500-1000 new tokens behind 0-2000, 8 kv heads of 4 (157 GFLOP): 190 us = 830 TFLOP/s in 128-row workgroups (64 rows: 259, 256 rows: 221); 256-node trees of
-// 8 rows x 32 heads behind 4200 keys (141 GFLOP): 181-184 us, 183 where the prefixes are contiguous; 1800-2000 new tokens under a window of 1024, head_dim 64: 42.5.
+// measured.  Eight rows of 500-1000 new tokens behind 0-2000, 8 kv heads of 4 (157 GFLOP): 189 us = 830 TFLOP/s in 128-row workgroups (64 rows: 259, 256 rows: 221); 256-node trees of
+// 8 rows x 32 heads behind 4200 keys (141 GFLOP): 181-184 us, 183 where the prefixes are contiguous; 1800-2000 new tokens under a window of 1024, head_dim 64: 41.5.
 // Sums of the probabilities as they are, before they are rounded, cost less than products with ones (196 -> 184 us for the trees: registers) and give an exact lse.
 template <int D>
 struct RingGeom {
@@ -522,7 +523,9 @@ __device__ __forceinline__ float rows4_max_raw(float v) {
   return vmax2(__uint_as_float(b.x), __uint_as_float(b.y));
 }
 
-// Block `blk` of the launch: a run of query rows of a row of the batch.  Rows are taken longest first (up to 64 of them), a row's blocks from its end, where a chain sees most.
+// Block `blk` of the launch: a run of query rows of a row of the batch, a row's blocks from its end, where a chain sees most.  Where there are more blocks than compute units,
+// rows are taken longest first (up to 64 of them).  64 rows of 25 tokens behind 74 keys: 10.3 us ranked row by row, 7.4 in order; of 60 behind 1000, many blocks: 56.1 us, ranked eight
+// at a time 54.9.
 __device__ __forceinline__ RowInfo block_row(const PagedParams& p, int blk, int rows_per_block, int lane, int* sb) {
   const paged_attn_args& a = p.a;
   RowInfo none = {-1, 0, 0, 0, 0};
@@ -535,13 +538,13 @@ __device__ __forceinline__ RowInfo block_row(const PagedParams& p, int blk, int 
       nb = mine.flag ? 1 : (mine.T * p.group + rows_per_block - 1) / rows_per_block;
     }
     int from = lane;   // the lane whose row stands at this lane's place
-    if (a.n_rows > 1 && a.n_rows <= 64) {
-      const int work = at < a.n_rows ? (mine.flag ? 0 : mine.P + mine.T) : -1;
+    if (!p.in_order) {
+      // lengths in steps of 32, and the lane, so that none are equal; lanes without a row stand behind
+      const unsigned work = at < a.n_rows ? (mine.flag ? 0u : (unsigned)(mine.P + mine.T) >> 5 << 6) + 127u - lane : 63u - lane;
       int rank = 0;
-      for (int r = 0; r < a.n_rows; ++r) {
-        const int w = __builtin_amdgcn_readlane(work, r);
-        rank += (w > work || (w == work && r < lane)) ? 1 : 0;
-      }
+      for (int r0 = 0; r0 < a.n_rows; r0 += 8)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) rank += (unsigned)__builtin_amdgcn_readlane((int)work, r0 + r) > work ? 1 : 0;
       if (lane >= a.n_rows) rank = lane;
       from = __builtin_amdgcn_ds_permute(4 * rank, lane);
       nb = __builtin_amdgcn_ds_bpermute(4 * from, nb);
@@ -1378,7 +1381,7 @@ int64_t most_blocks(const PagedParams& p, int rows) {
 }
 
 template <int D, int NS, int NQ, int NW, bool TREE>
-hipError_t launch_ring_k(cascade_ctx* ctx, const PagedParams& p) {
+hipError_t launch_ring_k(cascade_ctx* ctx, PagedParams& p) {
   constexpr int smem = ring_lds<D, NS, NQ, NW, TREE>();
   constexpr auto kern = paged_ring_kernel<D, NS, NQ, NW, TREE>;
   hipError_t e = allow_lds<kern>(smem, ctx->device);
@@ -1387,28 +1390,31 @@ hipError_t launch_ring_k(cascade_ctx* ctx, const PagedParams& p) {
   const int64_t blocks = most_blocks(p, 16 * NQ * NW);
   // (8 / n_kv_heads XCDs share a kv head: every one gets as many)
   const int64_t share = 8 % a.n_kv_heads == 0 ? 8 / a.n_kv_heads : 1;
+  p.in_order = a.n_rows == 1 || a.n_rows > 64 || blocks * a.n_kv_heads <= ctx->n_cu;
   KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
   CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)((blocks + share - 1) / share * share * a.n_kv_heads)), dim3(64 * NW), smem, ctx->stream, p);
   return hipGetLastError();
 }
 template <int D, bool TREE>
-hipError_t launch_ring(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
+hipError_t launch_ring(cascade_ctx* ctx, PagedParams& p, const Cut& c) {
   if (c.shape == RING_64) return launch_ring_k<D, 2, 1, 4, TREE>(ctx, p);
   if (c.shape == RING_128) return launch_ring_k<D, 2, 2, 4, TREE>(ctx, p);
   return launch_ring_k<D, 3, 2, 8, TREE>(ctx, p);
 }
 template <int DB, int NW, bool VEC, bool TREE>
-hipError_t launch_f32_k(cascade_ctx* ctx, const PagedParams& p) {
+hipError_t launch_f32_k(cascade_ctx* ctx, PagedParams& p) {
   constexpr int smem = (NW * 16 * (16 * DB + 4) + NW * 32) * 4;
   constexpr auto kern = paged_f32_kernel<DB, NW, VEC, TREE>;
   hipError_t e = allow_lds<kern>(smem, ctx->device);
   if (e != hipSuccess) return e;
+  const int64_t blocks = most_blocks(p, 16) * p.a.n_kv_heads;
+  p.in_order = p.a.n_rows == 1 || p.a.n_rows > 64 || blocks <= ctx->n_cu;
   KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
-  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)(most_blocks(p, 16) * p.a.n_kv_heads)), dim3(64 * NW), smem, ctx->stream, p);
+  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)blocks), dim3(64 * NW), smem, ctx->stream, p);
   return hipGetLastError();
 }
 template <int DB, int NW>
-hipError_t launch_f32_t(cascade_ctx* ctx, const PagedParams& p) {
+hipError_t launch_f32_t(cascade_ctx* ctx, PagedParams& p) {
   const paged_attn_args& a = p.a;
   // keys, values and queries 16 bytes at a time where everything lies on such boundaries, otherwise element by element
   const bool vec = ((a.head_dim | a.q_stride | a.kv_stride | a.stride_page | a.stride_head | a.stride_pos) % 4) == 0 &&
@@ -1416,12 +1422,12 @@ hipError_t launch_f32_t(cascade_ctx* ctx, const PagedParams& p) {
   if (a.parent) return vec ? launch_f32_k<DB, NW, true, true>(ctx, p) : launch_f32_k<DB, NW, false, true>(ctx, p);
   return vec ? launch_f32_k<DB, NW, true, false>(ctx, p) : launch_f32_k<DB, NW, false, false>(ctx, p);
 }
-hipError_t launch_f32(cascade_ctx* ctx, const PagedParams& p) {
+hipError_t launch_f32(cascade_ctx* ctx, PagedParams& p) {
   if (p.a.head_dim <= 64) return launch_f32_t<4, 16>(ctx, p);
   return p.a.head_dim <= 128 ? launch_f32_t<8, 8>(ctx, p) : launch_f32_t<16, 4>(ctx, p);
 }
 template <int D>
-hipError_t launch_bf16(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
+hipError_t launch_bf16(cascade_ctx* ctx, PagedParams& p, const Cut& c) {
   if (c.shape == FEW) return launch_few<D>(ctx, p, c);
   return p.a.parent ? launch_ring<D, true>(ctx, p, c) : launch_ring<D, false>(ctx, p, c);
 }
