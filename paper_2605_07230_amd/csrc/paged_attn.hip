@@ -175,8 +175,11 @@ __device__ __forceinline__ void write_nothing(const PagedParams& p, const RowInf
 // none is left: rows of very different lengths share the chip, and no workgroup is launched for nothing.
 // One token of 64 rows x 4200 keys, 8 kv heads of 4, head_dim 128 (1.1 GB): 199 us = 5.5 TB/s; of 90 to 4200 keys (602 MB) 131 us and the join's 4; two rows x 312 keys, 32 kv heads: 11 us, of
 // which the chain row -> table -> tile -> join of the waves is all.  Sixty-four rows dealt longest first, every second round backwards: no faster (131 -> 146).
+// Waves per SIMD: two, at head_dim 64, whose tiles are half as large, three of four-wave workgroups (64 rows of 90 to 4200 keys 70 -> 67 us, of 300 to 600 with 16 heads 28.3 -> 26.9).
+template <int D, int NW>
+constexpr int few_per_unit() { return D == 64 && NW == 4 ? 3 : 8 / NW; }
 template <int D, int NW, bool TREE>
-__global__ __launch_bounds__(64 * NW, 8 / NW) void paged_few_kernel(PagedParams p) {
+__global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_kernel(PagedParams p) {
   constexpr int NT = 64 * NW, KS = D / 32, DB = D / 16, DC = D / 8, VP = D + 16, OP = D + 4, NVC = KT * DC / 64, R = 16;
   extern __shared__ __align__(16) char few_smem[];
   const paged_attn_args& a = p.a;
@@ -238,42 +241,43 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_few_kernel(PagedParams 
     // anywhere; inside one, 32-bit offsets do.  Keys past the end are the last one again.
     u32x4 kf[4][KS], vr[NVC];
     const char *kn = (const char*)((const uint16_t*)a.k_new + lo * a.kv_stride + kvh * D), *vn = (const char*)((const uint16_t*)a.v_new + lo * a.kv_stride + kvh * D);
+    constexpr int GV = NVC / 4, KEYS = 64 / DC;   // value pieces of a lane in a group, keys between two of them
     auto request = [&](int t) {
       const bool fresh = t >= ti.n_p;
-      const int g0 = 4 * (fresh ? ti.new_tile(t - ti.n_p) : ti.prefix_tile(t)), end = (fresh ? T : P) - 1;
+      const int end = (fresh ? T : P) - 1;
       const unsigned pitch = 2u * (unsigned)(fresh ? a.kv_stride : a.stride_pos);
-      const char *kb = fresh ? kn : (const char*)a.k_pages, *vb = fresh ? vn : (const char*)a.v_pages;
-      long long off[4];
-      int last[4];
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        int gq;
-        if (fresh) {
-          gq = min(g0 + kt, end >> 4);
-          off[kt] = (long long)(16 * gq) * pitch;
-        } else {
-          gq = needed_group(p, ti, P, g0 + kt);
-          const int e = page_index(p, gq);
-          off[kt] = 2 * group_offset(p, checked_page(p, table_entry(p, r.s, e)), e, gq, kvh);
+      // the places of the four groups, by a lane each
+      long long off;
+      int gq = 4 * (fresh ? ti.new_tile(t - ti.n_p) : ti.prefix_tile(t)) + (lane & 3);
+      if (fresh) {
+        gq = min(gq, end >> 4);
+        off = (long long)(16 * gq) * pitch;
+      } else {
+        gq = needed_group(p, ti, P, gq);
+        const int e = page_index(p, gq);
+        int page = a.block_table[r.s * a.table_stride + e];
+        if ((unsigned)page >= (unsigned)a.n_pages) {   // as checked_page
+          atomicOr(p.dev_status, CASCADE_FLAG_PAGE);
+          page = 0;
         }
-        last[kt] = end - 16 * gq;
+        off = 2 * group_offset(p, page, e, gq, kvh);
       }
+      const int behind = end - 16 * gq;
+      const char *kb = fresh ? kn : (const char*)a.k_pages, *vb = fresh ? vn : (const char*)a.v_pages;
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt) {
-        const char* kp = kb + off[kt];
-        const unsigned at = (unsigned)min(l16, last[kt]) * pitch + 16u * g;
+        const long long o = (long long)(((u64)(unsigned)__builtin_amdgcn_readlane((int)(off >> 32), kt) << 32) | (unsigned)__builtin_amdgcn_readlane((int)off, kt));
+        const int last = __builtin_amdgcn_readlane(behind, kt);
+        const char *kp = kb + o, *vp = vb + o;
+        const unsigned at = (unsigned)min(l16, last) * pitch + 16u * g;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kf[kt][ks] = *(const u32x4*)(kp + (at + 64u * ks));
-      }
+        for (int ks = 0; ks < KS; ++ks) kf[kt][ks] = *(const u32x4*)(kp + 64 * ks + at);
 #pragma unroll
-      for (int it = 0; it < NVC; ++it) {
-        const int c = lane + 64 * it, kt = it / (NVC / 4);
-        vr[it] = *(const u32x4*)(vb + off[kt] + ((unsigned)min((c / DC) & 15, last[kt]) * pitch + 16u * (unsigned)(c % DC)));
+        for (int j = 0; j < GV; ++j) vr[GV * kt + j] = *(const u32x4*)(vp + ((unsigned)min(lane / DC + KEYS * j, last) * pitch + 16u * (unsigned)(lane % DC)));
       }
     };
-    // queries (B operand of S^T): rows past the end repeat the last one, masked and never stored
+    // queries (B operand of S^T): rows past the end repeat the last one, never stored
     Frag8 qf[KS];
-    const bool q_ok = l16 < M;
     const int qr = min(l16, M - 1), qi = token_of(p, qr);
     const uint16_t* qp = (const uint16_t*)a.q + (long long)(lo + qi) * a.q_stride + (kvh * G + qr - qi * G) * D + 8 * g;
 #pragma unroll
@@ -365,19 +369,23 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_few_kernel(PagedParams 
       __builtin_amdgcn_wave_barrier();   // keep the tile's stores ahead of its transposing reads in program order
       if (t + NW < t_end) request(t + NW);   // the wave's next tile streams in during the softmax
       Frag8 pf[2];
-      const u64 vis = q_ok ? valid : 0ull;
-      float mx = -INFINITY;
+      if (__any(valid != ~0ull)) {
 #pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        const uint32_t nib = (uint32_t)(vis >> (16 * kt + 4 * g));   // this lane's 4 keys of sub-tile kt
+        for (int kt = 0; kt < 4; ++kt) {
+          const uint32_t nib = (uint32_t)(valid >> (16 * kt + 4 * g));   // this lane's 4 keys of sub-tile kt
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const float z = ((nib >> c) & 1u) ? st[kt][c] * p.scale_log2e : -INFINITY;
-          st[kt][c] = z;
-          mx = fmaxf(mx, z);
+          for (int c = 0; c < 4; ++c) {
+            const uint32_t seen = (uint32_t)__builtin_amdgcn_sbfe((int)nib, c, 1);
+            st[kt][c] = __uint_as_float((seen & __float_as_uint(st[kt][c])) | (~seen & 0xff800000u));
+          }
         }
       }
-      mx = rows4_max(mx);
+      float mx = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) mx = fmaxf(mx, st[kt][c]);
+      mx = rows4_max(mx) * p.scale_log2e;
       const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
       const float alpha = fast_exp2(m_run - m_use);
       float ls = 0.f;
@@ -385,7 +393,7 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void paged_few_kernel(PagedParams 
       for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const float e = fast_exp2(st[kt][c] - m_use);
+          const float e = fast_exp2(fmaf(st[kt][c], p.scale_log2e, -m_use));
           st[kt][c] = e;
           ls += e;
         }
@@ -1363,7 +1371,7 @@ hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
   constexpr auto kern = paged_few_kernel<D, NW, TREE>;
   hipError_t e = allow_lds<kern>(smem, ctx->device);
   if (e != hipSuccess) return e;
-  const int64_t items = (int64_t)p.a.n_rows * p.a.n_kv_heads * p.parts, slots = (int64_t)ctx->n_cu * (8 / NW);
+  const int64_t items = (int64_t)p.a.n_rows * p.a.n_kv_heads * p.parts, slots = (int64_t)ctx->n_cu * few_per_unit<D, NW>();
   KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
   CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)std::min(items, slots)), dim3(64 * NW), smem, ctx->stream, p);
   return hipGetLastError();
