@@ -278,8 +278,12 @@ __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_ke
     };
     // queries (B operand of S^T): rows past the end repeat the last one, never stored
     Frag8 qf[KS];
+    // Opaque at head_dim 128, where registers run out: what follows from it is worked out here, not kept over the parts.  Without scratch memory 64 rows of 90 to 4200 keys
+    // take 130 -> 120 us, of 300 to 600 with 16 heads 56.6 -> 49.3; at head_dim 64 it only costs the small calls 0.5.
+    int asker = g;
+    if (D == 128) asm volatile("" : "+v"(asker));
     const int qr = min(l16, M - 1), qi = token_of(p, qr);
-    const uint16_t* qp = (const uint16_t*)a.q + (long long)(lo + qi) * a.q_stride + (kvh * G + qr - qi * G) * D + 8 * g;
+    const uint16_t* qp = (const uint16_t*)a.q + (long long)(lo + qi) * a.q_stride + (kvh * G + qr - qi * G) * D + 8 * asker;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks].u = *(const uint4*)(qp + 32 * ks);
     // trees (at most 16 nodes here): parents in the lanes; what a token sees of the new tokens, and its depth
@@ -437,18 +441,20 @@ __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_ke
     __syncthreads();
     float* mo = (float*)few_smem;          // [NW][R][OP]
     float* mml = mo + NW * R * OP;         // [NW][R][2]
+    int joiner = tid;
+    if (D == 128) asm volatile("" : "+v"(joiner));   // (as `asker`)
     const float l = rows4_sum(l_run);
-    float* orow = mo + (wave * R + l16) * OP;
+    float* orow = mo + (wave * R + (joiner & 15)) * OP + (joiner >> 4 & 3) * 4;
 #pragma unroll
-    for (int db = 0; db < DB; ++db) *(f32x4*)(orow + 16 * db + 4 * g) = ot[db];
-    if (g == 0) {
-      mml[(wave * R + l16) * 2] = m_run;
-      mml[(wave * R + l16) * 2 + 1] = l;
+    for (int db = 0; db < DB; ++db) *(f32x4*)(orow + 16 * db) = ot[db];
+    if ((joiner & 48) == 0) {
+      mml[(wave * R + joiner % 16) * 2] = m_run;
+      mml[(wave * R + joiner % 16) * 2 + 1] = l;
     }
     __syncthreads();
     constexpr int TPR = D / 4;             // threads per row, four elements each
-    for (int row = tid / TPR; row < M; row += NT / TPR) {
-      const int d = 4 * (tid % TPR);
+    for (int row = joiner / TPR; row < M; row += NT / TPR) {
+      const int d = 4 * (joiner % TPR);
       float m = -INFINITY, l = 0.f;
 #pragma unroll
       for (int w = 0; w < NW; ++w) m = fmaxf(m, mml[(w * R + row) * 2]);
