@@ -173,8 +173,9 @@ __device__ __forceinline__ void write_nothing(const PagedParams& p, const RowInf
 // - and needs no barrier until their end, where the waves' maxima, sums and outputs meet in LDS.  Keys are loaded in operand order (16 bytes of
 // a key per lane), values through a region of LDS of the wave's own.  A workgroup works through parts (row, kv head, run of part_tiles tiles) until
 // none is left: rows of very different lengths share the chip, and no workgroup is launched for nothing.
-// One token of 64 rows x 4200 keys, 8 kv heads of 4, head_dim 128 (1.1 GB): 199 us = 5.5 TB/s; of 90 to 4200 keys (602 MB) 131 us and the join's 4; two rows x 312 keys, 32 kv heads: 11 us, of
-// which the chain row -> table -> tile -> join of the waves is all.  Sixty-four rows dealt longest first, every second round backwards: no faster (131 -> 146).
+// One token of 64 rows x 4200 keys, 8 kv heads of 4, head_dim 128 (1.1 GB): 193 us = 5.7 TB/s; of 90 to 4200 keys (602 MB) 120 us and the join's 4; two rows x 312 keys, 32 kv heads: 9.5 us, of
+// which the chain row -> table -> tile -> join of the waves is all, and the way of its instructions from memory: lookups of a lane per group of keys on scalar bases and masks only where
+// something is masked (3600 -> 3000 instructions) took 1 us off every small call.  Sixty-four rows dealt longest first, every second round backwards: no faster (131 -> 146 then).
 // Waves per SIMD: two, at head_dim 64, whose tiles are half as large, three of four-wave workgroups (64 rows of 90 to 4200 keys 70 -> 67 us, of 300 to 600 with 16 heads 28.3 -> 26.9).
 template <int D, int NW>
 constexpr int few_per_unit() { return D == 64 && NW == 4 ? 3 : 8 / NW; }
