@@ -1,7 +1,7 @@
-"""CPU checker for the calls around the verification step: a cache in pages and the draw of tokens.  TEST INFRASTRUCTURE ONLY.
+"""CPU oracle for the calls around the verification step: a cache in pages and the draw of tokens.  TEST INFRASTRUCTURE ONLY.
 
 Plain numpy in float64, loops where a definition has them, no code shared with the GPU library.  Pins
-(tests/test_oracle_serving.py): attention over pages equals the tree checker on the gathered cache and a library's causal attention,
+(tests/test_oracle_serving.py): attention over pages equals the tree oracle on the gathered cache and a library's causal attention,
 a chain given as a tree equals a chain, a window of everything equals none; slots against a dictionary of positions; draws
 against a library's sampling filters written another way, and the frequencies of many uniforms.
 """

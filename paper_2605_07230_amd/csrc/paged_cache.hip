@@ -60,7 +60,7 @@ __global__ __launch_bounds__(SLOT_THREADS) void paged_slots_kernel(SlotParams p)
     free_n = f < 0 ? 0u : min((unsigned)f, (unsigned)a.free_capacity);
     if (s == 0 && part == 0 && tid == 0 && (unsigned)f != free_n) atomicOr(p.dev_status, CASCADE_FLAG_PAGE);
   }
-  unsigned tokens = 0, pages = 0;   // of the rows before this round's
+  unsigned tokens = 0, pages = 0;   // of the rows before these
   for (int r0 = 0; r0 < a.n_rows; r0 += SLOT_THREADS) {
     const int r = r0 + tid;
     int len = 0, n = 0, flag = 0;

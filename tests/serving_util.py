@@ -1,4 +1,4 @@
-"""Random problems for the calls on pages, and their comparison with the checker."""
+"""Random problems for the calls on pages, and their comparison with the oracle."""
 import numpy as np
 import torch
 
@@ -93,7 +93,7 @@ class Problem:
         return out
 
     def check(self, heads=None):
-        """Every token of every row against the checker.  A probability is rounded to the type (at most half a step, relative) where it enters
+        """Every token of every row against the oracle.  A probability is rounded to the type (at most half a step, relative) where it enters
         the product, and a result when it is written.  A score's error d (float32
         products of head_dim terms) moves each probability by d.  What float32 sums add is counted as (keys + 64) 2^-24."""
         out, lse = self.out.double().cpu().numpy(), self.lse.double().cpu().numpy()

@@ -1,4 +1,4 @@
-"""paged_attn against the checker: lengths, page sizes, orders of memory, windows, trees, both types."""
+"""paged_attn against the oracle: lengths, page sizes, orders of memory, windows, trees, both types."""
 import ctypes as C
 
 import numpy as np
@@ -62,7 +62,7 @@ F32 = {
 
 
 @pytest.mark.parametrize("name", [*CASES, *F32])
-def test_against_the_checker(name):
+def test_against_the_oracle(name):
     kw = dict(CASES.get(name) or dict(F32[name], dtype="f32"))
     print(f"[paged_attn] {name}: {kw}", flush=True)
     p = Problem(list([*CASES, *F32]).index(name), kw.pop("prefix"), kw.pop("new"), **kw)

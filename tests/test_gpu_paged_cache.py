@@ -1,4 +1,4 @@
-"""paged_slots and paged_append against the checker, and a commit to pages against kv_commit's."""
+"""paged_slots and paged_append against the oracle, and a commit to pages against kv_commit's."""
 import ctypes as C
 
 import numpy as np

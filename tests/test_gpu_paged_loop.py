@@ -32,7 +32,7 @@ def test_steps_over_pages_equal_steps_over_a_contiguous_cache(dtype, cfg):
                           head_dim=inp.head_dim, hidden=inp.hidden, vocab=inp.vocab)
 
     loop = decode.PagedLoop(inp, page_size=16, max_len=cap, max_chunk=400, n_pages=S * 40 + 3)
-    # the prompts arrive in two chunks; their attention is checked against the checker
+    # the prompts arrive in two chunks; their attention is checked against the oracle
     done = np.zeros(S, np.int64)
     for part in range(2):
         new = [int(p) // 2 if part == 0 else int(p) - int(p) // 2 for p in inp.prefix_len]

@@ -1,4 +1,4 @@
-"""sample_tokens against the checker.  Tokens have to be equal: weights are doubles with relative errors below 1e-12, so one uniform in about 1e12 / (entries)
+"""sample_tokens against the oracle.  Tokens have to be equal: weights are doubles with relative errors below 1e-12, so one uniform in about 1e12 / (entries)
 meets a border of the running mass that near (rows of equal weights apart, whose sums are whole numbers on both sides).  A probability is rounded once to
 float32."""
 import ctypes as C

@@ -1,4 +1,4 @@
-"""Pins of the checker for pages and draws (oracle/serving_oracle.py)."""
+"""Pins of the oracle for pages and draws (oracle/serving_oracle.py)."""
 import numpy as np
 import pytest
 import torch
@@ -16,7 +16,7 @@ def test_attention_of_a_chain_equals_a_librarys_causal_attention():
     assert np.all(mag >= np.abs(out) - 1e-12)
 
 
-def test_attention_of_a_tree_equals_the_tree_checker():
+def test_attention_of_a_tree_equals_the_tree_oracle():
     rng = np.random.default_rng(1)
     parent, P = np.array([-1, 0, 0, 1, 3, 2]), 7
     q, kt, vt = (rng.standard_normal((6, 1, 8)) for _ in range(3))
