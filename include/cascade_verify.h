@@ -495,7 +495,8 @@ int paged_append(cascade_ctx* ctx, const paged_append_args* args);
  *     q        element (t, g, d) at t*q_stride + g*head_dim + d;  k_new, v_new at t*kv_stride + kvh*head_dim + d
  *     out      [n_tokens, n_heads, head_dim] contiguous, dtype;  lse [n_tokens, n_heads] float32, may be NULL
  * Accumulation and softmax are float32.  Keys and values that a token does not attend, infinities and NaN among them, do not reach
- * its output.  Tokens behind q_off[n_rows] are not written.  A row whose q_off is not in order or in n_tokens, that has more than
+ * its output; infinite values that it attends make its output that infinity, unless their probability is 0 in float32 (then it may be NaN).
+ * Tokens behind q_off[n_rows] are not written.  A row whose q_off is not in order or in n_tokens, that has more than
  * max_new tokens, or whose prefix is negative or longer than max_prefix_len or its table, gets zeros and lse = -inf and sets the flag; an
  * entry of the table outside the pool sets it too, and what the tokens that need it get is then not defined (the pool's first page is read).
  * bf16: head_dim 64 or 128; strides multiples of 8 elements, stride_pos and kv_stride at most 2^25, buffers on 16-byte boundaries,

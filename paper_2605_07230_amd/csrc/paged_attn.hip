@@ -11,8 +11,8 @@
 // O^T = V^T P^T, whose A operand the transposing LDS read (ds_read_b64_tr_b16) takes from row-major values.
 //
 // A masked key has probability 0, but 0 x inf and 0 x NaN are NaN.  Places that no token of the workgroup sees are never taken from memory, or are
-// zeroed on the way; a tile that some tokens see and others do not is looked through for such values, and if it holds any they are taken out of the product
-// and added to the tokens that see them.
+// zeroed on the way; a tile that some tokens see and others do not, or whose places behind the last key hold that key again, is looked through for such values, and if
+// it holds any they are taken out of the product and added to the tokens that see them, once what was summed before has its scale (the first scale is 0).
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -349,8 +349,13 @@ __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_ke
           all &= ((u64)(unsigned)__shfl_xor((int)(all >> 32), s) << 32) | (unsigned)__shfl_xor((int)all, s);
         }
       }
-      bool odd = false;   // wave-uniform: values that must not meet a masked probability
-      // (a single token without a window sees every key that exists, and those past the end are the last one of them)
+      // Wave-uniform: values that must not meet a masked probability.  Keys past the end are copies of the last one, which the last pieces of such a tile hold.
+      // (without a branch: one that leaves the values alone on one side sends up to 81 registers to scratch)
+      uint32_t last_odd = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) last_odd |= odd_exponent(vr[NVC - 1][e]);
+      bool odd = __any(valid != ~0ull && (last_odd & 0x80008000u) != 0);
+      // (a single token without a window sees every key that exists: nothing to take out)
       if ((T > 1 || a.window > 0) && __any(some != ~0ull || all != ~0ull)) {
         uint32_t seen_odd = 0;
 #pragma unroll
@@ -862,49 +867,23 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
     const int far = fresh ? i1 : P + i1;             // no query's position is behind this one
     const bool cut = a.window > 0 && kb < far - a.window + 1 && kb + KT > a.n_sink - (fresh ? P : 0);
     const bool mixed = (fresh && (TREE || kb + KT - 1 > i0)) || cut;   // some queries see less of it than others
-    if (mixed || (!fresh && kb + KT > P)) {
-      u64 valid[NQ];
+    const bool partial = mixed || (!fresh && kb + KT > P);             // or it ends, and its last key is there again
+    auto sees = [&](int n) -> u64 {
+      if (qi[n] < 0) return 0ull;
+      if (fresh) return TREE ? s_anc[(t & 1) * RW + 16 * (wave + NW * n) + l16] : sees_chain(p, P, kb, qi[n]);
+      return sees_prefix(p, P, kb, P + q_depth[n]);
+    };
+    if (partial) {
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
-        if (fresh) valid[n] = TREE ? s_anc[(t & 1) * RW + 16 * (wave + NW * n) + l16] : sees_chain(p, P, kb, qi[n]);
-        else valid[n] = sees_prefix(p, P, kb, P + q_depth[n]);
-        if (qi[n] < 0) valid[n] = 0;
+        const u64 valid = sees(n);
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
-          const uint32_t nib = (uint32_t)(valid[n] >> (16 * kt + 4 * g));   // this lane's 4 keys of sub-tile kt
+          const uint32_t nib = (uint32_t)(valid >> (16 * kt + 4 * g));   // this lane's 4 keys of sub-tile kt
 #pragma unroll
           for (int c = 0; c < 4; ++c) st[n][kt][c] = ((nib >> c) & 1u) ? st[n][kt][c] : -INFINITY;
         }
         lmax[n] = lane_max(n);
-      }
-      if (mixed) {
-        // infinities and NaN among values that not every query sees (every wave looks through the whole tile, so all agree)
-        uint32_t odd = 0;
-        char* const vt = smem_raw + NS * GM::TILE + ST * GM::TILE;
-#pragma unroll
-        for (int c = 0; c < GM::CPT; ++c) {
-          const uint4 x = *(const uint4*)(vt + 1024 * c + 16 * lane);
-          odd |= odd_exponent(x.x) | odd_exponent(x.y) | odd_exponent(x.z) | odd_exponent(x.w);
-        }
-        if (__any((odd & 0x80008000u) != 0)) {   // they go to the queries that see them, and out of the tile
-          for (int key = 0; key < KT; ++key)
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const float v = bf16_bits_to_f32(*(const uint16_t*)(vt + key * GM::RB + 16 * ((2 * db + (g >> 1)) ^ GM::vswz(key)) + 8 * (g & 1) + 2 * c));
-                const bool is_odd = !(fabsf(v) < INFINITY);
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-                  if (is_odd && ((valid[n] >> key) & 1)) ot[n][db][c] += v;
-              }
-          __syncthreads();
-          for (int c = tid; c < GM::TILE / 16; c += NT) {
-            uint4* at = (uint4*)(vt + 16 * c);
-            *at = make_uint4(finite_only(at->x), finite_only(at->y), finite_only(at->z), finite_only(at->w));
-          }
-          __syncthreads();
-        }
       }
     }
     // ---- the reference of the exponentials: a lane sees 16 of its row's 64 scores; if none of the wave's lanes exceeds its row's by more than the step, no row does
@@ -922,6 +901,37 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
 #pragma unroll
         for (int db = 0; db < DB; ++db) ot[n][db] *= alpha;
         m_ref[n] = m_new;
+      }
+    }
+    if (partial) {
+      // infinities and NaN among values that not every query sees (every wave looks through the whole tile, so all agree); behind the rescaling, whose
+      // first factor is 0
+      uint32_t odd = 0;
+      char* const vt = smem_raw + NS * GM::TILE + ST * GM::TILE;
+#pragma unroll
+      for (int c = 0; c < GM::CPT; ++c) {
+        const uint4 x = *(const uint4*)(vt + 1024 * c + 16 * lane);
+        odd |= odd_exponent(x.x) | odd_exponent(x.y) | odd_exponent(x.z) | odd_exponent(x.w);
+      }
+      if (__any((odd & 0x80008000u) != 0)) {   // they go to the queries that see them, and out of the tile
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          const u64 valid = sees(n);
+          for (int key = 0; key < KT; ++key)
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const float v = bf16_bits_to_f32(*(const uint16_t*)(vt + key * GM::RB + 16 * ((2 * db + (g >> 1)) ^ GM::vswz(key)) + 8 * (g & 1) + 2 * c));
+                if (!(fabsf(v) < INFINITY) && ((valid >> key) & 1)) ot[n][db][c] += v;
+              }
+        }
+        __syncthreads();
+        for (int c = tid; c < GM::TILE / 16; c += NT) {
+          uint4* at = (uint4*)(vt + 16 * c);
+          *at = make_uint4(finite_only(at->x), finite_only(at->y), finite_only(at->z), finite_only(at->w));
+        }
+        __syncthreads();
       }
     }
     float m_neg[NQ];
