@@ -189,20 +189,22 @@ class PagedLoop:
 
     The step inputs are one synthetic record, as in ``DecodeLoop``; ``prompt_k`` / ``prompt_v`` of ``admit`` stand for what a model makes of
     the prompts' tokens.  Lengths, tables and free pages live on the device: a step needs nothing from the host but a bound of the prefix lengths.
+    A row grows to ``max_len``, rounded up to whole pages; one without room, there or in the pool, stays as it is, and ``ctx.device_status()`` says so.
     Calls run on the stream that was current when the loop was made; inputs have to be ready for it."""
 
     def __init__(self, inp, page_size: int = 64, n_pages: Optional[int] = None, max_len: int = 4096, max_chunk: int = 1024, device: str = "cuda:0"):
-        self.inp, self.page_size, self.max_len, self.max_chunk = inp, page_size, max_len, max_chunk
+        width = -(-max_len // page_size)
+        self.inp, self.page_size, self.max_len, self.max_chunk = inp, page_size, width * page_size, max_chunk
         self.dev = torch.device(device)
         with torch.cuda.device(self.dev):
-            self._allocate(inp, page_size, n_pages, max_len, max_chunk, device)
+            self._allocate(inp, page_size, n_pages, width, max_chunk, device)
 
-    def _allocate(self, inp, page_size, n_pages, max_len, max_chunk, device) -> None:
+    def _allocate(self, inp, page_size, n_pages, width, max_chunk, device) -> None:
         self.step_in = binding.DeviceStep(inp, device)
-        S, width = inp.n_rows, -(-max_len // page_size)
+        S = inp.n_rows
         self.n_pages = S * width if n_pages is None else n_pages
         self.ctx = binding.Context(max_rows=max(S, inp.n_prompts), max_nodes_total=max(inp.q.shape[0], S * max_chunk), max_nodes_per_tree=self.step_in.max_tree,
-                                   max_prefix=max_len, n_heads=inp.n_heads, head_dim=inp.head_dim, hidden=inp.hidden, vocab=inp.vocab)
+                                   max_prefix=self.max_len, n_heads=inp.n_heads, head_dim=inp.head_dim, hidden=inp.hidden, vocab=inp.vocab)
         self.step_in.ctx = self.ctx
         i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=self.dev)  # noqa: E731
         dt = self.step_in.q.dtype
