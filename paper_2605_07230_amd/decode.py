@@ -190,7 +190,8 @@ class PagedLoop:
     The step inputs are one synthetic record, as in ``DecodeLoop``; ``prompt_k`` / ``prompt_v`` of ``admit`` stand for what a model makes of
     the prompts' tokens.  Lengths, tables and free pages live on the device: a step needs nothing from the host but a bound of the prefix lengths.
     A row grows to ``max_len``, rounded up to whole pages; one without room, there or in the pool, stays as it is, and ``ctx.device_status()`` says so.
-    Calls run on the stream that was current when the loop was made; inputs have to be ready for it."""
+    Calls run on the stream that was current when the loop was made; inputs have to be ready for it.  What is given under another current stream may be
+    dropped at once: its memory is not handed out again before the loop's stream has passed the call."""
 
     def __init__(self, inp, page_size: int = 64, n_pages: Optional[int] = None, max_len: int = 4096, max_chunk: int = 1024, device: str = "cuda:0"):
         width = -(-max_len // page_size)
@@ -219,6 +220,13 @@ class PagedLoop:
         self.longest = 0                       # host bound on the rows' lengths
         self.rows = inp.n_rows
 
+    def _keep(self, *tensors) -> None:
+        """Tensors of a caller: tells the allocator that the loop's stream uses them."""
+        if torch.cuda.current_stream(self.dev) != self.ctx.stream:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.ctx.stream)
+
     def _place(self, tokens: int, **lengths):
         """Pages and slots for new tokens; the rows' lengths become those behind them."""
         slot_map, source = (torch.empty(tokens, dtype=torch.int32, device=self.dev) for _ in range(2))
@@ -236,6 +244,7 @@ class PagedLoop:
             raise ValueError(f"chunks of {list(new_len)} tokens, {q.shape[0]} given: one chunk for each of {self.rows} rows, {self.ctx.limits.max_nodes_total} tokens together")
         if max(new_len) == 0:
             return
+        self._keep(q, k_new, v_new, out, lse)
         with torch.cuda.stream(self.ctx.stream):
             lens = torch.tensor(new_len, dtype=torch.int32, device=self.dev)
             before = self.seq_len.clone()
@@ -263,6 +272,7 @@ class PagedLoop:
 
     def draw(self, u, token, prob=None, **parameters) -> None:
         """Plain decoding: one token of every prompt from the logits of its tree's root (of the last ``step``), with each prompt's own sampling parameters."""
+        self._keep(u, token, prob, *parameters.values())
         with torch.cuda.stream(self.ctx.stream):
             roots = self.step_in.node_off[:-1].long()
             binding.sample_tokens(self.ctx, logits=self.step_in.logits.index_select(0, roots), u=u, token=token, prob=prob, **parameters)
