@@ -422,6 +422,9 @@ int convergence_weights(cascade_ctx* ctx, const conv_weight_args* args);
  *                        block_table[s, x / page_size], at x % page_size in it.  Pages of a row's own; what stands behind the
  *                        pages that hold its positions is not read
  *     slot               page * page_size + x % page_size
+ *
+ * Without rows, tokens or layers a call on pages, and sample_tokens without rows, checks its other arguments and does nothing: no output is written (paged_slots:
+ * free_count_out is not either), and buffers of no elements may be NULL.
  */
 #define CASCADE_MAX_PAGE 1024
 

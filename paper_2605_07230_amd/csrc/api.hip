@@ -451,12 +451,11 @@ static int check_pages(int32_t n_pages, int32_t page_size) {
 
 int paged_slots(cascade_ctx* ctx, const paged_slots_args* a) {
   if (!ctx || !a) return CASCADE_EINVAL;
-  if (!a->seq_len || !a->block_table || !a->free_count || !a->free_count_out || !a->q_off || !a->seq_len_out || a->seq_len == a->seq_len_out ||
-      a->free_count == a->free_count_out)
-    return CASCADE_EINVAL;
+  if (!a->free_count || !a->free_count_out || !a->q_off || a->free_count == a->free_count_out) return CASCADE_EINVAL;
   if (a->n_rows < 0 || a->table_width < 0 || a->table_stride < a->table_width || a->max_tokens < 0 || a->free_capacity < 0) return CASCADE_EINVAL;
+  if (a->n_rows > 0 && (!a->seq_len || !a->seq_len_out || a->seq_len == a->seq_len_out || (a->table_width > 0 && !a->block_table))) return CASCADE_EINVAL;
   if ((a->max_tokens > 0 && !a->slot_map) || (a->free_capacity > 0 && !a->free_pages)) return CASCADE_EINVAL;
-  if (!a->new_len) {
+  if (!a->new_len && a->n_rows > 0) {
     if (!a->node_off || !a->row_prompt || !a->accept_len || (a->max_tokens > 0 && !a->source)) return CASCADE_EINVAL;
     if (a->n_prompts < 0 || a->max_depth < 0 || a->n_nodes_total < 0 || (a->max_depth > 0 && !a->path_nodes)) return CASCADE_EINVAL;
     if (a->max_depth > CASCADE_MAX_DEPTH || a->n_nodes_total > ctx->lim.max_nodes_total) return CASCADE_ESHAPE;
@@ -470,7 +469,8 @@ int paged_slots(cascade_ctx* ctx, const paged_slots_args* a) {
 
 int paged_append(cascade_ctx* ctx, const paged_append_args* a) {
   if (!ctx || !a) return CASCADE_EINVAL;
-  if (!a->slot_map || !a->k_new || !a->v_new || !a->k_pages || !a->v_pages) return CASCADE_EINVAL;
+  const bool some = a->n_layers != 0 && a->n_tokens != 0;   // (buffers of no elements need no address)
+  if (some && (!a->slot_map || !a->k_new || !a->v_new || !a->k_pages || !a->v_pages)) return CASCADE_EINVAL;
   if (a->dtype != CASCADE_F32 && a->dtype != CASCADE_BF16) return CASCADE_EDTYPE;
   if (a->n_layers < 0 || a->n_tokens < 0 || a->n_source < 0 || a->n_kv_heads <= 0 || a->head_dim <= 0) return CASCADE_EINVAL;
   if (!a->source && a->n_source < a->n_tokens) return CASCADE_EINVAL;
@@ -483,15 +483,16 @@ int paged_append(cascade_ctx* ctx, const paged_append_args* a) {
   if ((a->head_dim * e) % 16) return CASCADE_ESHAPE;
   if (((uintptr_t)a->k_new | (uintptr_t)a->v_new | (uintptr_t)a->k_pages | (uintptr_t)a->v_pages) & 15) return CASCADE_EINVAL;
   if (a->n_layers > 65535 || (int64_t)a->n_tokens * a->n_kv_heads * (a->head_dim * e / 16) > 0x7fffffff) return CASCADE_ESHAPE;
-  if (a->n_layers == 0 || a->n_tokens == 0) return CASCADE_OK;
+  if (!some) return CASCADE_OK;
   return on_device(ctx, [&] { return launch_paged_append(ctx, a); });
 }
 
 static int check_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a) {
-  if (!a->q_off || !a->prefix_len || !a->q || !a->k_new || !a->v_new || !a->out) return CASCADE_EINVAL;
+  const bool some = a->n_rows != 0 && a->n_tokens != 0;
+  if (some && (!a->q_off || !a->prefix_len || !a->q || !a->k_new || !a->v_new || !a->out)) return CASCADE_EINVAL;
   if (a->n_rows < 0 || a->n_tokens < 0 || a->max_new < 0 || a->max_prefix_len < 0 || a->window < 0 || a->n_sink < 0 || a->workspace_bytes < 0)
     return CASCADE_EINVAL;
-  if (a->max_prefix_len > 0 && (!a->k_pages || !a->v_pages || !a->block_table || a->n_pages == 0)) return CASCADE_EINVAL;
+  if (some && a->max_prefix_len > 0 && (!a->k_pages || !a->v_pages || !a->block_table || a->n_pages == 0)) return CASCADE_EINVAL;
   if (a->dtype != CASCADE_F32 && a->dtype != CASCADE_BF16) return CASCADE_EDTYPE;
   if (a->n_heads <= 0 || a->n_kv_heads <= 0 || a->head_dim <= 0 || bad_float(a->scale) || a->scale < 0.f) return CASCADE_EINVAL;
   if (a->n_heads % a->n_kv_heads != 0) return CASCADE_ESHAPE;
@@ -543,7 +544,7 @@ int paged_attn_workspace(const cascade_ctx* ctx, const paged_attn_args* a, int64
 
 int sample_tokens(cascade_ctx* ctx, const sample_args* a) {
   if (!ctx || !a) return CASCADE_EINVAL;
-  if (!a->logits || !a->u || !a->token) return CASCADE_EINVAL;
+  if (a->n_rows != 0 && (!a->logits || !a->u || !a->token)) return CASCADE_EINVAL;
   if (a->dtype != CASCADE_F32 && a->dtype != CASCADE_BF16) return CASCADE_EDTYPE;
   if (a->n_rows < 0 || a->vocab <= 0) return CASCADE_EINVAL;
   if (a->vocab > ctx->lim.vocab || (a->row_stride < a->vocab && a->n_rows > 1)) return CASCADE_ESHAPE;
