@@ -427,8 +427,18 @@ def _paged_attn_record(q_off, prefix_len, block_table, q, k_new, v_new, k_pages,
     n, heads, D = shape
     n_kv, kv_heads, D_kv = kv_shape
     q_stride, q_head, q_one = q.stride()
-    kv_strides = k_new.stride()
-    assert (D_kv == D == q_head == kv_strides[1] and q_one == 1 == kv_strides[2] and n_kv == n and kv_strides == v_new.stride() and kv_shape == v_new.shape
+    kv_stride, kv_head, kv_one = kv_strides = k_new.stride()
+    v_strides = v_new.stride()
+    if n <= 1 or q_head != D or kv_head != D or kv_strides != v_strides:   # a dimension of one element has any stride
+        v_stride, v_head, v_one = v_strides
+        if n <= 1:
+            q_stride, kv_stride, v_stride = heads * D, kv_heads * D, kv_heads * D
+        if heads == 1:
+            q_head = D
+        if kv_heads == 1:
+            kv_head = v_head = D
+        assert kv_stride == v_stride and kv_head == v_head and kv_one == v_one
+    assert (D_kv == D == q_head == kv_head and q_one == 1 == kv_one and n_kv == n and kv_shape == v_new.shape
             and out.shape == shape and out.is_contiguous() and dtype is k_new.dtype and dtype is v_new.dtype and dtype is out.dtype)
     if k_pages is not None:
         pool, (page_stride, head_stride, pos_stride, one) = k_pages.shape, k_pages.stride()
@@ -440,7 +450,7 @@ def _paged_attn_record(q_off, prefix_len, block_table, q, k_new, v_new, k_pages,
     else:
         pages, page_size, page_stride, head_stride, pos_stride, table_stride, width, kp, vp, table = 0, 16, 0, 0, 0, 0, 0, 0, 0, 0
     return _PAGED_ATTN(_dtype_code(q), prefix_len.numel(), q_off.data_ptr(), 0 if parent is None else parent.data_ptr(), prefix_len.data_ptr(), n, max_new,
-                       max_prefix_len, heads, kv_heads, D, scale, window, n_sink, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), q_stride, kv_strides[0], kp, vp,
+                       max_prefix_len, heads, kv_heads, D, scale, window, n_sink, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), q_stride, kv_stride, kp, vp,
                        page_stride, head_stride, pos_stride, pages, page_size, table, table_stride, width, out.data_ptr(), 0 if lse is None else lse.data_ptr(),
                        *((0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())))
 
