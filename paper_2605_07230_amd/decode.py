@@ -246,12 +246,17 @@ class PagedLoop:
             return
         self._keep(q, k_new, v_new, out, lse)
         with torch.cuda.stream(self.ctx.stream):
+            attn = dict(q_off=self.q_off, block_table=self.block_table, q=q, k_new=k_new, v_new=v_new, k_pages=self.k_pages[0], v_pages=self.v_pages[0], out=out, lse=lse,
+                        max_new=max(new_len), max_prefix_len=self.longest)
+            append = dict(k_new=k_new.unsqueeze(0), v_new=v_new.unsqueeze(0), k_pages=self.k_pages, v_pages=self.v_pages)
+            # what the two calls refuse they refuse before rows grow (an append of no tokens looks at everything else)
+            binding.paged_attn_workspace(self.ctx, prefix_len=self.seq_len, **attn)
+            binding.paged_append(self.ctx, slot_map=self.q_off[:0], **append)
             lens = torch.tensor(new_len, dtype=torch.int32, device=self.dev)
             before = self.seq_len.clone()
             slot_map, _ = self._place(q.shape[0], new_len=lens)
-            binding.paged_attn(self.ctx, q_off=self.q_off, prefix_len=before, block_table=self.block_table, q=q, k_new=k_new, v_new=v_new, k_pages=self.k_pages[0],
-                               v_pages=self.v_pages[0], out=out, lse=lse, max_new=max(new_len), max_prefix_len=self.longest)
-            binding.paged_append(self.ctx, k_new=k_new.unsqueeze(0), v_new=v_new.unsqueeze(0), slot_map=slot_map, k_pages=self.k_pages, v_pages=self.v_pages)
+            binding.paged_attn(self.ctx, prefix_len=before, **attn)
+            binding.paged_append(self.ctx, slot_map=slot_map, **append)
         self.longest = min(self.longest + max(new_len), self.max_len)
 
     def step(self, mode: int = binding.WALK_SEQUENTIAL) -> None:
