@@ -537,6 +537,10 @@ typedef struct {
 } paged_attn_args;
 int paged_attn(cascade_ctx* ctx, const paged_attn_args* args);
 int paged_attn_workspace(const cascade_ctx* ctx, const paged_attn_args* args, int64_t* bytes);
+/* How such a call (valid, non-empty, not recorded) is cut, as cascade_attention_cut does for the step's: HOST only, pointers are looked at for NULL alone.  query_rows: rows
+ * of a workgroup (16, 64, 128, 256; f32: 16); key_parts: parts that the keys are cut in at most; waves: of a workgroup.  ctx NULL: as on 256 compute units with all the
+ * workspace that a cut could use. */
+int cascade_paged_cut(const cascade_ctx* ctx, const paged_attn_args* args, int32_t* query_rows, int32_t* key_parts, int32_t* waves);
 
 /* ---------------------------------------------------------------------------------------------
  * sample_tokens — a token from each row of logits, with the row's own parameters and uniform (plain decoding; the tokens of a

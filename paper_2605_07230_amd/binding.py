@@ -30,7 +30,7 @@ EXPORTS = ["cascade_create", "cascade_destroy", "cascade_strerror", "cascade_dev
            "cascade_set_kernel_timing", "cascade_read_kernel_timing", "cascade_measure_hbm_read",
            "cascade_measure_mfma_bf16", "cascade_pack_lmhead_w", "tree_verify_attn", "tree_verify_attn_static",
            "lmhead_softmax_cfg", "cascade_attention_cut", "cascade_projection_tiles", "cascade_projection_streams", "cascade_accept", "select_path", "kv_commit", "convergence_weights",
-           "paged_slots", "paged_append", "paged_attn", "paged_attn_workspace", "sample_tokens"]
+           "paged_slots", "paged_append", "paged_attn", "paged_attn_workspace", "cascade_paged_cut", "sample_tokens"]
 
 _vp, _i32, _i64, _f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
 
@@ -174,6 +174,8 @@ def load_library() -> C.CDLL:
     lib.cascade_projection_streams.restype = C.c_int
     lib.paged_attn_workspace.argtypes = [_vp, C.POINTER(paged_attn_args), C.POINTER(_i64)]
     lib.paged_attn_workspace.restype = C.c_int
+    lib.cascade_paged_cut.argtypes = [_vp, C.POINTER(paged_attn_args)] + [C.POINTER(_i32)] * 3
+    lib.cascade_paged_cut.restype = C.c_int
     for name, st in (("tree_verify_attn", tree_attn_args), ("lmhead_softmax_cfg", lmhead_args),
                      ("cascade_accept", accept_args), ("select_path", select_args), ("kv_commit", kv_commit_args),
                      ("convergence_weights", conv_weight_args), ("paged_slots", paged_slots_args), ("paged_append", paged_append_args),
@@ -472,6 +474,17 @@ def paged_attn_workspace(ctx: Context, *, q_off, prefix_len, block_table, q, k_n
     n = _i64()
     _check(ctx.lib.paged_attn_workspace(ctx.handle, C.byref(a), C.byref(n)))
     return n.value
+
+
+def paged_cut(*, n_rows, n_tokens, max_new, max_prefix_len, n_heads, n_kv_heads, head_dim, tree: bool = False, window: int = 0, n_sink: int = 0, dtype: int = BF16,
+              ctx: Optional[Context] = None):
+    """(query rows of a workgroup, parts of the keys, waves of a workgroup) of a paged_attn call of these sizes."""
+    a = paged_attn_args()
+    a.n_rows, a.n_tokens, a.max_new, a.max_prefix_len, a.window, a.n_sink, a.parent = n_rows, n_tokens, max_new, max_prefix_len, window, n_sink, 1 if tree else None
+    a.dtype, a.n_heads, a.n_kv_heads, a.head_dim = dtype, n_heads, n_kv_heads, head_dim
+    rows, parts, waves = _i32(), _i32(), _i32()
+    _check(load_library().cascade_paged_cut(ctx.handle if ctx else None, C.byref(a), C.byref(rows), C.byref(parts), C.byref(waves)))
+    return rows.value, parts.value, waves.value
 
 
 def sample_tokens(ctx: Context, *, logits, u, token, prob=None, temperature=None, top_k=None, top_p=None, min_p=None) -> None:

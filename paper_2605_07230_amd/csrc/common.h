@@ -98,6 +98,7 @@ hipError_t launch_paged_slots(cascade_ctx* ctx, const paged_slots_args* a);
 hipError_t launch_paged_append(cascade_ctx* ctx, const paged_append_args* a);
 hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a);
 int64_t plan_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a);   // bytes of partial results that the call's cut leaves
+void plan_paged_cut(const paged_attn_args* a, int n_cu, size_t ws_bytes, int32_t* query_rows, int32_t* key_parts, int32_t* waves);
 hipError_t launch_sample(cascade_ctx* ctx, const sample_args* a);
 
 // ----------------------------------------------------------------------------------------------

@@ -1311,6 +1311,8 @@ int tiles_bound(const paged_attn_args* a, int ts = KT) {
   return t + n;
 }
 
+int f32_waves(const paged_attn_args* a) { return a->head_dim <= 64 ? 16 : (a->head_dim <= 128 ? 8 : 4); }
+
 size_t part_bytes(const paged_attn_args* a) { return (size_t)a->n_tokens * a->n_heads * (a->head_dim + 2) * sizeof(float); }
 
 // Estimated time of a cut of many query rows, us: what the longest workgroup takes, or what all of them have to do where several share a compute unit, whichever is more.  A tile costs a
@@ -1351,7 +1353,7 @@ Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
   const int most = (int)std::min<size_t>(ws_bytes / part_bytes(a), MOST_PARTS);
   if (a->dtype == CASCADE_F32) {
     // few blocks share the keys, four tiles to a wave at least
-    const int waves = a->head_dim <= 64 ? 16 : (a->head_dim <= 128 ? 8 : 4);
+    const int waves = f32_waves(a);
     const int64_t blocks = a->n_rows * ((M + 15) / 16) * a->n_kv_heads;
     c.parts = (int)std::max<int64_t>(1, std::min<int64_t>({most, n_cu / blocks, tiles_bound(a, 16) / (4 * waves)}));
     return c;
@@ -1382,6 +1384,9 @@ Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
   return c;
 }
 
+// eight waves to a part where every part has a compute unit of its own (trees, few of which are that small: one kernel)
+int few_waves(const paged_attn_args* a, const Cut& c, int n_cu) { return !a->parent && (int64_t)a->n_rows * a->n_kv_heads * c.parts <= n_cu ? 8 : 4; }
+
 template <int D, int NW, bool TREE>
 hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
   constexpr int v_bytes = NW * KT * (D + 16) * 2, o_bytes = NW * 16 * (D + 4 + 2) * 4, smem = v_bytes > o_bytes ? v_bytes : o_bytes;
@@ -1396,7 +1401,7 @@ hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
 template <int D>
 hipError_t launch_few(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
   if (p.a.parent) return launch_few_k<D, 4, true>(ctx, p);
-  return (int64_t)p.a.n_rows * p.a.n_kv_heads * c.parts <= ctx->n_cu ? launch_few_k<D, 8, false>(ctx, p) : launch_few_k<D, 4, false>(ctx, p);
+  return few_waves(&p.a, c, ctx->n_cu) == 8 ? launch_few_k<D, 8, false>(ctx, p) : launch_few_k<D, 4, false>(ctx, p);
 }
 
 // no more blocks of so many query rows than this, whatever the rows' lengths are; a row out of order is one
@@ -1491,4 +1496,11 @@ hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
 int64_t plan_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a) {
   const Cut c = choose(a, ctx->n_cu, (size_t)1 << 40);
   return c.parts > 1 ? (int64_t)c.parts * (int64_t)part_bytes(a) : 0;
+}
+
+void plan_paged_cut(const paged_attn_args* a, int n_cu, size_t ws_bytes, int32_t* query_rows, int32_t* key_parts, int32_t* waves) {
+  const Cut c = choose(a, n_cu, ws_bytes);
+  *query_rows = SHAPE_ROWS[c.shape];
+  *key_parts = c.parts;
+  *waves = c.shape == FEW ? few_waves(a, c, n_cu) : (c.shape == F32 ? f32_waves(a) : (c.shape == RING_256 ? 8 : 4));
 }

@@ -1,0 +1,32 @@
+"""What the GPU tests of attention over pages reach: every kernel instance that the launch rules can choose is run by a test that compares its results (no GPU: the rules
+are host code and are asked through the library)."""
+import test_gpu_paged_cuts as cuts
+from paper_2605_07230_amd import binding
+
+
+def test_every_cut_is_tested():
+    reached, items = set(), set()      # (query rows, waves, head_dim, tree, keys in parts)
+    for name, kw in cuts.CASES.items():
+        for head_dim in (64, 128):
+            rows, parts, waves = cuts.cut(name, head_dim)
+            reached.add((rows, waves, head_dim, "tree" in kw, parts > 1))
+            if rows == 16:             # more (row, kv head) pairs than workgroups that the chip holds: a workgroup takes several
+                items.add((head_dim, "tree" in kw, len(kw["prefix"]) * kw["kv_heads"] * parts > 3 * 256))
+    both = (False, True)
+    few = {(16, 4, d, t, c) for d in (64, 128) for t in both for c in both} | {(16, 8, d, False, c) for d in (64, 128) for c in both}
+    many = {(rows, 4, d, t, c) for rows in (64, 128) for d in (64, 128) for t in both for c in both} | {(256, 8, 64, t, c) for t in both for c in both}
+    assert reached == few | many
+    assert items == {(d, t, m) for d in (64, 128) for t in both for m in both}
+
+
+def test_every_f32_cut_is_tested():
+    reached = {(head_dim, *cuts.f32_cut(name, head_dim)[1:]) for name in cuts.F32 for head_dim in (64, 100, 251)}
+    assert {(d, w) for d, p, w in reached if p == 1} == {(d, w) for d, p, w in reached if p > 1} == {(64, 16), (100, 8), (251, 4)}
+
+
+def test_the_query_refuses_what_it_does_not_describe():
+    lib, n, a = binding.load_library(), binding.C.c_int32(), binding.paged_attn_args()
+    assert lib.cascade_paged_cut(None, None, n, n, n) == binding.EINVAL and lib.cascade_paged_cut(None, a, n, n, None) == binding.EINVAL
+    assert lib.cascade_paged_cut(None, a, n, n, n) == binding.EINVAL           # no rows
+    a.dtype = 7
+    assert lib.cascade_paged_cut(None, a, n, n, n) == binding.EDTYPE
