@@ -1362,7 +1362,7 @@ Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
   // (17 to 32 query rows in waves of their own, twice the registers: 0.6 to 1.1 of the time at head_dim 64, 1.5 to 2.6 at 128, where they do not fit)
   if (M > 16) {
     float best = INFINITY;
-    for (int shape = RING_64; shape <= RING_256; ++shape)
+    for (int shape = RING_64; shape <= (a->head_dim == 64 ? RING_256 : RING_128); ++shape)   // (256 rows at head_dim 128 cost more than 128 rows at any size)
       for (int parts = 1; parts <= 16 && parts <= std::max(most, 1) && parts <= tiles; parts = parts < 4 ? parts + 1 : parts * 2) {
         const float us = ring_estimate_us(shape, a, parts, n_cu);
         if (us < best) { best = us; c.shape = shape; c.parts = parts; }
@@ -1428,8 +1428,9 @@ hipError_t launch_ring_k(cascade_ctx* ctx, PagedParams& p) {
 template <int D, bool TREE>
 hipError_t launch_ring(cascade_ctx* ctx, PagedParams& p, const Cut& c) {
   if (c.shape == RING_64) return launch_ring_k<D, 2, 1, 4, TREE>(ctx, p);
-  if (c.shape == RING_128) return launch_ring_k<D, 2, 2, 4, TREE>(ctx, p);
-  return launch_ring_k<D, 3, 2, 8, TREE>(ctx, p);
+  if constexpr (D == 64)
+    if (c.shape == RING_256) return launch_ring_k<D, 3, 2, 8, TREE>(ctx, p);
+  return launch_ring_k<D, 2, 2, 4, TREE>(ctx, p);
 }
 template <int DB, int NW, bool VEC, bool TREE>
 hipError_t launch_f32_k(cascade_ctx* ctx, PagedParams& p) {

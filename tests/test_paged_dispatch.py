@@ -1,5 +1,7 @@
 """What the GPU tests of attention over pages reach: every kernel instance that the launch rules can choose is run by a test that compares its results (no GPU: the rules
 are host code and are asked through the library)."""
+import random
+
 import test_gpu_paged_cuts as cuts
 from paper_2605_07230_amd import binding
 
@@ -22,6 +24,17 @@ def test_every_cut_is_tested():
 def test_every_f32_cut_is_tested():
     reached = {(head_dim, *cuts.f32_cut(name, head_dim)[1:]) for name in cuts.F32 for head_dim in (64, 100, 251)}
     assert {(d, w) for d, p, w in reached if p == 1} == {(d, w) for d, p, w in reached if p > 1} == {(64, 16), (100, 8), (251, 4)}
+
+
+def test_no_call_takes_256_rows_at_head_dim_128():
+    """The launch has no such kernel."""
+    rng = random.Random(3)
+    for _ in range(3000):
+        rows, new = int(2 ** rng.uniform(0, 9)), int(2 ** rng.uniform(0, 12))
+        kv, group, tree = rng.choice([1, 2, 4, 8, 32]), rng.choice([1, 2, 3, 8]), rng.random() < 0.5
+        cut = binding.paged_cut(n_rows=rows, n_tokens=rng.randint(new, rows * new), max_new=new, max_prefix_len=int(2 ** rng.uniform(0, 16)) - 1, n_heads=kv * group,
+                                n_kv_heads=kv, head_dim=128, tree=tree, window=rng.choice([0, 0, 300]))
+        assert cut[0] in (16, 64, 128)
 
 
 def test_the_query_refuses_what_it_does_not_describe():
