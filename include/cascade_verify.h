@@ -423,6 +423,9 @@ int convergence_weights(cascade_ctx* ctx, const conv_weight_args* args);
  *                        pages that hold its positions is not read
  *     slot               page * page_size + x % page_size
  *
+ * A row that ends gives its pages back: the first ceil(seq_len[s] / page_size) entries of its table are copied, in any order, to free_pages[free_count ..], free_count grows by
+ * their number and seq_len[s] becomes 0, in work on the ctx stream between two calls of paged_slots (free_capacity: all pages of the pool, then).  Its table needs no clearing.
+ *
  * Without rows, tokens or layers a call on pages, and sample_tokens without rows, checks its other arguments and does nothing: no output is written (paged_slots:
  * free_count_out is not either), and buffers of no elements may be NULL.
  */
