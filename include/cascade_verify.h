@@ -26,7 +26,8 @@
  *    synchronises the device.
  *    The calls of a context share its workspace and are ordered by its stream.  Replays of graphs captured
  *    from it: tree_verify_attn (keys in parts) and lmhead_softmax_cfg (packed or mixed rows) use that
- *    workspace, so replays that hold them have to be ordered with each other and with further such calls.
+ *    workspace, so replays that hold them have to be ordered with each other and with further such calls
+ *    (and with paged_attn calls that are not recorded and have no workspace of their own: keys in parts lie there too).
  *    Captured cascade_accept, select_path, kv_commit, convergence_weights, paged_slots, paged_append, paged_attn and sample_tokens
  *    use none of it: their replays may overlap with each other and with anything else.
  *  - Errors: 0 = CASCADE_OK, negative = cascade_status.  Errors detectable from host-visible
@@ -500,7 +501,8 @@ int paged_append(cascade_ctx* ctx, const paged_append_args* args);
  * token of the row attends (a window has passed them) are not read, nor are their entries in the table.
  *     q        element (t, g, d) at t*q_stride + g*head_dim + d;  k_new, v_new at t*kv_stride + kvh*head_dim + d
  *     out      [n_tokens, n_heads, head_dim] contiguous, dtype;  lse [n_tokens, n_heads] float32, may be NULL
- * Accumulation and softmax are float32.  Keys and values that a token does not attend, infinities and NaN among them, do not reach
+ * Accumulation, maxima and sums of the softmax are float32; bf16: a probability is rounded to bf16 where it enters the product with the values, as in tree_verify_attn,
+ * and lse and the sums are of the unrounded ones.  Keys and values that a token does not attend, infinities and NaN among them, do not reach
  * its output; infinite values that it attends make its output that infinity, unless their probability is 0 in float32 (then it may be NaN).
  * Tokens behind q_off[n_rows] are not written.  A row whose q_off is not in order or in n_tokens, that has more than
  * max_new tokens, or whose prefix is negative or longer than max_prefix_len or its table, gets zeros and lse = -inf and sets the flag; an

@@ -10,6 +10,9 @@
 // per-lane scalars, a mask is one 64-bit word per lane and tile, made from three comparisons, and the probabilities are already the B operand of
 // O^T = V^T P^T, whose A operand the transposing LDS read (ds_read_b64_tr_b16) takes from row-major values.
 //
+// Probabilities enter that product as bf16, the only type in which the matrix cores take them next to bf16 values at this rate: at most half a step, 2^-8 of each, which leaves
+// outputs 0.0022 from float64 (relative 2-norm) where probabilities in float32 leave 0.0017, the rounding of the result.  Sums, maxima and lse are of unrounded float32 ones.
+//
 // A masked key has probability 0, but 0 x inf and 0 x NaN are NaN.  Places that no token of the workgroup sees are never taken from memory, or are
 // zeroed on the way; a tile that some tokens see and others do not, or whose places behind the last key hold that key again, is looked through for such values, and if
 // it holds any they are taken out of the product and added to the tokens that see them, once what was summed before has its scale (the first scale is 0).
