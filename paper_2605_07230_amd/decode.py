@@ -262,13 +262,13 @@ class PagedLoop:
     def step(self, mode: int = binding.WALK_SEQUENTIAL) -> None:
         """One verification step of every prompt's tree over the pages, and the commit of what it accepts to them."""
         st = self.step_in
-        binding.paged_attn(self.ctx, q_off=st.row_node_off, parent=st.row_parent, prefix_len=self.seq_len, block_table=self.block_table, q=st.q, k_new=st.k_tree,
-                           v_new=st.v_tree, k_pages=self.k_pages[0], v_pages=self.v_pages[0], out=st.attn_out, lse=st.attn_lse, max_new=st.max_tree,
-                           max_prefix_len=self.longest)
-        st.lmhead()
-        st.accept()
-        st.select(mode)
-        with torch.cuda.stream(self.ctx.stream):
+        with torch.cuda.stream(self.ctx.stream):   # and on its device
+            binding.paged_attn(self.ctx, q_off=st.row_node_off, parent=st.row_parent, prefix_len=self.seq_len, block_table=self.block_table, q=st.q, k_new=st.k_tree,
+                               v_new=st.v_tree, k_pages=self.k_pages[0], v_pages=self.v_pages[0], out=st.attn_out, lse=st.attn_lse, max_new=st.max_tree,
+                               max_prefix_len=self.longest)
+            st.lmhead()
+            st.accept()
+            st.select(mode)
             slot_map, source = self._place(self.rows * (st.max_depth + 1), node_off=st.row_node_off, row_prompt=self.row_prompt, accept_len=st.accept_len,
                                            path_nodes=st.path_nodes, n_nodes_total=st.q.shape[0])
             binding.paged_append(self.ctx, k_new=st.k_tree.unsqueeze(0), v_new=st.v_tree.unsqueeze(0), slot_map=slot_map, source=source, k_pages=self.k_pages,

@@ -56,3 +56,30 @@ def test_given_tensors_stay_until_they_are_read(what, monkeypatch):
         assert not _meet(spans, [_span(t) for t in again])
     torch.cuda.synchronize()
     assert loop.ctx.device_status() == binding.OK
+
+
+def test_every_call_of_a_step_is_made_on_the_loops_stream_and_device(monkeypatch):
+    """The step's older calls launch on the device that is current: the loop makes its own current, whichever one the caller left."""
+    print("[paged loop] calls of a step", flush=True)
+    _, loop = _loop()
+    seen = []
+
+    def watched(owner, name):
+        call = getattr(owner, name)
+
+        def watch(*args, **kw):
+            seen.append((name, torch.cuda.current_stream(), torch.cuda.current_device()))
+            return call(*args, **kw)
+
+        monkeypatch.setattr(owner, name, watch)
+
+    for name in ("lmhead", "accept", "select"):
+        watched(loop.step_in, name)
+    for name in ("paged_attn", "paged_slots", "paged_append"):
+        watched(binding, name)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        loop.step()
+    torch.cuda.synchronize()
+    assert [x[0] for x in seen] == ["paged_attn", "lmhead", "accept", "select", "paged_slots", "paged_append"]
+    assert all(x[1:] == (loop.ctx.stream, loop.dev.index) for x in seen)
+    assert loop.ctx.device_status() == binding.OK
