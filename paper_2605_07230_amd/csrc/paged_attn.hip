@@ -176,9 +176,10 @@ __device__ __forceinline__ void write_nothing(const PagedParams& p, const RowInf
 // - and needs no barrier until their end, where the waves' maxima, sums and outputs meet in LDS.  Keys are loaded in operand order (16 bytes of
 // a key per lane), values through a region of LDS of the wave's own.  A workgroup works through parts (row, kv head, run of part_tiles tiles) until
 // none is left: rows of very different lengths share the chip, and no workgroup is launched for nothing.
-// One token of 64 rows x 4200 keys, 8 kv heads of 4, head_dim 128 (1.1 GB): 193 us = 5.7 TB/s; of 90 to 4200 keys (602 MB) 120 us and the join's 4; two rows x 312 keys, 32 kv heads: 9.5 us, of
+// One token of 64 rows x 4200 keys, 8 kv heads of 4, head_dim 128 (1.1 GB): 193 us = 5.7 TB/s; of 90 to 4200 keys (602 MB) 120 us and the join's 4; two rows x 312 keys, 32 kv heads: 9.8 us, of
 // which the chain row -> table -> tile -> join of the waves is all, and the way of its instructions from memory: lookups of a lane per group of keys on scalar bases and masks only where
-// something is masked (3600 -> 3000 instructions) took 1 us off every small call.  Sixty-four rows dealt longest first, every second round backwards: no faster (131 -> 146 then).
+// something is masked (3600 -> 3000 instructions) took 1 us off every small call.  (The look at a last key's values, 20
+// instructions, takes 0.35 of one.)  Sixty-four rows dealt longest first, every second round backwards: no faster (131 -> 146 then).  Sixteen trees of 15 nodes x 600 keys, 32 heads: 37 us = 4.5 TB/s.
 // Waves per SIMD: two, at head_dim 64, whose tiles are half as large, three of four-wave workgroups (64 rows of 90 to 4200 keys 70 -> 67 us, of 300 to 600 with 16 heads 28.3 -> 26.9).
 template <int D, int NW>
 constexpr int few_per_unit() { return D == 64 && NW == 4 ? 3 : 8 / NW; }
@@ -507,9 +508,11 @@ __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_ke
 // A wave's rows of a tile (8 or 16) lie in one group of 16 keys, so their page is one entry of the table.  The workgroup keeps the entries of its part in LDS, as
 // many as fit, and reads the one for the next tile a tile ahead.
 //
-// Bound by the matrix cores and the vector ALU taking turns: products keep the former busy 41 % of the cycles (clock 2.0 GHz under this load), the table costs nothing that can be
-// measured.  Eight rows of 500-1000 new tokens behind 0-2000, 8 kv heads of 4 (157 GFLOP): 189 us = 830 TFLOP/s in 128-row workgroups (64 rows: 259, 256 rows: 221); 256-node trees of
-// 8 rows x 32 heads behind 4200 keys (141 GFLOP): 181-184 us, 183 where the prefixes are contiguous; 1800-2000 new tokens under a window of 1024, head_dim 64: 41.5.
+// Bound by the matrix cores and the vector ALU taking turns: products keep the former busy 40 to 42 % of the cycles, the latter 45 to 50 (clock 2.0 GHz under this load), the table costs nothing that can be
+// measured.  Eight rows of 500-1000 new tokens behind 0-2000, 8 kv heads of 4 (157 GFLOP): 188 us = 835 TFLOP/s in 128-row workgroups (64 rows: 259, 256 rows, tried there: 221); 256-node trees of
+// 8 rows x 32 heads behind 4200 keys (141 GFLOP): 181-184 us, 183 where the prefixes are contiguous; 1800-2000 new tokens under a window of 1024, head_dim 64: 40.2
+// (half the products per exponential: 21 and 48 %; the chunks above with that head_dim 125, the trees 130).  Three workgroups per compute unit are what head_dim 64 runs best with, and they leave
+// 128-row workgroups 168 registers: 9 (chains) and 14 (trees) go to scratch.
 // Sums of the probabilities as they are, before they are rounded, cost less than products with ones (196 -> 184 us for the trees: registers) and give an exact lse.
 template <int D>
 struct RingGeom {
@@ -1024,7 +1027,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
 //   O^T = V^T P^T product r takes P^T straight from register r of that result, and element c of the 16 bytes at d = 64 h + 4 l16 of key 4 g + r's value: its row l16
 //                 stands for that d + c (element loads: d = 16 db + l16).
 // Nothing passes through LDS before the waves meet.  Bound by the trips to memory, one after the other: the row's place, the table's entry, the first tile.
-// 15 new tokens x 8 heads x 64 behind 256 keys: 9 us.
+// 15 new tokens x 8 heads x 64 behind 256 keys: 9 us.  Many rows fetch every key again for each 16 of them: 8 rows of 200 tokens behind 1289 keys, 8 heads: 94 us at head_dim 64 (49 TFLOP/s; 30 at the rate
+// of a large product), 161 at 128 (57 TFLOP/s).
 template <int DB, int NW, bool VEC, bool TREE>
 __global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
   extern __shared__ __align__(16) float f32_smem[];   // [NW][16 queries][16 DB + 4] outputs, [NW][16][2] maxima and sums

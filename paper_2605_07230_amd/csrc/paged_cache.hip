@@ -8,7 +8,7 @@ namespace {
 // they reach; where they stop reaching, no later row gets any either.  That is one exclusive scan over the rows (of new tokens, which
 // also places them, then of pages), which every workgroup makes by itself from the lengths: two or three values of a few
 // hundred rows cost less than a second launch.  A workgroup then writes the tokens of its row, or of a part of it, a token to a thread.
-// Bound by launch and the chain lengths -> scan -> table -> slot: 16 rows 4.4 us, 256 rows with 165000 tokens 7.2.
+// Bound by launch and the chain lengths -> scan -> table -> slot: 16 rows 4.2 us, 256 rows with 159052 tokens 6.6.
 struct SlotParams {
   paged_slots_args a;
   int* dev_status;
@@ -157,8 +157,8 @@ __global__ __launch_bounds__(SLOT_THREADS) void paged_slots_kernel(SlotParams p)
 
 // --------------------------------------------------------------------------------------------------------------- paged_append
 // A gather / scatter of 16-byte pieces, like kv_commit: workgroup = (a run of pieces, layer, keys or values); a thread
-// requests its pieces' slots, then the pieces themselves, and stores them past the caches.  Bound by the copy: 495 MB (30 layers, 2000 tokens of 8 x 128) 84 us =
-// 5.9 TB/s, read and write counted; one token of 16 rows x 30 layers (16 MB) 4.8.
+// requests its pieces' slots, then the pieces themselves, and stores them past the caches.  Bound by the copy: 495 MB (30 layers, 2000 tokens of 8 x 128) 85 us =
+// 5.9 TB/s, read and write counted; one token of 16 rows x 30 layers (16 MB) 4.7.
 struct AppendParams {
   paged_append_args a;
   int* dev_status;

@@ -20,8 +20,9 @@
 // the bin where that happens, if they are 256 at most, are ranked against each other; more of them (masked rows, ties, narrow rows) are divided by the bits of their values.
 //
 // What bounds it: one row, the chain of passes, barriers and instruction fetches (code that a workgroup runs through once costs 10 to 20 ns an instruction); a full
-// chip, the weights - 17 instructions on doubles an entry are 17 us for a row of 65536 on one compute unit, as long as the row needs to come from memory.  Measured, one row of 16384, one of
-// 65536 and 256 of 65536 (67 MB, 13 us at the rate of a large copy): greedy 4.4, 7.2, 17 us; no cut 8, 21, 30; top-k 2000 13, 20, 30; top-p 0.9 22, 47, 62; both 16, 24, 34.
+// chip, a compute unit's vector instructions: without a cut 40 an entry, 17 of them on doubles, are 41 of the 60 thousand cycles that a row of 65536 takes (greedy 13 of 34,
+// top-k 32 of 61, top-p 86 of 127), and rows without top-p wait for those with it.  Measured, one row of 16384, one of 65536 and 256 of 65536 (67 MB, 13 us at the rate of a large
+// copy): greedy 4.0, 7.3, 17 us; no cut 9, 21, 30; top-k 2000 13, 20, 30; top-k 5000 18, 47, 64; top-p 0.9 23, 47, 61; top-k 2000 and top-p 16, 24, 34.
 // A row kept in registers, 64 entries to a thread, is read once for certain, but every loop over it is unrolled: its code does not fit the instruction cache, 52 us
 // for one row of 65536 without a cut and 57 with top-k 2000.
 #include "common.h"
