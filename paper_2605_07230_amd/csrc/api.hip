@@ -545,7 +545,8 @@ int paged_attn_workspace(const cascade_ctx* ctx, const paged_attn_args* a, int64
 int cascade_paged_cut(const cascade_ctx* ctx, const paged_attn_args* a, int32_t* query_rows, int32_t* key_parts, int32_t* waves) {
   if (!a || !query_rows || !key_parts || !waves) return CASCADE_EINVAL;
   if (a->dtype != CASCADE_F32 && a->dtype != CASCADE_BF16) return CASCADE_EDTYPE;
-  if (a->n_rows <= 0 || a->n_tokens <= 0 || a->max_new <= 0 || a->max_prefix_len < 0 || a->window < 0 || a->n_sink < 0 || a->n_kv_heads <= 0 ||
+  if (a->n_rows <= 0 || a->n_tokens <= 0 || a->max_new <= 0 || a->max_new > (1 << 30) || a->max_prefix_len < 0 || a->max_prefix_len > (1 << 30) || a->window < 0 ||
+      a->n_sink < 0 || a->n_kv_heads <= 0 ||
       a->n_heads < a->n_kv_heads || a->head_dim <= 0 || a->head_dim > 256 || (a->dtype == CASCADE_BF16 && a->head_dim != 64 && a->head_dim != 128))
     return CASCADE_EINVAL;
   plan_paged_cut(a, ctx ? ctx->n_cu : 256, ctx ? ctx->attn_ws_bytes : (size_t)1 << 40, query_rows, key_parts, waves);

@@ -43,3 +43,10 @@ def test_the_query_refuses_what_it_does_not_describe():
     assert lib.cascade_paged_cut(None, a, n, n, n) == binding.EINVAL           # no rows
     a.dtype = 7
     assert lib.cascade_paged_cut(None, a, n, n, n) == binding.EDTYPE
+    good = dict(n_rows=1, n_tokens=1, max_new=1, n_heads=2, n_kv_heads=1, head_dim=64, dtype=binding.BF16)
+    for changes in ({}, dict(dtype=binding.F32, head_dim=3)):
+        b = binding.paged_attn_args(**{**good, **changes})
+        assert lib.cascade_paged_cut(None, b, n, n, n) == binding.OK
+    for k, v in (("n_rows", 0), ("n_tokens", -1), ("max_new", 2 ** 31 - 1), ("max_prefix_len", 2 ** 31 - 1), ("max_prefix_len", -1), ("window", -1), ("n_sink", -1), ("n_kv_heads", 0),
+                 ("n_heads", 0), ("head_dim", 96)):
+        assert lib.cascade_paged_cut(None, binding.paged_attn_args(**{**good, k: v}), n, n, n) == binding.EINVAL, k
