@@ -13,7 +13,8 @@
  * prefix cache.
  *
  * Around the step: paged_slots, paged_append and paged_attn keep the prefixes of many requests in pages (prompts, single tokens,
- * drafted trees), sample_tokens draws tokens from rows of logits.
+ * drafted trees), paged_attn_shared is that attention where requests have a long prefix in common, paged_mass and paged_evict hold
+ * caches to a budget by what attention uses of them, sample_tokens draws tokens from rows of logits.
  *
  * General conventions
  * -------------------
@@ -27,9 +28,10 @@
  *    The calls of a context share its workspace and are ordered by its stream.  Replays of graphs captured
  *    from it: tree_verify_attn (keys in parts) and lmhead_softmax_cfg (packed or mixed rows) use that
  *    workspace, so replays that hold them have to be ordered with each other and with further such calls
- *    (and with paged_attn calls that are not recorded and have no workspace of their own: keys in parts lie there too).
- *    Captured cascade_accept, select_path, kv_commit, convergence_weights, paged_slots, paged_append, paged_attn and sample_tokens
- *    use none of it: their replays may overlap with each other and with anything else.
+ *    (and with paged_attn and paged_attn_shared calls that are not recorded and have no workspace of their own: keys in parts lie there too).
+ *    Captured cascade_accept, select_path, kv_commit, convergence_weights, paged_slots, paged_append, paged_attn, paged_attn_shared,
+ *    paged_mass, paged_evict and sample_tokens use none of it: their replays may overlap with each other and with anything else (but for
+ *    what they are given: a workspace, outputs, pages that one writes).
  *  - Errors: 0 = CASCADE_OK, negative = cascade_status.  Errors detectable from host-visible
  *    arguments (null pointers, shapes, limits, dtype) are reported before anything is enqueued and
  *    leave outputs untouched.  HIP runtime failures give CASCADE_EHIP.  Preconditions on device
@@ -101,8 +103,8 @@ const char* cascade_strerror(int status);
  * sized for - tree_attn_args.max_nodes_per_tree, cascade_limits.max_nodes_per_tree - whose nodes are
  * then not verified: bf16 attention rows of such a tree are written as zeros with lse = -inf (the f32
  * path has no such bound), acceptance scalars beyond the bound as zeros, the walk sees only the nodes
- * inside the bound; a kv_commit row without room or with a path entry outside its tree; what paged_slots, paged_append and
- * paged_attn say of themselves), and clears the flag. */
+ * inside the bound; a kv_commit row without room or with a path entry outside its tree; what paged_slots, paged_append,
+ * paged_attn, paged_attn_shared, paged_mass and paged_evict say of themselves), and clears the flag. */
 int cascade_device_status(cascade_ctx* ctx);
 /* Bytes of device workspace the ctx holds (HOST query). */
 int64_t cascade_workspace_bytes(const cascade_ctx* ctx);
@@ -124,10 +126,13 @@ typedef enum {
   CASCADE_K_PACK = 8,        /* hidden-state repacking in front of the packed projection */
   CASCADE_K_SLOTS = 9,       /* paged_slots */
   CASCADE_K_APPEND = 10,     /* paged_append */
-  CASCADE_K_PAGED_ATTN = 11, /* paged_attn main kernel */
-  CASCADE_K_PAGED_MERGE = 12, /* its merge of keys in parts */
+  CASCADE_K_PAGED_ATTN = 11, /* paged_attn main kernel; paged_attn_shared: both passes */
+  CASCADE_K_PAGED_MERGE = 12, /* their merge of keys in parts */
   CASCADE_K_SAMPLE = 13,     /* sample_tokens */
-  CASCADE_K_COUNT = 14
+  CASCADE_K_MASS = 14,       /* paged_mass */
+  CASCADE_K_EVICT = 15,      /* paged_evict: what stays */
+  CASCADE_K_EVICT_MOVE = 16, /* paged_evict: the moves */
+  CASCADE_K_COUNT = 17
 } cascade_kernel_id;
 int cascade_set_kernel_timing(cascade_ctx* ctx, int enable);
 int cascade_read_kernel_timing(cascade_ctx* ctx, int kernel_id, double* total_ms, int32_t* launches);
@@ -546,6 +551,120 @@ int paged_attn_workspace(const cascade_ctx* ctx, const paged_attn_args* args, in
  * of a workgroup (16, 64, 128, 256; f32: 16); key_parts: parts that the keys are cut in at most; waves: of a workgroup.  ctx NULL: as on 256 compute units with all the
  * workspace that a cut could use. */
 int cascade_paged_cut(const cascade_ctx* ctx, const paged_attn_args* args, int32_t* query_rows, int32_t* key_parts, int32_t* waves);
+
+/* paged_attn_shared — paged_attn for rows that have a prefix in common (many images of one prompt, the guidance rows of all of them): out and lse are those of
+ * paged_attn with `attn`, but for rounding.  Rows group_off[g] .. group_off[g+1] - 1 of the batch are group g; the pages of their positions 0 .. shared_len[g] - 1 are
+ * the same ones in the same order (each row's table names them).  Those keys and values are read once for the whole group, through the table of
+ * its first row, and meet the tokens of all its rows as one product; the rows' other positions and new tokens are taken as paged_attn takes them, and the results are joined.
+ * Where a row of the group has fewer positions in its cache than shared_len[g], the group shares as many as that row has; a group of one row, a shared_len below 64 (negative
+ * ones among them) and a row that paged_attn would not compute make the group's rows read everything by themselves.  group_off has to begin with 0, not to
+ * decrease, and to end with n_rows; if it does not no group shares anything and the flag is set.
+ * Calls in which a pass over shared keys cannot save anything are paged_attn's own: those with a window, without groups, recorded into a graph without a workspace, and with more
+ * query rows to a row than a matrix product of its own needs (cascade_paged_shared says).  Workspace as for paged_attn: both passes leave partial results.
+ */
+typedef struct {
+  paged_attn_args attn;
+  int32_t n_groups;
+  int32_t max_shared_len;       /* HOST upper bound on any shared_len[g] */
+  const int32_t* group_off;     /* [n_groups+1] */
+  const int32_t* shared_len;    /* [n_groups] */
+} paged_shared_args;
+int paged_attn_shared(cascade_ctx* ctx, const paged_shared_args* args);
+int paged_attn_shared_workspace(const cascade_ctx* ctx, const paged_shared_args* args, int64_t* bytes);
+/* How such a call (valid, non-empty, not recorded) is cut, as cascade_paged_cut says it for paged_attn: query rows of a workgroup and parts of the pass over the shared keys
+ * (0, 0: the call is paged_attn's), then of the rows' own pass. */
+int cascade_paged_shared(const cascade_ctx* ctx, const paged_shared_args* args, int32_t* shared_rows, int32_t* shared_parts, int32_t* own_rows, int32_t* own_parts);
+
+/* paged_mass — the attention weight that positions of a cache gather, for paged_evict.  For row s with L = seq_len[s] positions in the cache, the last
+ * n = q_off[s+1] - q_off[s] of which are its new tokens (the call comes behind paged_append), kv head h and position y:
+ *     w(y) = sum over tokens j of the row and query heads g of kv head h:  exp(scale * <q_jg, k_y> - lse_jg),  y among the positions that token j, at L - n + j, attends:
+ *            0 .. L - n + j,  with window > 0 only those with  (L - n + j) - y < window  or  y < n_sink
+ *     mass(s, h, y) = w(y)  for the new tokens' positions y >= L - n;   mass(s, h, y) += w(y)  for y below;   y < first[s] and y >= L are left as they are
+ * Token j is packed token q_off[s] + j of q and lse, or source[q_off[s] + j] (what paged_slots wrote for an accepted path: of a drafted tree the nodes that were kept
+ * count, with the lse of their ancestors).  lse is paged_attn's.  A token whose source is -1 counts nothing and so does one whose lse is not finite; the other
+ * sources outside the packed tokens set the flag.  Keys that no counted token attends do not reach the result, whatever they hold.
+ * A row whose q_off is not in order or in n_tokens, that has more than max_new tokens or fewer positions than tokens, or whose length is
+ * negative or larger than max_seq_len, its table or mass_cap, is left as it is and sets the flag, as do entries of the table outside the pool (their positions get nothing).
+ * Scores and sums are float32, in an order that depends on nothing but the call's sizes.
+ *     q, lse       as in paged_attn, n_source packed tokens;  k_pages, block_table likewise (the call is one layer's)
+ *     mass         element (s, h, y) at s*mass_stride_row + h*mass_stride_head + y, float32, mass_cap positions each
+ * bf16: head_dim 64 or 128, strides multiples of 8 elements, buffers on 16-byte boundaries.  f32: any head_dim up to 256.
+ */
+typedef struct {
+  cascade_dtype dtype;
+  int32_t n_rows;
+  const int32_t* q_off;         /* [n_rows+1] */
+  const int32_t* seq_len;       /* [n_rows] */
+  const int32_t* source;        /* [n_tokens], nullable => token t itself (n_source >= n_tokens) */
+  const int32_t* first;         /* [n_rows], nullable => 0 */
+  int32_t n_tokens;             /* HOST: tokens that q_off may count */
+  int32_t n_source;             /* HOST: tokens that q and lse hold */
+  int32_t max_new;              /* HOST upper bound on any row's tokens */
+  int32_t max_seq_len;          /* HOST upper bound on any seq_len[s] */
+  int32_t n_heads, n_kv_heads, head_dim;
+  float scale;                  /* 0 => 1/sqrt(head_dim) */
+  int32_t window, n_sink;       /* as the attention's */
+  const void* q;
+  int64_t q_stride;
+  const float* lse;             /* [n_source, n_heads] */
+  const void* k_pages;
+  int64_t stride_page, stride_head, stride_pos;
+  int32_t n_pages, page_size;
+  const int32_t* block_table;
+  int64_t table_stride;
+  int32_t table_width, mass_cap;
+  float* mass;
+  int64_t mass_stride_row, mass_stride_head;
+} paged_mass_args;
+int paged_mass(cascade_ctx* ctx, const paged_mass_args* args);
+
+/* paged_evict — rows that have outgrown their budget give up positions, in every layer and kv head those with the least mass.  For row s with L = seq_len[s]:
+ *     f = min(n_first[s], L) positions at the front and r = min(n_recent, L - f) at the end stay, whatever their mass;
+ *     N = max(min(budget[s], L), f + r) positions remain;  of f .. L - r - 1 the N - f - r with the largest mass (of equal ones the lower position) are kept
+ *     kept positions below N - r stay where they are;  the places f .. N - r - 1 that are given up receive, in ascending order, the kept positions from N - r on, in
+ *     ascending order;  then the last r go to N - r .. N - 1, in order
+ *     keys, values (bit for bit, in place) and mass (to mass_out, places 0 .. N - 1 of it; all of them, also where nothing moves) go along
+ *     seq_len_out[s] = N,  dropped[s] = L - N (may be NULL): what positions behind the cache have to be counted on by, since paged_slots' are of the cache
+ *     the entries ceil(N / page_size) .. ceil(L / page_size) - 1 of its table are put behind the first free_count[0] of free_pages, rows in order,
+ *     free_count_out[0] = their number and free_count[0]
+ * Heads and layers of a row keep positions of their own, so what stands at a place of the cache has no common position any more: attention over the row takes no window,
+ * and keys carry what they need to know of their positions.  Pages that rows share (paged_attn_shared) have to lie in the first n_first positions of each.
+ * NaN counts as less than any mass.  A negative n_first or budget counts as 0.  A row whose length is negative or larger than max_seq_len, its table or mass_cap is left as it is
+ * (seq_len_out = L, dropped 0, nothing of mass_out) and sets the flag.  Places whose page lies outside the pool are neither read nor written and set the flag; the entries
+ * are given back as they stand.  A free_count outside the list, or one behind which the entries have no room, sets it too: what has no place is not written.
+ *     mass, mass_out  element (layer, s, h, y) at layer*mass_stride_layer + s*mass_stride_row + h*mass_stride_head + y, float32, mass_cap positions each; they may not overlap
+ *     k_pages, v_pages  strides as for paged_append; head_dim and all strides multiples of 16 bytes, buffers on 16-byte boundaries
+ *     seq_len_out, free_count_out may not alias their inputs
+ *     workspace       of paged_evict_workspace's bytes, 16-byte boundary; calls that may overlap need one each
+ */
+typedef struct {
+  cascade_dtype dtype;
+  int32_t n_layers, n_rows, n_kv_heads, head_dim;
+  const int32_t* seq_len;       /* [n_rows] */
+  const int32_t* budget;        /* [n_rows] */
+  const int32_t* n_first;       /* [n_rows], nullable => 0 */
+  int32_t n_recent;
+  int32_t max_seq_len;          /* HOST upper bound on any seq_len[s] */
+  const float* mass;
+  float* mass_out;
+  int64_t mass_stride_layer, mass_stride_row, mass_stride_head;
+  int32_t mass_cap;
+  int32_t n_pages, page_size, table_width;
+  void *k_pages, *v_pages;
+  int64_t stride_layer, stride_page, stride_head, stride_pos;
+  const int32_t* block_table;
+  int64_t table_stride;
+  int32_t free_capacity;        /* HOST: entries of free_pages */
+  int32_t* free_pages;
+  const int32_t* free_count;    /* [1] */
+  int32_t* free_count_out;      /* [1] */
+  int32_t* seq_len_out;         /* [n_rows] */
+  int32_t* dropped;             /* [n_rows], nullable */
+  void* workspace;
+  int64_t workspace_bytes;
+} paged_evict_args;
+int paged_evict(cascade_ctx* ctx, const paged_evict_args* args);
+int paged_evict_workspace(const cascade_ctx* ctx, const paged_evict_args* args, int64_t* bytes);
 
 /* ---------------------------------------------------------------------------------------------
  * sample_tokens — a token from each row of logits, with the row's own parameters and uniform (plain decoding; the tokens of a

@@ -132,3 +132,35 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     over = np.flatnonzero(running > u * running[-1])
     token = int(over[0]) if len(over) else int(np.flatnonzero(w)[-1])
     return token, w[token] / running[-1], int(keep.sum())
+
+
+def attention_mass(q, lse, k, sees, scale=None):
+    """One kv head: q [T,G,D] and lse [T,G] of its query heads, k [n,D], sees [T,n].  Returns (weight that each key gathers, the same with each term times
+    its sum of |q_d k_d|, scaled, plus |lse|: what an error of the score is relative to)."""
+    q, lse, k = (np.asarray(x, F64) for x in (q, lse, k))
+    scale = scale or 1.0 / math.sqrt(q.shape[2])
+    got, size = np.zeros(len(k)), np.zeros(len(k))
+    for j in range(len(q)):
+        at = np.flatnonzero(sees[j])
+        for g in range(q.shape[1]):
+            if not np.isfinite(lse[j, g]) or not len(at):
+                continue
+            with np.errstate(invalid="ignore", over="ignore"):
+                w = np.exp(k[at] @ q[j, g] * scale - lse[j, g])
+                size[at] += w * (np.abs(lse[j, g]) + np.abs(k[at]) @ np.abs(q[j, g]) * scale)
+            got[at] += w
+    return got, size
+
+
+def evict_places(mass, length, budget, first=0, recent=0):
+    """One row of one layer and kv head: which position ends up in each place that remains."""
+    f = min(max(first, 0), length)
+    r = min(recent, length - f)
+    after = max(min(max(budget, 0), length), f + r)
+    weight = [-math.inf if math.isnan(x) else float(x) for x in mass[:length]]
+    nan = [math.isnan(x) for x in mass[:length]]
+    best = sorted(range(f, length - r), key=lambda y: (nan[y], -weight[y], y))[:after - r - f]
+    stay = {y for y in best if y < after - r}
+    come = sorted(y for y in best if y >= after - r)
+    place = list(range(f)) + [y if y in stay else None for y in range(f, after - r)] + list(range(length - r, length))
+    return [come.pop(0) if y is None else y for y in place]

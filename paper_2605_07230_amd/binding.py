@@ -21,7 +21,7 @@ F32, BF16 = 0, 1
 WALK_SEQUENTIAL, WALK_LONGEST = 0, 1
 FEATURES_HIDDEN, FEATURES_LOGITS = 0, 1
 K_ATTN, K_ATTN_MERGE, K_LMHEAD, K_ROW_STATS, K_ACCEPT, K_SELECT = range(6)
-K_SLOTS, K_APPEND, K_PAGED_ATTN, K_PAGED_MERGE, K_SAMPLE = range(9, 14)
+K_SLOTS, K_APPEND, K_PAGED_ATTN, K_PAGED_MERGE, K_SAMPLE, K_MASS, K_EVICT, K_EVICT_MOVE = range(9, 17)
 W_ROWMAJOR, W_PACKED32 = 0, 1
 CFG_MIX_LOGITS, CFG_MIX_HIDDEN = 0, 1
 OK, EINVAL, ESHAPE, EDTYPE, ENOMEM, EHIP, ETREE = 0, -1, -2, -3, -4, -5, -6
@@ -30,7 +30,8 @@ EXPORTS = ["cascade_create", "cascade_destroy", "cascade_strerror", "cascade_dev
            "cascade_set_kernel_timing", "cascade_read_kernel_timing", "cascade_measure_hbm_read",
            "cascade_measure_mfma_bf16", "cascade_pack_lmhead_w", "tree_verify_attn", "tree_verify_attn_static",
            "lmhead_softmax_cfg", "cascade_attention_cut", "cascade_projection_tiles", "cascade_projection_streams", "cascade_accept", "select_path", "kv_commit", "convergence_weights",
-           "paged_slots", "paged_append", "paged_attn", "paged_attn_workspace", "cascade_paged_cut", "sample_tokens"]
+           "paged_slots", "paged_append", "paged_attn", "paged_attn_workspace", "cascade_paged_cut", "paged_attn_shared",
+           "paged_attn_shared_workspace", "cascade_paged_shared", "paged_mass", "paged_evict", "paged_evict_workspace", "sample_tokens"]
 
 _vp, _i32, _i64, _f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
 
@@ -105,6 +106,28 @@ class paged_attn_args(C.Structure):
                 ("workspace_bytes", _i64)]
 
 
+class paged_shared_args(C.Structure):
+    # (its paged_attn_args come first and end on a boundary of eight bytes, so their fields stand here one by one)
+    _fields_ = paged_attn_args._fields_ + [("n_groups", _i32), ("max_shared_len", _i32), ("group_off", _vp), ("shared_len", _vp)]
+
+
+class paged_mass_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("n_rows", _i32), ("q_off", _vp), ("seq_len", _vp), ("source", _vp), ("first", _vp), ("n_tokens", _i32), ("n_source", _i32),
+                ("max_new", _i32), ("max_seq_len", _i32), ("n_heads", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("scale", _f32), ("window", _i32),
+                ("n_sink", _i32), ("q", _vp), ("q_stride", _i64), ("lse", _vp), ("k_pages", _vp), ("stride_page", _i64), ("stride_head", _i64),
+                ("stride_pos", _i64), ("n_pages", _i32), ("page_size", _i32), ("block_table", _vp), ("table_stride", _i64), ("table_width", _i32),
+                ("mass_cap", _i32), ("mass", _vp), ("mass_stride_row", _i64), ("mass_stride_head", _i64)]
+
+
+class paged_evict_args(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("n_layers", _i32), ("n_rows", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("seq_len", _vp), ("budget", _vp),
+                ("n_first", _vp), ("n_recent", _i32), ("max_seq_len", _i32), ("mass", _vp), ("mass_out", _vp), ("mass_stride_layer", _i64),
+                ("mass_stride_row", _i64), ("mass_stride_head", _i64), ("mass_cap", _i32), ("n_pages", _i32), ("page_size", _i32), ("table_width", _i32),
+                ("k_pages", _vp), ("v_pages", _vp), ("stride_layer", _i64), ("stride_page", _i64), ("stride_head", _i64), ("stride_pos", _i64),
+                ("block_table", _vp), ("table_stride", _i64), ("free_capacity", _i32), ("free_pages", _vp), ("free_count", _vp), ("free_count_out", _vp),
+                ("seq_len_out", _vp), ("dropped", _vp), ("workspace", _vp), ("workspace_bytes", _i64)]
+
+
 class sample_args(C.Structure):
     _fields_ = [("dtype", C.c_int), ("n_rows", _i32), ("vocab", _i32), ("logits", _vp), ("row_stride", _i64), ("temperature", _vp), ("top_k", _vp),
                 ("top_p", _vp), ("min_p", _vp), ("u", _vp), ("token", _vp), ("prob", _vp)]
@@ -131,6 +154,7 @@ class _Record:
 
 _TREE_ATTN, _LMHEAD, _ACCEPT, _SELECT, _COMMIT, _WEIGHTS = map(_Record, (tree_attn_args, lmhead_args, accept_args, select_args, kv_commit_args, conv_weight_args))
 _SLOTS, _APPEND, _PAGED_ATTN, _SAMPLE = map(_Record, (paged_slots_args, paged_append_args, paged_attn_args, sample_args))
+_SHARED_TAIL, _MASS, _EVICT = struct.Struct("@iiPP").pack, _Record(paged_mass_args), _Record(paged_evict_args)
 
 _lib = None
 
@@ -176,10 +200,17 @@ def load_library() -> C.CDLL:
     lib.paged_attn_workspace.restype = C.c_int
     lib.cascade_paged_cut.argtypes = [_vp, C.POINTER(paged_attn_args)] + [C.POINTER(_i32)] * 3
     lib.cascade_paged_cut.restype = C.c_int
+    lib.paged_attn_shared_workspace.argtypes = [_vp, C.POINTER(paged_shared_args), C.POINTER(_i64)]
+    lib.paged_attn_shared_workspace.restype = C.c_int
+    lib.cascade_paged_shared.argtypes = [_vp, C.POINTER(paged_shared_args)] + [C.POINTER(_i32)] * 4
+    lib.cascade_paged_shared.restype = C.c_int
+    lib.paged_evict_workspace.argtypes = [_vp, C.POINTER(paged_evict_args), C.POINTER(_i64)]
+    lib.paged_evict_workspace.restype = C.c_int
     for name, st in (("tree_verify_attn", tree_attn_args), ("lmhead_softmax_cfg", lmhead_args),
                      ("cascade_accept", accept_args), ("select_path", select_args), ("kv_commit", kv_commit_args),
                      ("convergence_weights", conv_weight_args), ("paged_slots", paged_slots_args), ("paged_append", paged_append_args),
-                     ("paged_attn", paged_attn_args), ("sample_tokens", sample_args)):
+                     ("paged_attn", paged_attn_args), ("paged_attn_shared", paged_shared_args), ("paged_mass", paged_mass_args),
+                     ("paged_evict", paged_evict_args), ("sample_tokens", sample_args)):
         fn = getattr(lib, name)
         fn.argtypes = [_vp, C.POINTER(st)]
         fn.restype = C.c_int
@@ -485,6 +516,112 @@ def paged_cut(*, n_rows, n_tokens, max_new, max_prefix_len, n_heads, n_kv_heads,
     rows, parts, waves = _i32(), _i32(), _i32()
     _check(load_library().cascade_paged_cut(ctx.handle if ctx else None, C.byref(a), C.byref(rows), C.byref(parts), C.byref(waves)))
     return rows.value, parts.value, waves.value
+
+
+def _paged_shared_record(group_off, shared_len, max_shared_len, **attn) -> bytes:
+    if group_off is None:
+        tail = _SHARED_TAIL(0, max_shared_len, 0, 0)
+    else:
+        n = shared_len.numel()
+        assert group_off.numel() == n + 1
+        tail = _SHARED_TAIL(n, max_shared_len, group_off.data_ptr(), shared_len.data_ptr())
+    return _paged_attn_record(**attn) + tail
+
+
+def paged_attn_shared(ctx: Context, *, group_off, shared_len, max_shared_len: int, q_off, prefix_len, block_table, q, k_new, v_new, k_pages, v_pages, out, lse=None,
+                      parent=None, scale: float = 0.0, window: int = 0, n_sink: int = 0, max_new: int, max_prefix_len: int,
+                      workspace: Optional[torch.Tensor] = None) -> None:
+    """paged_attn for rows whose first positions lie in the same pages: rows group_off[g] .. group_off[g + 1] - 1 share shared_len[g] of them
+    (group_off [n_groups + 1] and shared_len [n_groups] int32; None: nobody shares any).  workspace: paged_attn_shared_workspace says how much."""
+    _check(ctx.lib.paged_attn_shared_record(ctx.handle, _paged_shared_record(
+        group_off, shared_len, max_shared_len, q_off=q_off, prefix_len=prefix_len, block_table=block_table, q=q, k_new=k_new, v_new=v_new, k_pages=k_pages,
+        v_pages=v_pages, out=out, lse=lse, parent=parent, scale=scale, window=window, n_sink=n_sink, max_new=max_new, max_prefix_len=max_prefix_len,
+        workspace=workspace)))
+
+
+def paged_attn_shared_workspace(ctx: Context, *, group_off, shared_len, max_shared_len: int, q_off, prefix_len, block_table, q, k_new, v_new, k_pages, v_pages, out,
+                                lse=None, parent=None, scale: float = 0.0, window: int = 0, n_sink: int = 0, max_new: int, max_prefix_len: int) -> int:
+    """Bytes of scratch with which a paged_attn_shared call with these arguments never takes fewer parts than it would like."""
+    a = paged_shared_args.from_buffer_copy(_paged_shared_record(
+        group_off, shared_len, max_shared_len, q_off=q_off, prefix_len=prefix_len, block_table=block_table, q=q, k_new=k_new, v_new=v_new, k_pages=k_pages,
+        v_pages=v_pages, out=out, lse=lse, parent=parent, scale=scale, window=window, n_sink=n_sink, max_new=max_new, max_prefix_len=max_prefix_len,
+        workspace=None))
+    n = _i64()
+    _check(ctx.lib.paged_attn_shared_workspace(ctx.handle, C.byref(a), C.byref(n)))
+    return n.value
+
+
+def paged_shared_cut(*, n_rows, n_groups, n_tokens, max_new, max_prefix_len, max_shared_len, n_heads, n_kv_heads, head_dim, tree: bool = False, window: int = 0,
+                     dtype: int = BF16, ctx: Optional[Context] = None):
+    """(query rows of a workgroup, parts) of the pass over shared keys - (0, 0): none, the call is paged_attn's -, then of the rows' own, of a paged_attn_shared
+    call of these sizes."""
+    a = paged_shared_args()
+    a.n_rows, a.n_tokens, a.max_new, a.max_prefix_len, a.window, a.parent = n_rows, n_tokens, max_new, max_prefix_len, window, 1 if tree else None
+    a.dtype, a.n_heads, a.n_kv_heads, a.head_dim, a.n_groups, a.max_shared_len = dtype, n_heads, n_kv_heads, head_dim, n_groups, max_shared_len
+    out = [_i32() for _ in range(4)]
+    _check(load_library().cascade_paged_shared(ctx.handle if ctx else None, C.byref(a), *map(C.byref, out)))
+    return tuple(x.value for x in out)
+
+
+def paged_mass(ctx: Context, *, q_off, seq_len, block_table, q, lse, k_pages, mass, source=None, first=None, scale: float = 0.0, window: int = 0, n_sink: int = 0,
+               max_new: int, max_seq_len: int) -> None:
+    """q [N,Hq,D] (tokens any stride apart) and lse [N,Hq] of an attention call; q_off [S+1], seq_len [S] and source [tokens] as paged_slots wrote them (source None:
+    the tokens themselves); k_pages [pages,Hkv,page_size,D] in any order of memory (last dim contiguous), block_table [S,width]; first [S]; mass [S,Hkv,positions]
+    float32 (last dim contiguous), updated in place."""
+    n, heads, D = q.shape
+    q_stride, q_head, q_one = q.stride()
+    if n <= 1:   # a dimension of one element has any stride
+        q_stride = heads * D
+    if heads == 1:
+        q_head = D
+    pages, kv_heads, page_size, pool_D = k_pages.shape
+    page_stride, head_stride, pos_stride, one = k_pages.stride()
+    table_stride, table_one = block_table.stride()
+    rows, mass_heads, cap = mass.shape
+    mass_row, mass_head, mass_one = mass.stride()
+    assert (q_head == D == pool_D and q_one == 1 == one == table_one and q.dtype is k_pages.dtype and lse.shape == (n, heads) and lse.is_contiguous()
+            and (mass_one == 1 or cap <= 1) and rows == seq_len.numel() and mass_heads == kv_heads and mass.dtype is lse.dtype is torch.float32)
+    _check(ctx.lib.paged_mass_record(ctx.handle, _MASS(
+        _dtype_code(q), rows, q_off.data_ptr(), seq_len.data_ptr(), 0 if source is None else source.data_ptr(), 0 if first is None else first.data_ptr(),
+        n if source is None else source.numel(), n, max_new, max_seq_len, heads, kv_heads, D, scale, window, n_sink, q.data_ptr(), q_stride, lse.data_ptr(),
+        k_pages.data_ptr(), page_stride, head_stride, pos_stride, pages, page_size, block_table.data_ptr(), table_stride, block_table.shape[1], cap,
+        mass.data_ptr(), mass_row, mass_head)))
+
+
+def _paged_evict_record(seq_len, budget, block_table, k_pages, v_pages, mass, mass_out, free_pages, free_count, seq_len_out, free_count_out, n_first, n_recent,
+                        dropped, max_seq_len, workspace) -> bytes:
+    layers, pages, kv_heads, page_size, D = shape = k_pages.shape
+    stride = k_pages.stride()
+    m_layers, rows, m_heads, cap = mass.shape
+    m_stride = mass.stride()
+    table_stride, table_one = block_table.stride()
+    assert (v_pages.shape == shape and v_pages.stride() == stride and stride[4] == 1 == table_one and k_pages.dtype is v_pages.dtype and m_layers == layers
+            and m_heads == kv_heads and rows == seq_len.numel() == budget.numel() and mass_out.shape == mass.shape and mass_out.stride() == m_stride
+            and (m_stride[3] == 1 or cap <= 1) and mass.dtype is mass_out.dtype is torch.float32)
+    at = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
+    return _EVICT(_dtype_code(k_pages), layers, rows, kv_heads, D, seq_len.data_ptr(), budget.data_ptr(), at(n_first), n_recent, max_seq_len, mass.data_ptr(),
+                  mass_out.data_ptr(), *m_stride[:3], cap, pages, page_size, block_table.shape[1], k_pages.data_ptr(), v_pages.data_ptr(), *stride[:4],
+                  block_table.data_ptr(), table_stride, free_pages.numel(), free_pages.data_ptr(), free_count.data_ptr(), free_count_out.data_ptr(),
+                  seq_len_out.data_ptr(), at(dropped), *((0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())))
+
+
+def paged_evict(ctx: Context, *, seq_len, budget, block_table, k_pages, v_pages, mass, mass_out, free_pages, free_count, seq_len_out, free_count_out, n_first=None,
+                n_recent: int = 0, dropped=None, max_seq_len: int, workspace: torch.Tensor) -> None:
+    """k_pages/v_pages [L,pages,Hkv,page_size,D] as for paged_append, positions moved in place; mass/mass_out [L,S,Hkv,positions] float32 (last dim contiguous);
+    seq_len/budget/n_first/seq_len_out/dropped [S] int32; block_table [S,width]; free_pages [any], free_count/free_count_out [1].  workspace:
+    paged_evict_workspace bytes."""
+    _check(ctx.lib.paged_evict_record(ctx.handle, _paged_evict_record(seq_len, budget, block_table, k_pages, v_pages, mass, mass_out, free_pages, free_count,
+                                                                      seq_len_out, free_count_out, n_first, n_recent, dropped, max_seq_len, workspace)))
+
+
+def paged_evict_workspace(ctx: Context, *, seq_len, budget, block_table, k_pages, v_pages, mass, mass_out, free_pages, free_count, seq_len_out, free_count_out,
+                          n_first=None, n_recent: int = 0, dropped=None, max_seq_len: int) -> int:
+    """Bytes of scratch that a paged_evict call with these arguments needs."""
+    a = paged_evict_args.from_buffer_copy(_paged_evict_record(seq_len, budget, block_table, k_pages, v_pages, mass, mass_out, free_pages, free_count, seq_len_out,
+                                                              free_count_out, n_first, n_recent, dropped, max_seq_len, None))
+    n = _i64()
+    _check(ctx.lib.paged_evict_workspace(ctx.handle, C.byref(a), C.byref(n)))
+    return n.value
 
 
 def sample_tokens(ctx: Context, *, logits, u, token, prob=None, temperature=None, top_k=None, top_p=None, min_p=None) -> None:

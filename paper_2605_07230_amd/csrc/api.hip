@@ -542,14 +542,146 @@ int paged_attn_workspace(const cascade_ctx* ctx, const paged_attn_args* a, int64
   return CASCADE_OK;
 }
 
+// sizes that a question about a cut may have
+static bool valid_for_cut(const paged_attn_args* a) {
+  return a->n_rows > 0 && a->n_tokens > 0 && a->max_new > 0 && a->max_new <= (1 << 30) && a->max_prefix_len >= 0 && a->max_prefix_len <= (1 << 30) && a->window >= 0 &&
+         a->n_sink >= 0 && a->n_kv_heads > 0 && a->n_heads >= a->n_kv_heads && a->head_dim > 0 && a->head_dim <= 256 &&
+         (a->dtype != CASCADE_BF16 || a->head_dim == 64 || a->head_dim == 128);
+}
+
 int cascade_paged_cut(const cascade_ctx* ctx, const paged_attn_args* a, int32_t* query_rows, int32_t* key_parts, int32_t* waves) {
   if (!a || !query_rows || !key_parts || !waves) return CASCADE_EINVAL;
   if (a->dtype != CASCADE_F32 && a->dtype != CASCADE_BF16) return CASCADE_EDTYPE;
-  if (a->n_rows <= 0 || a->n_tokens <= 0 || a->max_new <= 0 || a->max_new > (1 << 30) || a->max_prefix_len < 0 || a->max_prefix_len > (1 << 30) || a->window < 0 ||
-      a->n_sink < 0 || a->n_kv_heads <= 0 ||
-      a->n_heads < a->n_kv_heads || a->head_dim <= 0 || a->head_dim > 256 || (a->dtype == CASCADE_BF16 && a->head_dim != 64 && a->head_dim != 128))
-    return CASCADE_EINVAL;
+  if (!valid_for_cut(a)) return CASCADE_EINVAL;
   plan_paged_cut(a, ctx ? ctx->n_cu : 256, ctx ? ctx->attn_ws_bytes : (size_t)1 << 40, query_rows, key_parts, waves);
+  return CASCADE_OK;
+}
+
+static int check_paged_shared(const cascade_ctx* ctx, const paged_shared_args* a) {
+  const int st = check_paged_attn(ctx, &a->attn);
+  if (st != CASCADE_OK) return st;
+  if (a->n_groups < 0 || a->max_shared_len < 0 || (a->n_groups > 0 && a->attn.n_rows > 0 && (!a->group_off || !a->shared_len))) return CASCADE_EINVAL;
+  return a->max_shared_len > a->attn.max_prefix_len ? CASCADE_ESHAPE : CASCADE_OK;
+}
+
+int paged_attn_shared(cascade_ctx* ctx, const paged_shared_args* a) {
+  if (!ctx || !a) return CASCADE_EINVAL;
+  const int st = check_paged_shared(ctx, a);
+  if (st != CASCADE_OK) return st;
+  if (a->attn.n_rows == 0 || a->attn.n_tokens == 0) return CASCADE_OK;
+  if (a->attn.max_new == 0) return CASCADE_ESHAPE;   // (as paged_attn)
+  return on_device(ctx, [&] { return launch_paged_shared(ctx, a); });
+}
+
+int paged_attn_shared_workspace(const cascade_ctx* ctx, const paged_shared_args* a, int64_t* bytes) {
+  if (!ctx || !a || !bytes) return CASCADE_EINVAL;
+  const int st = check_paged_shared(ctx, a);
+  if (st != CASCADE_OK) return st;
+  *bytes = 0;
+  if (a->attn.n_rows == 0 || a->attn.n_tokens == 0 || a->attn.max_new == 0) return CASCADE_OK;
+  *bytes = plan_paged_shared(ctx, a);
+  return CASCADE_OK;
+}
+
+int cascade_paged_shared(const cascade_ctx* ctx, const paged_shared_args* a, int32_t* shared_rows, int32_t* shared_parts, int32_t* own_rows, int32_t* own_parts) {
+  if (!a || !shared_rows || !shared_parts || !own_rows || !own_parts) return CASCADE_EINVAL;
+  if (a->attn.dtype != CASCADE_F32 && a->attn.dtype != CASCADE_BF16) return CASCADE_EDTYPE;
+  if (!valid_for_cut(&a->attn) || a->n_groups < 0 || a->max_shared_len < 0) return CASCADE_EINVAL;
+  plan_shared_cut(a, ctx ? ctx->n_cu : 256, ctx ? ctx->attn_ws_bytes : (size_t)1 << 40, shared_rows, shared_parts, own_rows, own_parts);
+  return CASCADE_OK;
+}
+
+static int check_paged_mass(const cascade_ctx* ctx, const paged_mass_args* a) {
+  const bool some = a->n_rows != 0 && a->n_tokens != 0;
+  if (some && (!a->q_off || !a->seq_len || !a->q || !a->lse || !a->k_pages || !a->block_table || !a->mass || a->n_pages == 0)) return CASCADE_EINVAL;
+  if (a->n_rows < 0 || a->n_tokens < 0 || a->n_source < 0 || a->max_new < 0 || a->max_seq_len < 0 || a->window < 0 || a->n_sink < 0 || a->mass_cap < 0)
+    return CASCADE_EINVAL;
+  if ((!a->source && a->n_source < a->n_tokens) || (some && a->n_source == 0)) return CASCADE_EINVAL;
+  if (a->dtype != CASCADE_F32 && a->dtype != CASCADE_BF16) return CASCADE_EDTYPE;
+  if (a->n_heads <= 0 || a->n_kv_heads <= 0 || a->head_dim <= 0 || bad_float(a->scale) || a->scale < 0.f) return CASCADE_EINVAL;
+  if (a->n_heads % a->n_kv_heads != 0) return CASCADE_ESHAPE;
+  const int st = check_pages(a->n_pages, a->page_size);
+  if (st != CASCADE_OK) return st;
+  if (a->table_width < 0 || a->table_stride < a->table_width) return CASCADE_EINVAL;
+  if (a->stride_page < 0 || a->stride_head < 0 || a->stride_pos < 0 || a->q_stride < (int64_t)a->n_heads * a->head_dim) return CASCADE_ESHAPE;
+  // (rows and heads of sums that lie on each other would be a race)
+  if (a->mass_stride_head < 0 || a->mass_stride_row < 0 || (a->n_kv_heads > 1 && a->mass_stride_head < a->mass_cap) ||
+      (a->n_rows > 1 && a->mass_stride_row < a->mass_cap))
+    return CASCADE_ESHAPE;
+  const cascade_limits& L = ctx->lim;
+  if (a->n_rows > L.max_rows || a->n_tokens > L.max_nodes_total || a->n_source > L.max_nodes_total || a->max_seq_len > L.max_prefix || a->n_heads > L.n_heads ||
+      a->head_dim > L.head_dim)
+    return CASCADE_ESHAPE;
+  // query rows of a row and what a launch counts stay below 2^30 (256 threads to 64 keys at least)
+  if (a->max_seq_len > (1 << 30) || (int64_t)a->max_new * (a->n_heads / a->n_kv_heads) > (1 << 30) || (int64_t)a->n_tokens * a->n_heads > (1 << 30) ||
+      (double)a->n_rows * a->n_kv_heads * ((a->max_seq_len + 63) / 64) > (double)(1 << 23))
+    return CASCADE_ESHAPE;
+  if (a->dtype == CASCADE_BF16) {
+    if (a->head_dim != 64 && a->head_dim != 128) return CASCADE_ESHAPE;
+    if ((a->stride_page | a->stride_head | a->stride_pos | a->q_stride) % 8) return CASCADE_ESHAPE;
+    if (((uintptr_t)a->q | (uintptr_t)a->k_pages) & 15) return CASCADE_EINVAL;
+  } else if (a->head_dim > 256) {
+    return CASCADE_ESHAPE;
+  }
+  return CASCADE_OK;
+}
+
+int paged_mass(cascade_ctx* ctx, const paged_mass_args* a) {
+  if (!ctx || !a) return CASCADE_EINVAL;
+  const int st = check_paged_mass(ctx, a);
+  if (st != CASCADE_OK) return st;
+  if (a->n_rows == 0 || a->n_tokens == 0) return CASCADE_OK;
+  if (a->max_new == 0 || a->max_seq_len == 0) return CASCADE_ESHAPE;   // tokens without a bound, or a cache, that holds them
+  return on_device(ctx, [&] { return launch_paged_mass(ctx, a); });
+}
+
+static int check_paged_evict(const cascade_ctx* ctx, const paged_evict_args* a) {
+  const bool some = a->n_rows != 0 && a->n_layers != 0;
+  if (some && (!a->seq_len || !a->budget || !a->seq_len_out || !a->free_count || !a->free_count_out)) return CASCADE_EINVAL;
+  if (some && a->max_seq_len > 0 && (!a->mass || !a->mass_out || !a->k_pages || !a->v_pages || !a->block_table || a->n_pages == 0)) return CASCADE_EINVAL;
+  if (some && a->free_capacity > 0 && !a->free_pages) return CASCADE_EINVAL;
+  if (some && (a->seq_len == a->seq_len_out || a->free_count == a->free_count_out || (a->mass && a->mass == a->mass_out))) return CASCADE_EINVAL;
+  if (a->dtype != CASCADE_F32 && a->dtype != CASCADE_BF16) return CASCADE_EDTYPE;
+  if (a->n_layers < 0 || a->n_rows < 0 || a->n_kv_heads <= 0 || a->head_dim <= 0 || a->n_recent < 0 || a->max_seq_len < 0 || a->mass_cap < 0 || a->free_capacity < 0 ||
+      a->workspace_bytes < 0)
+    return CASCADE_EINVAL;
+  const int st = check_pages(a->n_pages, a->page_size);
+  if (st != CASCADE_OK) return st;
+  if (a->table_width < 0 || a->table_stride < a->table_width) return CASCADE_EINVAL;
+  const int64_t e = a->dtype == CASCADE_BF16 ? 2 : 4;
+  const int64_t strides[4] = {a->stride_layer, a->stride_page, a->stride_head, a->stride_pos};
+  for (int i = 0; i < 4; ++i)
+    if (strides[i] < 0 || (strides[i] * e) % 16) return CASCADE_ESHAPE;
+  if ((a->head_dim * e) % 16) return CASCADE_ESHAPE;
+  if (((uintptr_t)a->k_pages | (uintptr_t)a->v_pages | (uintptr_t)a->workspace) & 15) return CASCADE_EINVAL;
+  // (weights that lie on each other would be a race)
+  if (a->mass_stride_head < 0 || a->mass_stride_row < 0 || a->mass_stride_layer < 0 || (a->n_kv_heads > 1 && a->mass_stride_head < a->mass_cap) ||
+      (a->n_rows > 1 && a->mass_stride_row < a->mass_cap) || (a->n_layers > 1 && a->mass_stride_layer < a->mass_cap))
+    return CASCADE_ESHAPE;
+  const cascade_limits& L = ctx->lim;
+  if (a->n_rows > L.max_rows || a->max_seq_len > L.max_prefix) return CASCADE_ESHAPE;
+  // what the launches count, and the pages that may go back
+  if (a->max_seq_len > (1 << 30) || (int64_t)a->table_width * a->page_size > 0x7fffffff || (int64_t)a->n_rows * (a->max_seq_len / a->page_size + 1) > 0x3fffffff ||
+      a->free_capacity > (1 << 30) || (double)a->n_layers * a->n_rows * a->n_kv_heads * ((a->head_dim * e + 127) / 128) > (double)(1 << 21))
+    return CASCADE_ESHAPE;
+  return CASCADE_OK;
+}
+
+int paged_evict(cascade_ctx* ctx, const paged_evict_args* a) {
+  if (!ctx || !a) return CASCADE_EINVAL;
+  const int st = check_paged_evict(ctx, a);
+  if (st != CASCADE_OK) return st;
+  if (a->n_rows == 0 || a->n_layers == 0) return CASCADE_OK;
+  if (!a->workspace) return CASCADE_EINVAL;
+  if (a->workspace_bytes < plan_paged_evict(a)) return CASCADE_ESHAPE;
+  return on_device(ctx, [&] { return launch_paged_evict(ctx, a); });
+}
+
+int paged_evict_workspace(const cascade_ctx* ctx, const paged_evict_args* a, int64_t* bytes) {
+  if (!ctx || !a || !bytes) return CASCADE_EINVAL;
+  const int st = check_paged_evict(ctx, a);
+  if (st != CASCADE_OK) return st;
+  *bytes = a->n_rows == 0 || a->n_layers == 0 ? 0 : plan_paged_evict(a);
   return CASCADE_OK;
 }
 

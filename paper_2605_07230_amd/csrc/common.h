@@ -99,6 +99,12 @@ hipError_t launch_paged_append(cascade_ctx* ctx, const paged_append_args* a);
 hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a);
 int64_t plan_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a);   // bytes of partial results that the call's cut leaves
 void plan_paged_cut(const paged_attn_args* a, int n_cu, size_t ws_bytes, int32_t* query_rows, int32_t* key_parts, int32_t* waves);
+hipError_t launch_paged_shared(cascade_ctx* ctx, const paged_shared_args* a);
+int64_t plan_paged_shared(const cascade_ctx* ctx, const paged_shared_args* a);   // (as plan_paged_attn)
+void plan_shared_cut(const paged_shared_args* a, int n_cu, size_t ws_bytes, int32_t* shared_rows, int32_t* shared_parts, int32_t* own_rows, int32_t* own_parts);
+hipError_t launch_paged_mass(cascade_ctx* ctx, const paged_mass_args* a);
+hipError_t launch_paged_evict(cascade_ctx* ctx, const paged_evict_args* a);
+int64_t plan_paged_evict(const paged_evict_args* a);   // bytes of the lists of moves
 hipError_t launch_sample(cascade_ctx* ctx, const sample_args* a);
 
 // ----------------------------------------------------------------------------------------------

@@ -48,7 +48,14 @@ struct PagedParams {
   bool in_order;         // (other kernels) rows of the batch are taken in order, not longest first
   float* ws_o;           // [parts][n_tokens * n_heads][head_dim]
   float* ws_ml;          // [parts][n_tokens * n_heads][2]
+  // paged_attn_shared: groups of rows; the parts of the pass over their shared keys come first, those of the rows' own behind them
+  const int32_t *group_off, *shared_len;
+  int n_groups, most_shared;   // (the bound on shared_len)
+  int part0;             // the first part that this pass writes
 };
+
+// What a kernel goes through: a whole call's keys; the keys that the rows of a group share, for all of the group's tokens; what is left of each row's keys.
+enum Pass { ALONE, SHARED, OWN };
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
@@ -91,7 +98,7 @@ struct Tiles {
   __device__ __forceinline__ int new_tile(int t) const { return t < sinks_n ? t : t + skip_n; }
 };
 template <int TS = KT>   // keys per tile
-__device__ __forceinline__ Tiles tiles_of(const PagedParams& p, int P, int i0, int i1, bool tree) {
+__device__ __forceinline__ Tiles tiles_of(const PagedParams& p, int P, int i0, int i1, bool tree, int shared = 0) {   // shared: tiles of KT that another pass takes
   const int W = p.a.window, n_pt = (P + TS - 1) / TS, n_nt = i1 / TS + 1;
   Tiles t = {n_pt, 0, 0, n_nt, 0, 0, 0};
   if (W > 0) {
@@ -107,7 +114,63 @@ __device__ __forceinline__ Tiles tiles_of(const PagedParams& p, int P, int i0, i
       t.n_n = n_nt - t.skip_n;
     }
   }
+  if (shared) {   // (no window, then)
+    t.skip_p = shared * (KT / TS);
+    t.n_p = n_pt - t.skip_p;
+  }
   return t;
+}
+
+// ---- groups of rows that share their first keys
+// What the rows of each group share, in tiles: worked out by every workgroup from the lengths, since a row that cannot be computed, or that is shorter than what its group
+// shares, changes it for all of its rows.  A thread to a group, then to a row; rows find their group by bisection.  In LDS: the groups' offsets and their tiles.
+constexpr int MOST_GROUPS = 512;   // calls with more rows share nothing
+struct Groups {
+  int off[MOST_GROUPS + 1];
+  int tiles[MOST_GROUPS];
+};
+__device__ __forceinline__ int group_of_row(const Groups& gr, int n_groups, int s) {
+  int lo = 0, hi = n_groups - 1;   // the last group that begins at or before the row (empty ones lie in front of it)
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (gr.off[mid] <= s) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+__device__ __forceinline__ void find_groups(const PagedParams& p, Groups& gr, int tid, int threads) {
+  const paged_attn_args& a = p.a;
+  bool bad = false;
+  for (int g = tid; g <= p.n_groups; g += threads) {
+    const int at = p.group_off[g];
+    gr.off[g] = at;
+    if (g < p.n_groups) {
+      const int next = p.group_off[g + 1];
+      bad |= at > next || (g == 0 && at != 0);
+      gr.tiles[g] = (unsigned)at < (unsigned)next && next - at > 1 ? min(max(p.shared_len[g], 0), p.most_shared) / KT : 0;
+    } else {
+      bad |= at != a.n_rows;
+    }
+  }
+  if (__syncthreads_or(bad)) {   // nobody shares anything
+    for (int g = tid; g < p.n_groups; g += threads) gr.tiles[g] = 0;
+    if (tid == 0 && blockIdx.x == 0) atomicOr(p.dev_status, CASCADE_FLAG_TREE_SIZE);
+  } else {
+    for (int s = tid; s < a.n_rows; s += threads) {
+      const RowInfo r = check_row(p, s, a.q_off[s], a.q_off[s + 1], a.prefix_len[s]);
+      atomicMin(&gr.tiles[group_of_row(gr, p.n_groups, s)], r.flag ? 0 : r.P / KT);
+    }
+  }
+  __syncthreads();
+}
+// the parts of the other pass, for a row that shares nothing
+__device__ __forceinline__ void write_no_shared(const PagedParams& p, int lo, int T, int kvh, int row0, int row1, int tid, int threads) {
+  const int G = p.group;
+  for (int i = row0 * p.part0 + tid; i < row1 * p.part0; i += threads) {
+    const int r = i / p.part0, part = i - r * p.part0;
+    float* ml = p.ws_ml + ((long long)part * p.a.n_tokens * p.a.n_heads + (long long)(lo + r / G) * p.a.n_heads + kvh * G + r % G) * 2;
+    ml[0] = -INFINITY;
+    ml[1] = 0.f;
+  }
 }
 
 // keys kb .. kb + 63 of the pages that a token at position x sees; of a chain's new tokens, that token i sees
@@ -154,14 +217,15 @@ __device__ __forceinline__ uint32_t finite_only(uint32_t x) {
 }
 
 // zeros for the tokens of a row that cannot be computed, query heads of one kv head; empty parts where there are several
-template <typename T>
+template <typename T, int PASS>
 __device__ __forceinline__ void write_nothing(const PagedParams& p, const RowInfo& r, int kvh, int part, int tid, int threads) {
   const int D = p.a.head_dim, G = p.group;
+  if (PASS == OWN && part == 0) write_no_shared(p, r.lo, r.T, kvh, 0, r.T * G, tid, threads);
   if (tid == 0 && part == 0) atomicOr(p.dev_status, r.flag);
   for (int i = tid; i < r.T * G; i += threads) {
     const long long row = (long long)(r.lo + i / G) * p.a.n_heads + kvh * G + i % G;
-    if (p.parts > 1) {
-      float* ml = p.ws_ml + ((long long)part * p.a.n_tokens * p.a.n_heads + row) * 2;
+    if (PASS != ALONE || p.parts > 1) {
+      float* ml = p.ws_ml + ((long long)(part + (PASS ? p.part0 : 0)) * p.a.n_tokens * p.a.n_heads + row) * 2;
       ml[0] = -INFINITY;
       ml[1] = 0.f;
     } else if (part == 0) {
@@ -183,32 +247,38 @@ __device__ __forceinline__ void write_nothing(const PagedParams& p, const RowInf
 // Waves per SIMD: two, at head_dim 64, whose tiles are half as large, three of four-wave workgroups (64 rows of 90 to 4200 keys 70 -> 67 us, of 300 to 600 with 16 heads 28.3 -> 26.9).
 template <int D, int NW>
 constexpr int few_per_unit() { return D == 64 && NW == 4 ? 3 : 8 / NW; }
-template <int D, int NW, bool TREE>
+template <int D, int NW, bool TREE, int PASS>
 __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_kernel(PagedParams p) {
+  static_assert(PASS != SHARED, "the tokens of a group come in any number");
   constexpr int NT = 64 * NW, KS = D / 32, DB = D / 16, DC = D / 8, VP = D + 16, OP = D + 4, NVC = KT * DC / 64, R = 16;
   extern __shared__ __align__(16) char few_smem[];
   const paged_attn_args& a = p.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4, G = p.group;
   uint16_t* vt = (uint16_t*)few_smem + (size_t)wave * KT * VP;
+  __shared__ typename std::conditional<PASS == OWN, Groups, int>::type groups;
+  if constexpr (PASS == OWN) find_groups(p, groups, tid, NT);
 
   for (int item = blockIdx.x;; item += gridDim.x) {
     const int kvh = item % a.n_kv_heads;
     int part = item / a.n_kv_heads;
     // which row this part belongs to
     RowInfo r = {-1, 0, 0, 0, 0};
-    int n_parts = 0;
+    int n_parts = 0, part_tiles = p.part_tiles, shared = 0;
     for (int base = 0; base < a.n_rows && r.s < 0; base += 64) {
       const int at = base + lane;
       RowInfo mine = {at, 0, 0, 0, 0};
-      int n = 0;
+      int n = 0, mine_shared = 0, mine_tiles = p.part_tiles;
       if (at < a.n_rows) {
         mine = check_row(p, at, a.q_off[at], a.q_off[at + 1], a.prefix_len[at]);
         if (mine.flag) {
           n = 1;   // (reported even if it holds no token)
         } else if (mine.T > 0) {
-          const Tiles ti = tiles_of(p, mine.P, 0, mine.T - 1, TREE);
-          n = (ti.n_p + ti.n_n + p.part_tiles - 1) / p.part_tiles;
+          if constexpr (PASS == OWN) mine_shared = groups.tiles[group_of_row(groups, p.n_groups, at)];
+          const Tiles ti = tiles_of(p, mine.P, 0, mine.T - 1, TREE, mine_shared);
+          // (the launch knows how long rows are, not how much of them is shared: never more parts than there is room for)
+          if (PASS == OWN) mine_tiles = max(p.part_tiles, (ti.n_p + ti.n_n + p.parts - 1) / p.parts);
+          n = (ti.n_p + ti.n_n + mine_tiles - 1) / mine_tiles;
         }
       }
       const int incl = wave_scan_incl_i(n);
@@ -221,6 +291,10 @@ __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_ke
         r.P = __builtin_amdgcn_readlane(mine.P, l);
         r.flag = __builtin_amdgcn_readlane(mine.flag, l);
         n_parts = __builtin_amdgcn_readlane(n, l);
+        if (PASS == OWN) {
+          part_tiles = __builtin_amdgcn_readlane(mine_tiles, l);
+          shared = __builtin_amdgcn_readlane(mine_shared, l);
+        }
         part -= __builtin_amdgcn_readlane(incl - n, l);
       } else {
         part -= __builtin_amdgcn_readlane(incl, 63);
@@ -228,16 +302,17 @@ __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_ke
     }
     if (r.s < 0) return;
     if (r.flag) {
-      for (int q = 0; q < p.parts; ++q) write_nothing<uint16_t>(p, r, kvh, q, tid, NT);
+      for (int q = 0; q < p.parts; ++q) write_nothing<uint16_t, PASS>(p, r, kvh, q, tid, NT);
       continue;
     }
     const int lo = r.lo, T = r.T, P = r.P, M = T * G;
-    const Tiles ti = tiles_of(p, P, 0, T - 1, TREE);
-    const int nt = ti.n_p + ti.n_n, t_begin = part * p.part_tiles, t_end = min(nt, t_begin + p.part_tiles);
+    const Tiles ti = tiles_of(p, P, 0, T - 1, TREE, shared);
+    const int nt = ti.n_p + ti.n_n, t_begin = part * part_tiles, t_end = min(nt, t_begin + part_tiles), part0 = PASS == OWN ? p.part0 : 0;
+    if (PASS == OWN && part == 0 && shared == 0) write_no_shared(p, lo, T, kvh, 0, M, tid, NT);
     if (part == 0 && p.parts > n_parts)   // parts that this row has not
       for (int i = tid; i < M * (p.parts - n_parts); i += NT) {
         const int q = i % M;
-        float* ml = p.ws_ml + ((long long)(n_parts + i / M) * a.n_tokens * a.n_heads + (long long)(lo + q / G) * a.n_heads + kvh * G + q % G) * 2;
+        float* ml = p.ws_ml + ((long long)(part0 + n_parts + i / M) * a.n_tokens * a.n_heads + (long long)(lo + q / G) * a.n_heads + kvh * G + q % G) * 2;
         ml[0] = -INFINITY;
         ml[1] = 0.f;
       }
@@ -480,8 +555,8 @@ __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_ke
       }
       const int tok = token_of(p, row);
       const long long at = (long long)(lo + tok) * a.n_heads + kvh * G + row - tok * G;
-      if (p.parts > 1) {
-        const long long w = (long long)part * a.n_tokens * a.n_heads + at;
+      if (PASS != ALONE || p.parts > 1) {
+        const long long w = (long long)(part0 + part) * a.n_tokens * a.n_heads + at;
         *(f32x4*)(p.ws_o + w * D + d) = o;
         if (d == 0) { p.ws_ml[w * 2] = m; p.ws_ml[w * 2 + 1] = l; }
       } else {
@@ -590,7 +665,33 @@ __device__ __forceinline__ RowInfo block_row(const PagedParams& p, int blk, int 
   return none;
 }
 
-template <int D, int NS, int NQ, int NW, bool TREE>
+// Block `blk` of the pass over shared keys: a run of the query rows of a group, which stands for a row of the batch with all its tokens; its keys lie where the group's first row has them.
+__device__ __forceinline__ RowInfo block_group(const PagedParams& p, const Groups& groups, int blk, int rows_per_block, int lane, int* sb) {
+  RowInfo none = {-1, 0, 0, 0, 0};
+  for (int base = 0; base < p.n_groups; base += 64) {
+    const int at = base + lane;
+    RowInfo mine = none;
+    int nb = 0;
+    if (at < p.n_groups && groups.tiles[at] > 0) {   // then all of its rows are in order
+      mine.s = groups.off[at];
+      mine.lo = p.a.q_off[mine.s];
+      mine.T = p.a.q_off[groups.off[at + 1]] - mine.lo;
+      mine.P = KT * groups.tiles[at];
+      nb = (int)(((long long)mine.T * p.group + rows_per_block - 1) / rows_per_block);
+    }
+    const int incl = wave_scan_incl_i(nb);
+    const u64 who = __ballot(blk < incl);
+    if (who) {
+      const int l = __ffsll((long long)who) - 1;
+      *sb = blk - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(nb, l));
+      return RowInfo{__builtin_amdgcn_readlane(mine.s, l), __builtin_amdgcn_readlane(mine.lo, l), __builtin_amdgcn_readlane(mine.T, l), __builtin_amdgcn_readlane(mine.P, l), 0};
+    }
+    blk -= __builtin_amdgcn_readlane(incl, 63);
+  }
+  return none;
+}
+
+template <int D, int NS, int NQ, int NW, bool TREE, int PASS>
 __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3) : 2)) void paged_ring_kernel(PagedParams p) {
   using GM = RingGeom<D>;
   constexpr int NT = 64 * NW, RW = 16 * NQ * NW, KS = D / 32, DB = D / 16;
@@ -616,19 +717,35 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
     else { kvh = h % H; b = h / H; }
   }
   const int part = b % p.parts;
-  int sb = 0;
-  const RowInfo ri = block_row(p, b / p.parts, RW, lane, &sb);
+  int sb = 0, shared = 0;
+  RowInfo ri;
+  if constexpr (PASS == ALONE) {
+    ri = block_row(p, b / p.parts, RW, lane, &sb);
+  } else {   // (the groups stand where tiles are loaded later)
+    Groups& groups = *(Groups*)ring_smem;
+    find_groups(p, groups, tid, NT);
+    if (PASS == SHARED) {
+      ri = block_group(p, groups, b / p.parts, RW, lane, &sb);
+    } else {
+      ri = block_row(p, b / p.parts, RW, lane, &sb);
+      if (ri.s >= 0 && !ri.flag) shared = groups.tiles[group_of_row(groups, p.n_groups, ri.s)];
+    }
+    __syncthreads();
+  }
   if (ri.s < 0) return;   // the grid is an upper bound of the number of blocks
-  if (ri.flag) { write_nothing<uint16_t>(p, ri, kvh, part, tid, NT); return; }
+  if (ri.flag) { write_nothing<uint16_t, PASS>(p, ri, kvh, part, tid, NT); return; }
   auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
   const int lo = uniform(ri.lo), T = uniform(ri.T), P = uniform(ri.P), M = T * G, row0 = uniform(sb) * RW;
   const int i0 = uniform(token_of(p, row0)), i1 = uniform(token_of(p, min(row0 + RW, M) - 1));
-  const Tiles ti = tiles_of(p, P, i0, i1, TREE);
+  Tiles ti = tiles_of(p, P, i0, i1, TREE, PASS == OWN ? uniform(shared) : 0);
+  if (PASS == SHARED) ti.n_n = 0;
   const int nt = ti.n_p + ti.n_n, per = (nt + p.parts - 1) / p.parts, t_begin = part * per, t_end = min(nt, t_begin + per);
   const long long all_rows = (long long)a.n_tokens * a.n_heads;
+  const int part0 = PASS == ALONE ? 0 : p.part0;
+  if (PASS == OWN && part == 0 && shared == 0) write_no_shared(p, lo, T, kvh, row0, min(row0 + RW, M), tid, NT);
   if (t_begin >= t_end) {   // fewer tiles than parts: an empty one
     for (int r = row0 + tid; r < min(row0 + RW, M); r += NT) {
-      float* ml = p.ws_ml + (part * all_rows + (long long)(lo + r / G) * a.n_heads + kvh * G + r % G) * 2;
+      float* ml = p.ws_ml + ((part0 + part) * all_rows + (long long)(lo + r / G) * a.n_heads + kvh * G + r % G) * 2;
       ml[0] = -INFINITY;
       ml[1] = 0.f;
     }
@@ -999,8 +1116,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
   for (int n = 0; n < NQ; ++n) {
     const float l = rows4_sum(lsum[n]);
     if (qi[n] < 0) continue;
-    if (p.parts > 1) {
-      const long long w = part * all_rows + out_row[n];
+    if (PASS != ALONE || p.parts > 1) {
+      const long long w = (part0 + part) * all_rows + out_row[n];
 #pragma unroll
       for (int db = 0; db < DB; ++db) *(f32x4*)(p.ws_o + w * D + 16 * db + 4 * g) = ot[n][db];
       if (g == 0) { p.ws_ml[w * 2] = m_ref[n]; p.ws_ml[w * 2 + 1] = l; }
@@ -1029,7 +1146,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
 // Nothing passes through LDS before the waves meet.  Bound by the trips to memory, one after the other: the row's place, the table's entry, the first tile.
 // 15 new tokens x 8 heads x 64 behind 256 keys: 9 us.  Many rows fetch every key again for each 16 of them: 8 rows of 200 tokens behind 1289 keys, 8 heads: 94 us at head_dim 64 (49 TFLOP/s; 30 at the rate
 // of a large product), 161 at 128 (57 TFLOP/s).
-template <int DB, int NW, bool VEC, bool TREE>
+template <int DB, int NW, bool VEC, bool TREE, int PASS>
 __global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
   extern __shared__ __align__(16) float f32_smem[];   // [NW][16 queries][16 DB + 4] outputs, [NW][16][2] maxima and sums
   __shared__ int s_parent[TREE ? CASCADE_MAX_TREE : 1];
@@ -1038,12 +1155,27 @@ __global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4, G = p.group, D = a.head_dim;
   const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads, part = b % p.parts;
-  int sb = 0;
-  const RowInfo ri = block_row(p, b / p.parts, 16, lane, &sb);
+  int sb = 0, shared = 0;
+  RowInfo ri;
+  if constexpr (PASS == ALONE) {
+    ri = block_row(p, b / p.parts, 16, lane, &sb);
+  } else {
+    Groups& groups = *(Groups*)f32_smem;
+    find_groups(p, groups, tid, 64 * NW);
+    if (PASS == SHARED) {
+      ri = block_group(p, groups, b / p.parts, 16, lane, &sb);
+    } else {
+      ri = block_row(p, b / p.parts, 16, lane, &sb);
+      if (ri.s >= 0 && !ri.flag) shared = groups.tiles[group_of_row(groups, p.n_groups, ri.s)];
+    }
+    __syncthreads();
+  }
   if (ri.s < 0) return;   // the grid is an upper bound of the number of blocks
-  if (ri.flag) { write_nothing<float>(p, ri, kvh, part, tid, 64 * NW); return; }
+  if (ri.flag) { write_nothing<float, PASS>(p, ri, kvh, part, tid, 64 * NW); return; }
   const int lo = ri.lo, T = ri.T, P = ri.P, M = T * G, row0 = 16 * sb, rows = min(16, M - row0);
-  const Tiles ti = tiles_of<TS>(p, P, token_of(p, row0), token_of(p, row0 + rows - 1), TREE);
+  Tiles ti = tiles_of<TS>(p, P, token_of(p, row0), token_of(p, row0 + rows - 1), TREE, shared);
+  if (PASS == SHARED) ti.n_n = 0;
+  if (PASS == OWN && part == 0 && shared == 0) write_no_shared(p, lo, T, kvh, row0, row0 + rows, tid, 64 * NW);
   const int nt = ti.n_p + ti.n_n, per = (nt + p.parts - 1) / p.parts, t_begin = part * per, t_end = min(nt, t_begin + per);
   const int qr = row0 + min(l16, rows - 1);   // rows past the end repeat the last one, never stored
   const int qi = token_of(p, qr);
@@ -1221,15 +1353,17 @@ __global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
     const float ll = wave_sum(lane < NW ? f * lw : 0.f);
     const int tok = token_of(p, row);
     const long long at = (long long)(lo + tok) * a.n_heads + kvh * G + row - tok * G;
-    float* out = p.parts > 1 ? p.ws_o + (part * all_rows + at) * D : (float*)a.out + at * D;
+    const bool partial = PASS != ALONE || p.parts > 1;
+    const int slot = PASS == ALONE ? part : p.part0 + part;
+    float* out = partial ? p.ws_o + (slot * all_rows + at) * D : (float*)a.out + at * D;
     for (int d = lane; d < D; d += 64) {
       float o = 0.f;
 #pragma unroll
       for (int i = 0; i < NW; ++i) o = fmaf(__int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i)), f32_smem[(i * 16 + r) * OP + d], o);
-      out[d] = p.parts > 1 ? o : o / ll;
+      out[d] = partial ? o : o / ll;
     }
     if (lane == 0) {
-      if (p.parts > 1) { p.ws_ml[(part * all_rows + at) * 2] = mm; p.ws_ml[(part * all_rows + at) * 2 + 1] = ll; }
+      if (partial) { p.ws_ml[(slot * all_rows + at) * 2] = mm; p.ws_ml[(slot * all_rows + at) * 2 + 1] = ll; }
       else if (a.lse) a.lse[at] = mm * LN2 + logf(ll);
     }
   }
@@ -1394,10 +1528,10 @@ Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
 // eight waves to a part where every part has a compute unit of its own (trees, few of which are that small: one kernel)
 int few_waves(const paged_attn_args* a, const Cut& c, int n_cu) { return !a->parent && (int64_t)a->n_rows * a->n_kv_heads * c.parts <= n_cu ? 8 : 4; }
 
-template <int D, int NW, bool TREE>
+template <int D, int NW, bool TREE, int PASS>
 hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
   constexpr int v_bytes = NW * KT * (D + 16) * 2, o_bytes = NW * 16 * (D + 4 + 2) * 4, smem = v_bytes > o_bytes ? v_bytes : o_bytes;
-  constexpr auto kern = paged_few_kernel<D, NW, TREE>;
+  constexpr auto kern = paged_few_kernel<D, NW, TREE, PASS>;
   hipError_t e = allow_lds<kern>(smem, ctx->device);
   if (e != hipSuccess) return e;
   const int64_t items = (int64_t)p.a.n_rows * p.a.n_kv_heads * p.parts, slots = (int64_t)ctx->n_cu * few_per_unit<D, NW>();
@@ -1405,26 +1539,28 @@ hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
   CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)std::min(items, slots)), dim3(64 * NW), smem, ctx->stream, p);
   return hipGetLastError();
 }
-template <int D>
+template <int D, int PASS>
 hipError_t launch_few(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
-  if (p.a.parent) return launch_few_k<D, 4, true>(ctx, p);
-  return few_waves(&p.a, c, ctx->n_cu) == 8 ? launch_few_k<D, 8, false>(ctx, p) : launch_few_k<D, 4, false>(ctx, p);
+  if (p.a.parent) return launch_few_k<D, 4, true, PASS>(ctx, p);
+  return few_waves(&p.a, c, ctx->n_cu) == 8 ? launch_few_k<D, 8, false, PASS>(ctx, p) : launch_few_k<D, 4, false, PASS>(ctx, p);
 }
 
 // no more blocks of so many query rows than this, whatever the rows' lengths are; a row out of order is one
+template <int PASS>
 int64_t most_blocks(const PagedParams& p, int rows) {
+  if (PASS == SHARED) return ((int64_t)p.a.n_tokens * p.group / rows + p.n_groups) * p.parts;
   const int64_t each = ((int64_t)p.a.max_new * p.group + rows - 1) / rows;
   return std::min((int64_t)p.a.n_tokens * p.group / rows + p.a.n_rows, each * p.a.n_rows) * p.parts;
 }
 
-template <int D, int NS, int NQ, int NW, bool TREE>
+template <int D, int NS, int NQ, int NW, bool TREE, int PASS>
 hipError_t launch_ring_k(cascade_ctx* ctx, PagedParams& p) {
   constexpr int smem = ring_lds<D, NS, NQ, NW, TREE>();
-  constexpr auto kern = paged_ring_kernel<D, NS, NQ, NW, TREE>;
+  constexpr auto kern = paged_ring_kernel<D, NS, NQ, NW, TREE, PASS>;
   hipError_t e = allow_lds<kern>(smem, ctx->device);
   if (e != hipSuccess) return e;
   const paged_attn_args& a = p.a;
-  const int64_t blocks = most_blocks(p, 16 * NQ * NW);
+  const int64_t blocks = most_blocks<PASS>(p, 16 * NQ * NW);
   // (8 / n_kv_heads XCDs share a kv head: every one gets as many)
   const int64_t share = 8 % a.n_kv_heads == 0 ? 8 / a.n_kv_heads : 1;
   p.in_order = a.n_rows == 1 || a.n_rows > 64 || blocks * a.n_kv_heads <= ctx->n_cu;
@@ -1432,48 +1568,58 @@ hipError_t launch_ring_k(cascade_ctx* ctx, PagedParams& p) {
   CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)((blocks + share - 1) / share * share * a.n_kv_heads)), dim3(64 * NW), smem, ctx->stream, p);
   return hipGetLastError();
 }
-template <int D, bool TREE>
+template <int D, bool TREE, int PASS>
 hipError_t launch_ring(cascade_ctx* ctx, PagedParams& p, const Cut& c) {
-  if (c.shape == RING_64) return launch_ring_k<D, 2, 1, 4, TREE>(ctx, p);
+  if (c.shape == RING_64) return launch_ring_k<D, 2, 1, 4, TREE, PASS>(ctx, p);
   if constexpr (D == 64)
-    if (c.shape == RING_256) return launch_ring_k<D, 3, 2, 8, TREE>(ctx, p);
-  return launch_ring_k<D, 2, 2, 4, TREE>(ctx, p);
+    if (c.shape == RING_256) return launch_ring_k<D, 3, 2, 8, TREE, PASS>(ctx, p);
+  return launch_ring_k<D, 2, 2, 4, TREE, PASS>(ctx, p);
 }
-template <int DB, int NW, bool VEC, bool TREE>
+template <int DB, int NW, bool VEC, bool TREE, int PASS>
 hipError_t launch_f32_k(cascade_ctx* ctx, PagedParams& p) {
   constexpr int smem = (NW * 16 * (16 * DB + 4) + NW * 32) * 4;
-  constexpr auto kern = paged_f32_kernel<DB, NW, VEC, TREE>;
+  constexpr auto kern = paged_f32_kernel<DB, NW, VEC, TREE, PASS>;
   hipError_t e = allow_lds<kern>(smem, ctx->device);
   if (e != hipSuccess) return e;
-  const int64_t blocks = most_blocks(p, 16) * p.a.n_kv_heads;
+  const int64_t blocks = most_blocks<PASS>(p, 16) * p.a.n_kv_heads;
   p.in_order = p.a.n_rows == 1 || p.a.n_rows > 64 || blocks <= ctx->n_cu;
   KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
   CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)blocks), dim3(64 * NW), smem, ctx->stream, p);
   return hipGetLastError();
 }
-template <int DB, int NW>
+template <int DB, int NW, int PASS>
 hipError_t launch_f32_t(cascade_ctx* ctx, PagedParams& p) {
   const paged_attn_args& a = p.a;
   // keys, values and queries 16 bytes at a time where everything lies on such boundaries, otherwise element by element
   const bool vec = ((a.head_dim | a.q_stride | a.kv_stride | a.stride_page | a.stride_head | a.stride_pos) % 4) == 0 &&
                    (((uintptr_t)a.q | (uintptr_t)a.k_new | (uintptr_t)a.v_new | (uintptr_t)a.k_pages | (uintptr_t)a.v_pages) & 15) == 0;
-  if (a.parent) return vec ? launch_f32_k<DB, NW, true, true>(ctx, p) : launch_f32_k<DB, NW, false, true>(ctx, p);
-  return vec ? launch_f32_k<DB, NW, true, false>(ctx, p) : launch_f32_k<DB, NW, false, false>(ctx, p);
+  if constexpr (PASS != SHARED)   // (whose new tokens are none)
+    if (a.parent) return vec ? launch_f32_k<DB, NW, true, true, PASS>(ctx, p) : launch_f32_k<DB, NW, false, true, PASS>(ctx, p);
+  return vec ? launch_f32_k<DB, NW, true, false, PASS>(ctx, p) : launch_f32_k<DB, NW, false, false, PASS>(ctx, p);
 }
+template <int PASS>
 hipError_t launch_f32(cascade_ctx* ctx, PagedParams& p) {
-  if (p.a.head_dim <= 64) return launch_f32_t<4, 16>(ctx, p);
-  return p.a.head_dim <= 128 ? launch_f32_t<8, 8>(ctx, p) : launch_f32_t<16, 4>(ctx, p);
+  if (p.a.head_dim <= 64) return launch_f32_t<4, 16, PASS>(ctx, p);
+  return p.a.head_dim <= 128 ? launch_f32_t<8, 8, PASS>(ctx, p) : launch_f32_t<16, 4, PASS>(ctx, p);
 }
-template <int D>
+template <int D, int PASS>
 hipError_t launch_bf16(cascade_ctx* ctx, PagedParams& p, const Cut& c) {
-  if (c.shape == FEW) return launch_few<D>(ctx, p, c);
-  return p.a.parent ? launch_ring<D, true>(ctx, p, c) : launch_ring<D, false>(ctx, p, c);
+  if constexpr (PASS == SHARED) return launch_ring<D, false, PASS>(ctx, p, c);
+  else {
+    if (c.shape == FEW) return launch_few<D, PASS>(ctx, p, c);
+    return p.a.parent ? launch_ring<D, true, PASS>(ctx, p, c) : launch_ring<D, false, PASS>(ctx, p, c);
+  }
+}
+template <int PASS>
+hipError_t launch_pass(cascade_ctx* ctx, PagedParams& p, const Cut& c) {
+  p.parts = c.parts;
+  p.part_tiles = c.part_tiles;
+  if (c.shape == F32) return launch_f32<PASS>(ctx, p);
+  return p.a.head_dim == 128 ? launch_bf16<128, PASS>(ctx, p, c) : launch_bf16<64, PASS>(ctx, p, c);
 }
 
-}  // namespace
-
-hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
-  PagedParams p;
+PagedParams params_of(const cascade_ctx* ctx, const paged_attn_args* a) {
+  PagedParams p = {};
   p.a = *a;
   p.group = a->n_heads / a->n_kv_heads;
   p.group_inv = p.group == 1 ? 0u : (unsigned)((1ull << 32) / p.group + 1);
@@ -1482,23 +1628,106 @@ hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
   p.dev_status = ctx->dev_status;
   p.page16 = a->page_size / 16;
   p.page16_inv = p.page16 == 1 ? 0u : (unsigned)((1ull << 32) / p.page16 + 1);
-  char* ws = a->workspace ? (char*)a->workspace : ctx->attn_ws;
-  size_t ws_bytes = a->workspace ? (size_t)a->workspace_bytes : (recorded(ctx->stream) ? 0 : ctx->attn_ws_bytes);
-  const Cut c = choose(a, ctx->n_cu, ws_bytes);
-  p.parts = c.parts;
-  p.part_tiles = c.part_tiles;
+  return p;
+}
+void place_parts(PagedParams& p, char* ws, int parts) {
   p.ws_o = (float*)ws;
-  p.ws_ml = (float*)ws + (size_t)c.parts * a->n_tokens * a->n_heads * a->head_dim;
-  hipError_t e = c.shape == F32 ? launch_f32(ctx, p) : (a->head_dim == 128 ? launch_bf16<128>(ctx, p, c) : launch_bf16<64>(ctx, p, c));
-  if (e != hipSuccess) return e;
-  if (c.parts > 1) {
-    const dim3 grid((unsigned)((a->n_tokens * a->n_heads + 3) / 4));
-    KernelTimer t(ctx, CASCADE_K_PAGED_MERGE);
-    if (a->dtype == CASCADE_F32) CASCADE_TIMED_LAUNCH(t, (paged_merge_kernel<float, 4>), grid, dim3(256), 0, ctx->stream, p);
-    else if (a->head_dim == 128) CASCADE_TIMED_LAUNCH(t, (paged_merge_kernel<uint16_t, 2>), grid, dim3(256), 0, ctx->stream, p);
-    else CASCADE_TIMED_LAUNCH(t, (paged_merge_kernel<uint16_t, 1>), grid, dim3(256), 0, ctx->stream, p);
-  }
+  p.ws_ml = (float*)ws + (size_t)parts * p.a.n_tokens * p.a.n_heads * p.a.head_dim;
+}
+char* parts_of(const cascade_ctx* ctx, const paged_attn_args* a, size_t* bytes) {
+  *bytes = a->workspace ? (size_t)a->workspace_bytes : (recorded(ctx->stream) ? 0 : ctx->attn_ws_bytes);
+  return a->workspace ? (char*)a->workspace : ctx->attn_ws;
+}
+hipError_t launch_merge(cascade_ctx* ctx, const PagedParams& p) {
+  const paged_attn_args& a = p.a;
+  const dim3 grid((unsigned)((a.n_tokens * a.n_heads + 3) / 4));
+  KernelTimer t(ctx, CASCADE_K_PAGED_MERGE);
+  if (a.dtype == CASCADE_F32) CASCADE_TIMED_LAUNCH(t, (paged_merge_kernel<float, 4>), grid, dim3(256), 0, ctx->stream, p);
+  else if (a.head_dim == 128) CASCADE_TIMED_LAUNCH(t, (paged_merge_kernel<uint16_t, 2>), grid, dim3(256), 0, ctx->stream, p);
+  else CASCADE_TIMED_LAUNCH(t, (paged_merge_kernel<uint16_t, 1>), grid, dim3(256), 0, ctx->stream, p);
   return hipGetLastError();
+}
+
+// How a call with shared keys is cut: both passes, or paged_attn's own way (shared.parts 0).
+struct SharedCut {
+  Cut shared, own;
+};
+SharedCut choose_shared(const paged_shared_args* a, int n_cu, size_t ws_bytes) {
+  const paged_attn_args* t = &a->attn;
+  SharedCut c = {{FEW, 0, 0}, {FEW, 0, 0}};
+  const int G = t->n_heads / t->n_kv_heads, most = (int)std::min<size_t>(ws_bytes / part_bytes(t), MOST_PARTS);
+  if (t->window > 0 || a->n_groups >= t->n_rows || a->n_groups == 0 || t->n_rows > MOST_GROUPS || a->max_shared_len < KT || most < 2 ||
+      (double)t->n_tokens * G * G >= 4294967296.0)
+    return c;
+  // the groups as rows of a batch, as long as they are in the mean
+  paged_attn_args groups = *t;
+  groups.parent = nullptr;
+  groups.n_rows = a->n_groups;
+  groups.max_new = (t->n_tokens + a->n_groups - 1) / a->n_groups;
+  groups.max_prefix_len = std::min(a->max_shared_len, t->max_prefix_len) / KT * KT;
+  const size_t part = part_bytes(t);
+  if (t->dtype == CASCADE_F32) {
+    c.shared = choose(&groups, n_cu, (most - 1) * part);
+  } else {
+    float best = INFINITY;
+    const int tiles = groups.max_prefix_len / KT;
+    for (int shape = RING_64; shape <= (t->head_dim == 64 ? RING_256 : RING_128); ++shape)
+      for (int parts = 1; parts <= 16 && parts < most && parts <= tiles; parts = parts < 4 ? parts + 1 : parts * 2) {
+        const float us = ring_estimate_us(shape, &groups, parts, n_cu);
+        if (us < best) { best = us; c.shared = {shape, parts, 0}; }
+      }
+  }
+  paged_attn_args own = *t;
+  own.max_prefix_len = std::max(0, t->max_prefix_len - groups.max_prefix_len);
+  c.own = choose(&own, n_cu, (most - c.shared.parts) * part);
+  return c;
+}
+
+}  // namespace
+
+hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
+  PagedParams p = params_of(ctx, a);
+  size_t ws_bytes;
+  char* ws = parts_of(ctx, a, &ws_bytes);
+  const Cut c = choose(a, ctx->n_cu, ws_bytes);
+  place_parts(p, ws, c.parts);
+  const hipError_t e = launch_pass<ALONE>(ctx, p, c);
+  return e != hipSuccess || c.parts == 1 ? e : launch_merge(ctx, p);
+}
+
+hipError_t launch_paged_shared(cascade_ctx* ctx, const paged_shared_args* a) {
+  size_t ws_bytes;
+  char* ws = parts_of(ctx, &a->attn, &ws_bytes);
+  const SharedCut c = choose_shared(a, ctx->n_cu, ws_bytes);
+  if (c.shared.parts == 0) return launch_paged_attn(ctx, &a->attn);
+  PagedParams p = params_of(ctx, &a->attn);
+  p.group_off = a->group_off;
+  p.shared_len = a->shared_len;
+  p.n_groups = a->n_groups;
+  p.most_shared = std::min(a->max_shared_len, p.most_prefix);
+  place_parts(p, ws, c.shared.parts + c.own.parts);
+  hipError_t e = launch_pass<SHARED>(ctx, p, c.shared);
+  if (e != hipSuccess) return e;
+  p.part0 = c.shared.parts;
+  e = launch_pass<OWN>(ctx, p, c.own);
+  if (e != hipSuccess) return e;
+  p.parts = c.shared.parts + c.own.parts;
+  return launch_merge(ctx, p);
+}
+
+int64_t plan_paged_shared(const cascade_ctx* ctx, const paged_shared_args* a) {
+  const SharedCut c = choose_shared(a, ctx->n_cu, (size_t)1 << 40);
+  return std::max((int64_t)(c.shared.parts + c.own.parts) * (int64_t)part_bytes(&a->attn), plan_paged_attn(ctx, &a->attn));
+}
+
+void plan_shared_cut(const paged_shared_args* a, int n_cu, size_t ws_bytes, int32_t* shared_rows, int32_t* shared_parts, int32_t* own_rows, int32_t* own_parts) {
+  const SharedCut c = choose_shared(a, n_cu, ws_bytes);
+  const bool share = c.shared.parts > 0;
+  const Cut alone = choose(&a->attn, n_cu, ws_bytes);
+  *shared_rows = share ? SHAPE_ROWS[c.shared.shape] : 0;
+  *shared_parts = c.shared.parts;
+  *own_rows = SHAPE_ROWS[share ? c.own.shape : alone.shape];
+  *own_parts = share ? c.own.parts : alone.parts;
 }
 
 int64_t plan_paged_attn(const cascade_ctx* ctx, const paged_attn_args* a) {
