@@ -633,7 +633,7 @@ int paged_mass(cascade_ctx* ctx, const paged_mass_args* args);
  * (seq_len_out = L, dropped 0, nothing of mass_out) and sets the flag.  Places whose page lies outside the pool are neither read nor written and set the flag; the entries
  * are given back as they stand.  A free_count outside the list, or one behind which the entries have no room, sets it too: what has no place is not written.
  *     mass, mass_out  element (layer, s, h, y) at layer*mass_stride_layer + s*mass_stride_row + h*mass_stride_head + y, float32, mass_cap positions each; they may not overlap
- *     k_pages, v_pages  strides as for paged_append; head_dim and all strides multiples of 16 bytes, buffers on 16-byte boundaries
+ *     k_pages, v_pages  strides as for paged_append; head_dim and all strides multiples of 16 bytes, a key at most 4096, buffers on 16-byte boundaries
  *     seq_len_out, free_count_out may not alias their inputs
  *     workspace       of paged_evict_workspace's bytes, 16-byte boundary; calls that may overlap need one each
  */

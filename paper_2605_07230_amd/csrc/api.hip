@@ -662,7 +662,7 @@ static int check_paged_evict(const cascade_ctx* ctx, const paged_evict_args* a) 
   if (a->n_rows > L.max_rows || a->max_seq_len > L.max_prefix) return CASCADE_ESHAPE;
   // what the launches count, and the pages that may go back
   if (a->max_seq_len > (1 << 30) || (int64_t)a->table_width * a->page_size > 0x7fffffff || (int64_t)a->n_rows * (a->max_seq_len / a->page_size + 1) > 0x3fffffff ||
-      a->free_capacity > (1 << 30) || (double)a->n_layers * a->n_rows * a->n_kv_heads * ((a->head_dim * e + 127) / 128) > (double)(1 << 21))
+      a->free_capacity > (1 << 30) || (double)a->n_layers * a->n_rows * a->n_kv_heads > (double)(1 << 21) || a->head_dim * e > 4096)
     return CASCADE_ESHAPE;
   return CASCADE_OK;
 }

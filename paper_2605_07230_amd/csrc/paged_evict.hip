@@ -14,7 +14,7 @@ namespace {
 typedef unsigned long long u64;
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int THREADS = 256, PER = 4, STRIP = THREADS * PER;   // positions that a workgroup ranks at a time, four to a thread
+constexpr int THREADS = 256;   // of a workgroup that moves
 
 struct EvictParams {
   paged_evict_args a;
@@ -22,9 +22,14 @@ struct EvictParams {
   int units;        // (layer, row, kv head)
   int most_moves;   // pairs that a unit's list has room for
   int* dev_status;
-  int2* list;       // [units][1 + most_moves]: {number of pairs, 0}, then {place, position that goes there}
-  int pieces, slices;   // 16-byte pieces of a key; workgroups that share them
+  int2* list;       // [units][1 + most_moves]: how many of the first and the second kind, then pairs {place, position that goes there}, the second kind from the list's end
+  int pieces;       // 16-byte pieces of a key
+  int splits;       // workgroups that share a unit's moves of keys (and of values)
+  unsigned page16_inv;   // floor(2^32 / (page_size / 16)) + 1: a position's page as a high product (positions / 16 stay below 2^26); 0 for pages of 16
 };
+__device__ __forceinline__ int page_index(const EvictParams& p, int y) {
+  return p.page16_inv ? (int)__umulhi((unsigned)y >> 4, p.page16_inv) : y >> 4;
+}
 
 // ---- what remains of a row
 struct RowPlan {
@@ -50,23 +55,6 @@ __device__ __forceinline__ unsigned rank_of(float v) {
   if (!(v == v)) return 0u;
   const unsigned u = __float_as_uint(v + 0.f);
   return u >> 31 ? ~u : u | 0x80000000u;
-}
-
-// inclusive sum over the workgroup's threads, and the total
-__device__ __forceinline__ int block_scan(int* s_wave, int v, int* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  v = wave_scan_incl_i(v);
-  __syncthreads();
-  if (lane == 63) s_wave[wave] = v;
-  __syncthreads();
-  int base = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) {
-    if (w < wave) base += s_wave[w];
-    all += s_wave[w];
-  }
-  *total = all;
-  return base + v;
 }
 
 // The lengths, the pages that go back and their list: a wave to a row, behind the units' workgroups.
@@ -99,159 +87,352 @@ __device__ __forceinline__ void give_back(const EvictParams& p, int s) {
 }
 
 // Workgroup = (layer, row, kv head): the pairs of its list, and its weights.
-__global__ __launch_bounds__(THREADS) void evict_stay_kernel(EvictParams p) {
+// The weight that decides is found by radix selection of the ranks, 12, 10 and 10 bits: with the whole exponent and three bits of the fraction in the first digit, weights that spread
+// over some octaves spread over the bins.  Once no more than a wave of candidates begin like the one that decides they are ranked against each other, by weight and position, and the
+// other digits are left out.  A thread holds HELD ranks in registers (rows of up to HELD NT positions are read once); positions are dealt out in stripes of NT, so that
+// a stripe's ballots, counted per wave, place everything in the order of positions with one scan over all stripes.
+template <int NT, int HELD>
+__global__ __launch_bounds__(NT) void evict_stay_kernel(EvictParams p) {
+  constexpr int NW = NT / 64, BINS = 4096, WORDS = BINS + BINS / 16, SPAN = HELD * NT, COUNTS = (HELD * NW + 63) / 64 * 64;
   const paged_evict_args& a = p.a;
-  __shared__ int s_bin[256];
-  __shared__ int s_wave[THREADS / 64];
-  __shared__ int s_digit, s_left;
-  const int tid = threadIdx.x;
+  __shared__ int s_bin[WORDS];   // (a word between runs of 16: threads that each go through a run meet in no bank)
+  __shared__ int s_hole[WORDS];  // places given up, where a row has no more of them
+  __shared__ int s_sum[16];
+  __shared__ int s_digit, s_left, s_same, s_count;
+  __shared__ int2 s_near[64];    // candidates: rank, position
+  auto bin = [](int i) { return i + (i >> 4); };
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if ((int)blockIdx.x >= p.units) {
-    give_back(p, ((int)blockIdx.x - p.units) * (THREADS / 64) + (tid >> 6));
+    give_back(p, ((int)blockIdx.x - p.units) * NW + wave);
     return;
   }
   const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads, s = b % a.n_rows, layer = b / a.n_rows;
   int2* list = p.list + (long long)blockIdx.x * (1 + p.most_moves);
   const RowPlan w = plan_row(p, s);
-  const float* mass = a.mass + layer * a.mass_stride_layer + s * a.mass_stride_row + kvh * a.mass_stride_head;
-  float* out = a.mass_out + (mass - a.mass);
+  for (int i = tid; i < WORDS; i += NT) s_bin[i] = 0;
+  const long long at = layer * a.mass_stride_layer + s * a.mass_stride_row + kvh * a.mass_stride_head;
+  const float* mass = a.mass + at;
+  float* out = a.mass_out + at;
   const int L = w.ok ? w.L : 0, f = w.f, m = w.N - w.r, end = L - w.r, keep = m - f;   // `keep` of f .. end - 1; places f .. m - 1
   if (w.N >= L) {
     if (tid == 0) list[0] = int2{0, 0};
-    for (int y = tid; y < L; y += THREADS) out[y] = mass[y];
+    for (int y = tid; y < L; y += NT) out[y] = mass[y];
     return;
   }
-  // ---- the keep-th largest rank, eight bits at a time; `left` of those that have it are kept
-  unsigned least = 0;
-  int left = keep;
+  unsigned u[HELD];
+  const int spans = (end - f + SPAN - 1) / SPAN;
+  auto stripes = [&](int span) { return min(HELD, (end - f - span * SPAN + NT - 1) / NT); };
+  auto load = [&](int span) {
+    const int used = stripes(span);
+    float v[HELD];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      v[i] = 0.f;
+      if (i >= used) continue;
+      const int y = f + span * SPAN + i * NT + tid;
+      if (y < end) v[i] = mass[y];
+    }
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) u[i] = rank_of(v[i]);
+  };
+  if (spans == 1) load(0);
+  for (int y = tid; y < f; y += NT) out[y] = mass[y];
+  for (int y = tid; y < w.r; y += NT) out[m + y] = mass[end + y];
+  // ---- what is kept: ranks above `least`, and of those equal to it the positions up to `last`; (rank >> shift) is compared
+  unsigned least = 0xffffffffu;
+  int last = -1, shift = 0, left = 0;
+  bool by_order = false;   // of equal ones the first `left`, as they come
   if (keep > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      s_bin[tid] = 0;
+    least = 0;
+    left = keep;
+    last = 0x7fffffff;
+    for (int digit = 0; digit < 3; ++digit) {
+      const int bits = digit == 0 ? 12 : 10, bins = 1 << bits;
+      shift = digit == 0 ? 20 : (digit == 1 ? 10 : 0);
+      if (digit > 0)
+        for (int i = tid; i < bin(bins); i += NT) s_bin[i] = 0;
+      if (tid == 0) s_count = 0;
       __syncthreads();
-      const unsigned above = shift == 24 ? 0u : ~0u << (shift + 8);
-      for (int y = f + tid; y < end; y += THREADS) {
-        const unsigned u = rank_of(mass[y]);
-        if ((u & above) == least) atomicAdd(&s_bin[(u >> shift) & 255], 1);
+      for (int span = 0; span < spans; ++span) {
+        if (spans > 1) load(span);
+        const int used = stripes(span);
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+          if (i >= used) continue;
+          const bool in = f + span * SPAN + i * NT + tid < end && (digit == 0 || u[i] >> (shift + bits) == least);
+          if (in) atomicAdd(&s_bin[bin((u[i] >> shift) & (bins - 1))], 1);
+        }
       }
       __syncthreads();
-      // bins from the largest digit down: thread t holds digit 255 - t
-      const int mine = s_bin[255 - tid];
-      int total;
-      const int upto = block_scan(s_wave, mine, &total);
-      if (upto >= left && upto - mine < left) { s_digit = 255 - tid; s_left = left - (upto - mine); }
+      // from the largest digit down, some bins to a thread
+      const int each = bins / NT > 0 ? bins / NT : 1;
+      int mine = 0;
+      if (tid * each < bins)
+        for (int i = 0; i < each; ++i) mine += s_bin[bin(bins - 1 - (tid * each + i))];
+      const int incl = wave_scan_incl_i(mine);
+      if (lane == 63) s_sum[wave] = incl;
       __syncthreads();
-      least |= (unsigned)s_digit << shift;
+      int upto = incl;
+      for (int v = 0; v < wave; ++v) upto += s_sum[v];
+      if (upto >= left && upto - mine < left) {   // one thread's
+        int before = upto - mine, d = bins - 1 - tid * each;
+        while (before + s_bin[bin(d)] < left) before += s_bin[bin(d--)];
+        s_digit = d;
+        s_left = left - before;
+        s_same = s_bin[bin(d)];
+      }
+      __syncthreads();
+      least = (digit == 0 ? 0u : least << bits) | (unsigned)s_digit;
       left = s_left;
+      const int same = s_same;
+      if (left == same) break;   // all that begin so are kept
+      if (same <= 64) {
+        for (int span = 0; span < spans; ++span) {
+          if (spans > 1) load(span);
+          const int used = stripes(span);
+#pragma unroll
+          for (int i = 0; i < HELD; ++i) {
+            if (i >= used) continue;
+            const int y = f + span * SPAN + i * NT + tid;
+            if (y < end && u[i] >> shift == least) s_near[atomicAdd(&s_count, 1)] = int2{(int)u[i], y};
+          }
+        }
+        __syncthreads();
+        const int2 c = lane < same ? s_near[lane] : int2{0, 0x7fffffff};   // every wave for itself
+        int ahead = 0;
+        for (int j = 0; j < same; ++j) {
+          const unsigned other = (unsigned)__builtin_amdgcn_readlane(c.x, j);
+          const int where = __builtin_amdgcn_readlane(c.y, j);
+          ahead += other > (unsigned)c.x || (other == (unsigned)c.x && where < c.y) ? 1 : 0;
+        }
+        const int who = __ffsll((long long)__ballot(lane < same && ahead == left - 1)) - 1;   // (positions differ, so do the ranks)
+        least = (unsigned)__builtin_amdgcn_readlane(c.x, who);
+        last = __builtin_amdgcn_readlane(c.y, who);
+        shift = 0;
+        break;
+      }
+      by_order = digit == 2;
+    }
+  }
+  // Counts of `kinds` kinds of positions in all stripes and waves become what is in front of each, a wave to a kind; their sums go to s_sum.
+  auto scan = [&](int kinds) {
+    __syncthreads();
+    if (wave < kinds) {
+      int base = 0;
+#pragma unroll
+      for (int c = 0; c < COUNTS; c += 64) {
+        const int n = c + lane < HELD * NW ? s_bin[wave * COUNTS + c + lane] : 0, incl = wave_scan_incl_i(n);
+        s_bin[wave * COUNTS + c + lane] = base + incl - n;
+        base += __builtin_amdgcn_readlane(incl, 63);
+      }
+      if (lane == 0) s_sum[wave] = base;
+    }
+    __syncthreads();
+  };
+  const u64 below = (1ull << lane) - 1ull;
+  const bool in_order = w.r > L - w.N;   // the last ones move onto places of their own: the other kernel takes them one run after the other
+  int ties = 0, holes = 0, fills = 0, plain = 0;   // so far
+  for (int span = 0; span < spans; ++span) {
+    if (spans > 1) load(span);
+    const int used = stripes(span);
+    unsigned kept = 0;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int y = f + span * SPAN + i * NT + tid;
+      const unsigned x = u[i] >> shift;
+      if (y < end && keep > 0 && (x > least || (x == least && y <= last))) kept |= 1u << i;
+    }
+    if (by_order) {
       __syncthreads();
+#pragma unroll
+      for (int i = 0; i < HELD; ++i) {
+        const u64 who = i < used ? __ballot(((kept >> i) & 1) && u[i] == least) : 0ull;
+        if (lane == 0) s_bin[i * NW + wave] = __popcll(who);
+      }
+      scan(1);
+#pragma unroll
+      for (int i = 0; i < HELD; ++i) {
+        if (i >= used) continue;
+        const bool tie = ((kept >> i) & 1) && u[i] == least;
+        const u64 who = __ballot(tie);
+        if (tie && ties + s_bin[i * NW + wave] + __popcll(who & below) >= left) kept &= ~(1u << i);
+      }
+      ties += s_sum[0];
+    }
+    // three kinds of positions that the lists are made of: places given up below m; kept positions from m on; and, where the last ones come from behind all places, those of
+    // their places that nothing has to leave first
+    auto kind_of = [&](int i) {
+      const int y = f + span * SPAN + i * NT + tid;
+      const bool k = (kept >> i) & 1;
+      if (y >= end) return 3;
+      if (y < m) return k ? 3 : 0;
+      return k ? 1 : (!in_order && y < w.N ? 2 : 3);
+    };
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int kind = i < used ? kind_of(i) : 3;
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        const u64 who = __ballot(kind == k);
+        if (lane == 0) s_bin[k * COUNTS + i * NW + wave] = __popcll(who);
+      }
+    }
+    scan(3);
+    const bool in_lds = spans == 1 && s_sum[0] <= WORDS;
+    int rank[HELD];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      rank[i] = 0;
+      if (i >= used) continue;
+      const int kind = kind_of(i), y = f + span * SPAN + i * NT + tid;
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        const u64 who = __ballot(kind == k);
+        if (kind == k) rank[i] = s_bin[k * COUNTS + i * NW + wave] + __popcll(who & below);
+      }
+      if (kind == 0) {
+        if (in_lds) s_hole[rank[i]] = y;
+        else list[1 + holes + rank[i]].x = y;
+      }
+      if (kind == 1 && !in_lds) list[1 + fills + rank[i]].y = y;
+      if (kind == 2) list[p.most_moves - (plain + rank[i])] = int2{y, y + L - w.N};
+      if (y < m && ((kept >> i) & 1)) out[y] = mass[y];
+    }
+    holes += s_sum[0];
+    fills += s_sum[1];
+    plain += s_sum[2];
+    if (in_lds) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < HELD; ++i) {
+        if (i >= used || kind_of(i) != 1) continue;
+        const int y = f + i * NT + tid, to = s_hole[rank[i]];
+        list[1 + rank[i]] = int2{to, y};
+        out[to] = mass[y];
+      }
+      if (tid == 0) list[0] = int2{holes, plain};
+      return;
     }
   }
-  // ---- the lists, in order of positions
-  int ties = 0, holes = 0, fills = 0;   // so far
-  for (int y0 = f; y0 < end; y0 += STRIP) {
-    unsigned u[PER];
-    int n_tie = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int y = y0 + PER * tid + i;
-      u[i] = y < end ? rank_of(mass[y]) : 0u;
-      n_tie += y < end && u[i] == least ? 1 : 0;
-    }
-    int all_ties, all;
-    int tie = ties + block_scan(s_wave, n_tie, &all_ties) - n_tie;
-    // holes in the low half of a word, fills in the high one: a strip has at most 1024 of both
-    int marks = 0;
-    bool hole[PER], fill[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int y = y0 + PER * tid + i;
-      const bool kept = keep > 0 && (u[i] > least || (u[i] == least && tie < left));
-      if (y < end && u[i] == least) ++tie;
-      hole[i] = y < m && !kept;
-      fill[i] = y >= m && y < end && kept;
-      marks += (hole[i] ? 1 : 0) + (fill[i] ? 1 << 16 : 0);
-    }
-    const int at = block_scan(s_wave, marks, &all) - marks;
-    int h = holes + (at & 0xffff), q = fills + (at >> 16);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int y = y0 + PER * tid + i;
-      if (hole[i]) list[1 + h++].x = y;
-      if (fill[i]) list[1 + q++].y = y;
-      if (y < m && !hole[i]) out[y] = mass[y];
-    }
-    ties += all_ties;
-    holes += all & 0xffff;
-    fills += all >> 16;
-  }
-  if (tid == 0) list[0] = int2{holes, 0};
+  if (tid == 0) list[0] = int2{holes, plain};
   __syncthreads();
-  for (int i = tid; i < holes; i += THREADS) {
+  for (int i = tid; i < holes; i += NT) {
     const int2 pair = list[1 + i];
     out[pair.x] = mass[pair.y];
   }
-  for (int y = tid; y < f; y += THREADS) out[y] = mass[y];
-  for (int y = tid; y < w.r; y += THREADS) out[m + y] = mass[end + y];
 }
 
-// Workgroup = (unit, keys or values, part of their 16-byte pieces).  First the pairs, whose places and positions are different ones; then the last r, which may go to places
-// that others of them leave: a run of them is in registers before its places are written, and every later run comes from behind those.
+// Workgroup = (unit, keys or values, part of the moves).
+// Pairs of the first kind bring a kept position to a place that was given up.  Where it stood may be a place of the last n_recent: then the thread that has taken the old
+// key away brings the new one, and no other has anything to do with it.  The second kind are the other places of the last ones.  So nobody waits for anybody.
+// Only if more of the last ones move than positions go (n_recent > L - N), some move onto places of others of them: then the pairs go first, in workgroups that share the
+// 16-byte pieces of all keys, and the last ones follow in runs, each in registers before its places are written; every later run comes from behind those.
 __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictParams p) {
   const paged_evict_args& a = p.a;
-  const int tid = threadIdx.x, per = p.pieces / p.slices;
+  const int tid = threadIdx.x;
   int b = blockIdx.x;
-  const int slice = b % p.slices;
-  b /= p.slices;
+  const int split = b % p.splits;
+  b /= p.splits;
   const bool values = b & 1;
-  const int unit = b >> 1, kvh = unit % a.n_kv_heads, s = unit / a.n_kv_heads % a.n_rows, layer = unit / a.n_kv_heads / a.n_rows;
+  const int unit = b >> 1, kvh = unit % a.n_kv_heads, sl = unit / a.n_kv_heads, s = sl % a.n_rows, layer = sl / a.n_rows;
+  const int2* list = p.list + (long long)unit * (1 + p.most_moves);
+  const int2 counts = list[0];
   const RowPlan w = plan_row(p, s);
   if (!w.ok || w.N >= w.L) return;
-  const long long esize = a.dtype == CASCADE_BF16 ? 2 : 4;
-  char* const base = (char*)(values ? a.v_pages : a.k_pages) + (layer * a.stride_layer + kvh * a.stride_head) * esize + 16ll * slice * per;
+  const int gone = w.L - w.N;
+  const bool in_order = w.r > gone;
+  int pieces = p.pieces, slice = 0, splits = p.splits, mine = split;
+  if (in_order) {   // whole lines of 128 bytes
+    const int slices = p.pieces % 8 == 0 ? min(p.splits, p.pieces / 8) : 1, per = p.pieces / 8 / max(slices, 1) * 8;
+    if (slices > 1 && p.pieces % (8 * slices) == 0) {
+      if (split >= slices) return;
+      pieces = per;
+      slice = split * per;
+    } else if (split > 0) {
+      return;
+    }
+    splits = 1;
+    mine = 0;
+  }
+  const long long esize = a.dtype == CASCADE_BF16 ? 2 : 4, stride_page = a.stride_page * esize, stride_pos = a.stride_pos * esize;
+  const int each = THREADS / pieces, entry = tid / pieces, piece = tid - entry * pieces;   // keys that the workgroup moves at a time; this thread's
+  if (each == 0) return;   // (the host asks for no more pieces than threads)
+  const bool idle = entry >= each;
+  char* const base = (char*)(values ? a.v_pages : a.k_pages) + (layer * a.stride_layer + kvh * a.stride_head) * esize + 16 * (slice + piece);
   const int32_t* table = a.block_table + s * a.table_stride;
   auto place = [&](int y) -> char* {   // nullptr: outside the pool
-    const int e = y / a.page_size, page = table[e];
+    const int e = page_index(p, y), page = table[e];
     if ((unsigned)page >= (unsigned)a.n_pages) {
       atomicOr(p.dev_status, CASCADE_FLAG_PAGE);
       return nullptr;
     }
-    return base + (page * a.stride_page + (long long)(y - e * a.page_size) * a.stride_pos) * esize;
+    return base + page * stride_page + (y - e * a.page_size) * stride_pos;
   };
-  const int2* list = p.list + (long long)unit * (1 + p.most_moves);
-  const long long n = (long long)list[0].x * per;
   constexpr int U = 4;
-  for (long long i0 = tid; i0 < n; i0 += U * THREADS) {
-    u32x4 x[U];
-    char* to[U];
+  const int n = counts.x + (in_order ? 0 : counts.y), step = splits * U * each;
+  // A round's keys are on their way while the next round's places are looked up and the pairs of the one after that are read.
+  int2 pair[U];   // x < 0: none
+  char *to[U], *from[U];
+  const char* next[U];
+  auto read_pairs = [&](int i0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const long long i = i0 + u * THREADS;
-      to[u] = nullptr;
-      if (i < n) {
-        const int k = (int)(i / per), piece = (int)(i - (long long)k * per);
-        const int2 pair = list[1 + k];
-        const char* from = place(pair.y);
-        to[u] = from ? place(pair.x) : nullptr;
-        if (to[u]) { x[u] = *(const u32x4*)(from + 16 * piece); to[u] += 16 * piece; }
+      const int i = i0 + u * each;
+      pair[u] = i < n ? list[i < counts.x ? 1 + i : p.most_moves - (i - counts.x)] : int2{-1, 0};
+    }
+  };
+  auto look_up = [&]() {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      to[u] = from[u] = nullptr;
+      next[u] = nullptr;
+      if (pair[u].x >= 0) {
+        from[u] = place(pair[u].y);
+        to[u] = place(pair[u].x);
+        if (!in_order && pair[u].y < w.N) next[u] = place(pair[u].y + gone);
       }
     }
+  };
+  if (!idle) {
+    int i0 = mine * U * each + entry;
+    read_pairs(i0);
+    look_up();
+    read_pairs(i0 + step);
+    for (; i0 < n; i0 += step) {
+      u32x4 x[U], then[U];
+      char *here[U], *there[U];
+      bool chain[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (to[u]) *(u32x4*)to[u] = x[u];
+      for (int u = 0; u < U; ++u) {
+        here[u] = from[u] ? to[u] : nullptr;
+        there[u] = from[u];
+        chain[u] = from[u] && next[u];
+        if (here[u]) x[u] = *(const u32x4*)from[u];
+        if (chain[u]) then[u] = *(const u32x4*)next[u];
+      }
+      look_up();
+      read_pairs(i0 + 2 * step);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (here[u]) *(u32x4*)here[u] = x[u];
+        if (chain[u]) *(u32x4*)there[u] = then[u];
+      }
+    }
   }
+  if (!in_order) return;
   __syncthreads();
   const int m = w.N - w.r, end = w.L - w.r;
-  const long long nr = (long long)w.r * per;
-  for (long long i0 = 0; i0 < nr; i0 += U * THREADS) {
+  for (int i0 = 0; i0 < w.r; i0 += U * each) {
     u32x4 x[U];
-    char* to[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const long long i = i0 + u * THREADS + tid;
+      const int i = i0 + u * each + entry;
       to[u] = nullptr;
-      if (i < nr) {
-        const int k = (int)(i / per), piece = (int)(i - (long long)k * per);
-        const char* from = place(end + k);
-        to[u] = from ? place(m + k) : nullptr;
-        if (to[u]) { x[u] = *(const u32x4*)(from + 16 * piece); to[u] += 16 * piece; }
+      if (i < w.r && !idle) {
+        const char* from = place(end + i);
+        to[u] = from ? place(m + i) : nullptr;
+        if (to[u]) x[u] = *(const u32x4*)from;
       }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the run is in registers
@@ -279,14 +460,24 @@ hipError_t launch_paged_evict(cascade_ctx* ctx, const paged_evict_args* a) {
   p.dev_status = ctx->dev_status;
   p.list = (int2*)a->workspace;
   p.pieces = a->head_dim * (a->dtype == CASCADE_BF16 ? 2 : 4) / 16;
-  p.slices = p.pieces % 8 == 0 ? p.pieces / 8 : 1;   // whole lines of 128 bytes
+  const int page16 = a->page_size / 16;
+  p.page16_inv = page16 == 1 ? 0u : (unsigned)((1ull << 32) / page16 + 1);
   {
-    KernelTimer t(ctx, CASCADE_K_EVICT);
-    CASCADE_TIMED_LAUNCH(t, evict_stay_kernel, dim3((unsigned)(p.units + (a->n_rows + THREADS / 64 - 1) / (THREADS / 64))), dim3(THREADS), 0, ctx->stream, p);
+    auto run = [&](auto kernel, int nt) {
+      const int waves = nt / 64;
+      KernelTimer t(ctx, CASCADE_K_EVICT);
+      CASCADE_TIMED_LAUNCH(t, kernel, dim3((unsigned)(p.units + (a->n_rows + waves - 1) / waves)), dim3(nt), 0, ctx->stream, p);
+    };
+    if (a->max_seq_len <= 4 * 256) run(evict_stay_kernel<256, 4>, 256);
+    else if (a->max_seq_len <= 8 * 512) run(evict_stay_kernel<512, 8>, 512);
+    else run(evict_stay_kernel<1024, 16>, 1024);
   }
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.units == 0) return e;
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  // eight workgroups to a compute unit, 64 keys to each
+  const int64_t want = std::min<int64_t>(8 * ctx->n_cu / (2 * p.units) + 1, (p.most_moves + 63) / 64);
+  p.splits = (int)std::max<int64_t>(want, 1);
   KernelTimer t(ctx, CASCADE_K_EVICT_MOVE);
-  CASCADE_TIMED_LAUNCH(t, evict_move_kernel, dim3((unsigned)(p.units * 2 * p.slices)), dim3(THREADS), 0, ctx->stream, p);
+  CASCADE_TIMED_LAUNCH(t, evict_move_kernel, dim3((unsigned)(p.units * 2 * p.splits)), dim3(THREADS), 0, ctx->stream, p);
   return hipGetLastError();
 }
