@@ -613,7 +613,7 @@ static int check_paged_mass(const cascade_ctx* ctx, const paged_mass_args* a) {
       a->head_dim > L.head_dim)
     return CASCADE_ESHAPE;
   // query rows of a row and what a launch counts stay below 2^30 (256 threads to 64 keys at least)
-  if (a->max_seq_len > (1 << 30) || (int64_t)a->max_new * (a->n_heads / a->n_kv_heads) > (1 << 30) || (int64_t)a->n_tokens * a->n_heads > (1 << 30) ||
+  if (a->max_seq_len > (1 << 30) || ((double)a->max_new + 256.0) * (a->n_heads / a->n_kv_heads) * (a->n_heads / a->n_kv_heads) >= 4294967296.0 || a->max_new > (1 << 29) || (int64_t)a->n_tokens * a->n_heads > (1 << 30) ||
       (double)a->n_rows * a->n_kv_heads * ((a->max_seq_len + 63) / 64) > (double)(1 << 23))
     return CASCADE_ESHAPE;
   if (a->dtype == CASCADE_BF16) {

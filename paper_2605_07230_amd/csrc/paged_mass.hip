@@ -7,6 +7,8 @@
 //
 // S = Q K^T (queries as A, keys as B): a lane owns a key of each group of 16 and adds up the queries 4 g .. 4 g + 3 of every product; the four 16-lane rows meet once at the end.
 #include <algorithm>
+#include <atomic>
+#include <type_traits>
 
 #include "common.h"
 
@@ -15,13 +17,13 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int WAVES = 4, STAGE = 64 * WAVES;   // query rows that are looked up together, a thread each
 
-typedef unsigned long long u64;
 
 struct MassParams {
   paged_mass_args a;
   int group, most_len;   // query heads of a kv head; the longest row that the bounds allow
   int key_blocks;        // workgroups that a row's keys may need
   float scale_log2e;
+  unsigned group_inv;    // floor(2^32 / group) + 1: a query row's token as a high product (rows times group stay below 2^32); 0 for one head
   int* dev_status;
 };
 
@@ -70,7 +72,66 @@ struct Operand<float, D, VEC> {
   }
 };
 
-// Workgroup = (row, kv head, 64 KW positions), a wave to 16 KW of them.
+// ---- a row of the batch: its tokens, where they stand, the first position that is asked for; n = 0: nothing to do
+struct MassRow {
+  int s, lo, n, L, Lp, first;
+};
+__device__ __forceinline__ MassRow row_of(const MassParams& p, int s, bool report) {
+  const paged_mass_args& a = p.a;
+  const int lo = a.q_off[s], hi = a.q_off[s + 1], L = a.seq_len[s], first = a.first ? max(a.first[s], 0) : 0;
+  int flag = 0;
+  if (lo < 0 || hi > a.n_tokens || lo > hi || hi - lo > a.max_new) flag = CASCADE_FLAG_TREE_SIZE;
+  else if (L < hi - lo || L > p.most_len) flag = CASCADE_FLAG_CAPACITY;   // (negative lengths among them)
+  if (flag) {
+    if (report) atomicOr(p.dev_status, flag);
+    return MassRow{s, 0, 0, 0, 0, 0};
+  }
+  return MassRow{s, lo, hi - lo, L, L - (hi - lo), first};
+}
+
+// A wave's keys, groups of 16 from kb on; returns the groups that hold some.  A group that no token attends, or none of whose positions is asked for, is not read, nor
+// is its entry of the table.
+template <typename Op, typename T, int KW>
+__device__ __forceinline__ unsigned load_keys(const MassParams& p, const MassRow& r, int kvh, int kb, Op (&key)[KW]) {
+  const paged_mass_args& a = p.a;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+  unsigned there = 0;
+  const int reach = a.window > 0 ? max(r.Lp - a.window + 1, 0) : 0;   // the first position that a token sees through the window
+#pragma unroll
+  for (int kt = 0; kt < KW; ++kt) {
+    const int y0 = kb + 16 * kt;
+    if (y0 >= r.L || y0 + 15 < r.first || (y0 + 15 < reach && y0 >= a.n_sink)) continue;
+    const int e = y0 / a.page_size, page = __builtin_amdgcn_readfirstlane(a.block_table[r.s * a.table_stride + e]);
+    if ((unsigned)page >= (unsigned)a.n_pages) {
+      if (lane == 0) atomicOr(p.dev_status, CASCADE_FLAG_PAGE);
+      continue;
+    }
+    there |= 1u << kt;
+    const int inside = y0 - e * a.page_size + min(l16, r.L - 1 - y0);   // behind the last key: that one again, masked
+    key[kt].load((const T*)a.k_pages + page * a.stride_page + kvh * a.stride_head + inside * a.stride_pos, g, a.head_dim);
+  }
+  return there;
+}
+
+// The sums of a wave's groups: lane (l16, g) writes position 16 g + l16 of them.
+template <int KW>
+__device__ __forceinline__ void write_sums(const MassParams& p, const MassRow& r, int kvh, int kb, const float (&sum)[KW]) {
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+  float mine = 0.f;
+#pragma unroll
+  for (int kt = 0; kt < KW; ++kt) {
+    const float all = rows4_sum(sum[kt]);
+    if (g == kt) mine = all;
+  }
+  const int y = kb + lane;
+  if (lane < 16 * KW && y >= r.first && y < r.L) {
+    float* m = p.a.mass + r.s * p.a.mass_stride_row + kvh * p.a.mass_stride_head + y;
+    *m = y >= r.Lp ? mine : *m + mine;
+  }
+}
+
+// ----------------------------------------------------------------------------------------------------- f32, and bf16 with few query rows
+// Workgroup = (row, kv head, 64 KW positions), a wave to 16 KW of them.  Query rows come straight from memory, 16 at a time, for each wave.
 template <typename T, int D, int KW, bool VEC>
 __global__ __launch_bounds__(64 * WAVES) void paged_mass_kernel(MassParams p) {
   const paged_mass_args& a = p.a;
@@ -78,37 +139,14 @@ __global__ __launch_bounds__(64 * WAVES) void paged_mass_kernel(MassParams p) {
   __shared__ __align__(16) int s_x[STAGE];      // its position; -1: it counts nothing
   __shared__ __align__(16) float s_lse[STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4, G = p.group;
-  const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads, kblk = b % p.key_blocks, s = b / p.key_blocks;
-  const int lo = a.q_off[s], hi = a.q_off[s + 1], L = a.seq_len[s];
-  int flag = 0;
-  if (lo < 0 || hi > a.n_tokens || lo > hi || hi - lo > a.max_new) flag = CASCADE_FLAG_TREE_SIZE;
-  else if (L < hi - lo || L > p.most_len) flag = CASCADE_FLAG_CAPACITY;   // (negative lengths among them)
-  if (flag) {
-    if (kblk == 0 && kvh == 0 && tid == 0) atomicOr(p.dev_status, flag);
-    return;
-  }
-  const int n = hi - lo, M = n * G, Lp = L - n, first = a.first ? max(a.first[s], 0) : 0, W = a.window;
+  const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads, kblk = b % p.key_blocks;
+  const MassRow row = row_of(p, b / p.key_blocks, kblk == 0 && kvh == 0 && tid == 0);
+  const int lo = row.lo, n = row.n, M = n * G, Lp = row.Lp, W = a.window;
   const int kb0 = 16 * KW * WAVES * kblk;
-  if (n == 0 || kb0 >= L || kb0 + 16 * KW * WAVES <= first) return;
-
-  // ---- this wave's keys.  A group of 16 that no token attends, or none of whose positions is asked for, is not read, nor is its entry of the table.
+  if (n == 0 || kb0 >= row.L || kb0 + 16 * KW * WAVES <= row.first) return;
   const int kb = kb0 + 16 * KW * wave;
   Operand<T, D, VEC> key[KW];
-  unsigned there = 0;   // groups that hold keys
-  const int reach = W > 0 ? max(Lp - W + 1, 0) : 0;   // the first position that a token sees through the window
-#pragma unroll
-  for (int kt = 0; kt < KW; ++kt) {
-    const int y0 = kb + 16 * kt;
-    if (y0 >= L || y0 + 15 < first || (y0 + 15 < reach && y0 >= a.n_sink)) continue;
-    const int e = y0 / a.page_size, page = __builtin_amdgcn_readfirstlane(a.block_table[s * a.table_stride + e]);
-    if ((unsigned)page >= (unsigned)a.n_pages) {
-      if (lane == 0) atomicOr(p.dev_status, CASCADE_FLAG_PAGE);
-      continue;
-    }
-    there |= 1u << kt;
-    const int inside = y0 - e * a.page_size + min(l16, L - 1 - y0);   // behind the last key: that one again, masked
-    key[kt].load((const T*)a.k_pages + page * a.stride_page + kvh * a.stride_head + inside * a.stride_pos, g, a.head_dim);
-  }
+  const unsigned there = load_keys<Operand<T, D, VEC>, T, KW>(p, row, kvh, kb, key);
   // ---- the query rows that see some of them, in blocks of 16
   int from = 0, to = M;
   if (!there) to = 0;
@@ -172,18 +210,174 @@ __global__ __launch_bounds__(64 * WAVES) void paged_mass_kernel(MassParams p) {
       }
     }
   }
-  // ---- lane (l16, g) writes position 16 g + l16 of the wave's
-  float mine = 0.f;
+  write_sums<KW>(p, row, kvh, kb, sum);
+}
+
+// ------------------------------------------------------------------------------------------------------------ bf16, many query rows
+// Workgroup = (row, kv head, 64 KG positions), 64 to a wave; where KG is less than 4 the waves of the same keys share the query rows of a block.  Blocks of 64 query rows and their
+// lse pass through a ring in LDS, filled by LDS-direct loads (M0 = the LDS address of a wave's 1 KiB) two blocks ahead of their use: a wave waits for its own loads of the block
+// needed next (vmcnt), then one bare barrier makes everybody's visible and the oldest place free.  Such a load puts lane l's 16 bytes at 16 l, so rows cannot be padded;
+// slot q of row r holds piece q ^ swz(r), and the 16 rows of an operand meet in no bank.  lse of rows that are not there, and of tokens without a source, come from a place that
+// holds infinity: they count nothing.
+constexpr int QB = 64, STAGES = 3;   // query rows of a block, places of the ring
+__device__ const float s_nothing = INFINITY;
+
+template <int D>
+struct ManyGeom {
+  static constexpr int RB = 2 * D;          // bytes of a row
+  static constexpr int PPR = RB / 16;       // 16-byte pieces of a row
+  static constexpr int RPL = 1024 / RB;     // rows of a wave-wide load
+  static constexpr int LPW = QB / RPL / WAVES;   // such loads of a wave in a block
+  static constexpr int BLOCK = QB * RB, LSE = WAVES * QB * 4;   // a block in LDS; its lse, a copy to a wave
+  static constexpr int LDS = STAGES * (BLOCK + LSE);
+  __device__ static constexpr int swz(int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); }
+};
+template <int N>
+__device__ __forceinline__ void wait_and_sync() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <int D, int KG, bool SOURCE>
+__global__ __launch_bounds__(64 * WAVES, 3) void paged_mass_ring_kernel(MassParams p) {
+  using GM = ManyGeom<D>;
+  constexpr int KW = 4, KEYS = 16 * KW * KG, KS = D / 32, NQ = KG;   // NQ: groups of 16 query rows of a block that a wave takes
+  typedef Operand<uint16_t, D, true> Op;
+  extern __shared__ __align__(1024) char many_smem[];
+  __shared__ float s_join[KG < WAVES ? WAVES * 64 : 1];
+  const paged_mass_args& a = p.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4, G = p.group;
+  const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads, kblk = b / a.n_rows;   // positions that all tokens see come first
+  // (rows one further with every block of keys: workgroups that meet on a compute unit are rarely all of the longest row)
+  const MassRow row = row_of(p, (b + kblk + (kblk >> 2)) % a.n_rows, kblk == 0 && kvh == 0 && tid == 0);
+  const int lo = row.lo, n = row.n, M = n * G, Lp = row.Lp, W = a.window;
+  const int kb0 = KEYS * kblk, kb = kb0 + 16 * KW * (wave % KG), qw = wave / KG;
+  if (n == 0 || kb0 >= row.L || kb0 + KEYS <= row.first) return;
+  auto token_of = [&](int r) { return (int)(p.group_inv ? __umulhi((unsigned)r, p.group_inv) : (unsigned)r); };
+  // ---- the query rows that see some of the workgroup's keys, and of the wave's
+  auto rows_of = [&](int k0, int keys, int* from, int* to) {
+    *from = k0 > Lp ? min(k0 - Lp, n) * G : 0;
+    *to = W > 0 && k0 >= a.n_sink ? (int)min((long long)M, max(0ll, (long long)(k0 + keys - 1) + W - Lp) * G) : M;
+  };
+  int wg_from, wg_to, from, to;
+  rows_of(kb0, KEYS, &wg_from, &wg_to);
+  rows_of(kb, 16 * KW, &from, &to);
+  wg_from &= ~(QB - 1);
+
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(size_t)many_smem);
+  auto request = [&](int r0, int stage) {   // (rows behind the last: that one again, and nothing for its lse)
 #pragma unroll
-  for (int kt = 0; kt < KW; ++kt) {
-    const float all = rows4_sum(sum[kt]);
-    if (g == kt) mine = all;
+    for (int i = 0; i < GM::LPW; ++i) {
+      const int in = (GM::LPW * wave + i) * GM::RPL + lane / GM::PPR, r = min(r0 + in, M - 1), j = token_of(r);
+      int t = SOURCE ? a.source[lo + j] : lo + j;
+      if (SOURCE && (unsigned)t >= (unsigned)a.n_source) t = 0;
+      const uint16_t* at = (const uint16_t*)a.q + t * a.q_stride + (kvh * G + r - j * G) * D + 8 * ((lane % GM::PPR) ^ GM::swz(in));
+      const unsigned l = lds0 + stage * GM::BLOCK + (GM::LPW * wave + i) * 1024;
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(l), "v"(at) : "memory");
+    }
+    const int r = r0 + lane, j = token_of(min(r, M - 1)), h = kvh * G + min(r, M - 1) - j * G;
+    int t = SOURCE ? a.source[lo + j] : lo + j;
+    if (SOURCE && t != -1 && (unsigned)t >= (unsigned)a.n_source) { atomicOr(p.dev_status, CASCADE_FLAG_PATH); t = -1; }
+    const float* at = r < M && t >= 0 ? a.lse + (long long)t * a.n_heads + h : &s_nothing;
+    const unsigned l = lds0 + STAGES * GM::BLOCK + stage * GM::LSE + wave * (QB * 4);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(l), "v"(at) : "memory");
+  };
+  constexpr int LOADS = GM::LPW + 1;
+  if (wg_from < wg_to)
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) request(wg_from + i * QB, i);
+  Op key[KW];
+  const unsigned there = load_keys<Op, uint16_t, KW>(p, row, kvh, kb, key);
+  if (!there) to = 0;
+  float sum[KW];
+#pragma unroll
+  for (int kt = 0; kt < KW; ++kt) sum[kt] = 0.f;
+
+  auto block = [&](int r0, auto stage_const) {
+    constexpr int ST = decltype(stage_const)::value;
+    wait_and_sync<LOADS*(STAGES - 2)>();
+    request(r0 + (STAGES - 1) * QB, (ST + STAGES - 1) % STAGES);
+    if (r0 + QB <= from || r0 >= to) return;
+    const uint16_t* qs = (const uint16_t*)(many_smem + ST * GM::BLOCK);
+    float* ls = (float*)(many_smem + STAGES * GM::BLOCK + ST * GM::LSE) + wave * QB;
+    auto operand = [&](Op& q, int qb) {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) q.x[ks] = *(const bf16x8*)(qs + (16 * qb + l16) * D + 8 * ((4 * ks + g) ^ GM::swz(l16)));
+    };
+    // whether every row sees all of the wave's keys
+    const int rows = min(QB, M - r0), x0 = Lp + token_of(r0), x1 = Lp + token_of(r0 + rows - 1);
+    const float mine = ls[lane] * LOG2E;   // (the wave's own copy)
+    ls[lane] = mine;
+    __builtin_amdgcn_wave_barrier();
+    const bool whole = __all(fabsf(mine) < INFINITY) && there == (1u << KW) - 1 && kb + 16 * KW - 1 <= x0 && (W == 0 || x1 - kb < W);
+    if (whole) {
+      // the products of the next 16 rows stand among the exponentials of these
+      Op q[2];
+      f32x4 w[2][KW];
+      operand(q[0], NQ * qw);
+      if (NQ > 1) operand(q[1], NQ * qw + 1);
+#pragma unroll
+      for (int kt = 0; kt < KW; ++kt) w[0][kt] = Op::product(q[0], key[kt]);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        const f32x4 lse = *(const f32x4*)(ls + 16 * (NQ * qw + i) + 4 * g);
+        if (i + 2 < NQ) operand(q[i & 1], NQ * qw + i + 2);
+#pragma unroll
+        for (int kt = 0; kt < KW; ++kt) {
+          if (i + 1 < NQ) w[(i + 1) & 1][kt] = Op::product(q[(i + 1) & 1], key[kt]);
+          f32x4 e;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) e[c] = fast_exp2(fmaf(w[i & 1][kt][c], p.scale_log2e, -lse[c]));
+          sum[kt] += (e[0] + e[1]) + (e[2] + e[3]);
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < NQ; ++i) {
+        const int qb = NQ * qw + i, r = r0 + 16 * qb + 4 * g;
+        Op q;
+        operand(q, qb);
+        const f32x4 lse = *(const f32x4*)(ls + 16 * qb + 4 * g);
+        int at[4];   // positions; -1: the row counts nothing
+#pragma unroll
+        for (int c = 0; c < 4; ++c) at[c] = fabsf(lse[c]) < INFINITY ? Lp + token_of(r + c) : -1;
+#pragma unroll
+        for (int kt = 0; kt < KW; ++kt) {
+          const int y = kb + 16 * kt + l16;
+          const f32x4 w = Op::product(q, key[kt]);
+          f32x4 e;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const bool seen = y <= at[c] && (W == 0 || at[c] - y < W || y < a.n_sink) && ((there >> kt) & 1);
+            e[c] = seen ? fast_exp2(fmaf(w[c], p.scale_log2e, -lse[c])) : 0.f;
+          }
+          sum[kt] += (e[0] + e[1]) + (e[2] + e[3]);
+        }
+      }
+    }
+  };
+  for (int r0 = wg_from; r0 < wg_to; r0 += STAGES * QB) {
+    block(r0, std::integral_constant<int, 0>{});
+    if (r0 + QB < wg_to) block(r0 + QB, std::integral_constant<int, 1>{});
+    if (r0 + 2 * QB < wg_to) block(r0 + 2 * QB, std::integral_constant<int, 2>{});
   }
-  const int y = kb + lane;
-  if (lane < 16 * KW && y >= first && y < L) {
-    float* m = a.mass + s * a.mass_stride_row + kvh * a.mass_stride_head + y;
-    *m = y >= Lp ? mine : *m + mine;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the loads that nothing uses must not outlive the workgroup's LDS
+  if constexpr (KG < WAVES) {   // the waves that share keys join, in order
+#pragma unroll
+    for (int kt = 0; kt < KW; ++kt) {
+      const float all = rows4_sum(sum[kt]);
+      if (g == 0) s_join[wave * 64 + 16 * kt + l16] = all;
+    }
+    __syncthreads();
+    if (qw > 0) return;
+#pragma unroll
+    for (int kt = 0; kt < KW; ++kt) {
+      sum[kt] = 0.f;
+      if (g == 0)
+#pragma unroll
+        for (int w = 0; w < WAVES / KG; ++w) sum[kt] += s_join[(wave + KG * w) * 64 + 16 * kt + l16];
+    }
   }
+  write_sums<KW>(p, row, kvh, kb, sum);
 }
 
 template <typename T, int D, int KW, bool VEC>
@@ -194,6 +388,39 @@ hipError_t launch_k(cascade_ctx* ctx, MassParams& p) {
   KernelTimer t(ctx, CASCADE_K_MASS);
   CASCADE_TIMED_LAUNCH(t, (paged_mass_kernel<T, D, KW, VEC>), dim3((unsigned)blocks), dim3(64 * WAVES), 0, ctx->stream, p);
   return hipGetLastError();
+}
+template <auto KERNEL>
+hipError_t allow_lds(int bytes, int device) {   // more than a launch may have by default: said once per kernel and device
+  static std::atomic<unsigned long long> done{0};
+  const unsigned long long bit = 1ull << (device & 63);
+  if (device < 64 && (done.load(std::memory_order_relaxed) & bit)) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+template <int D, int KG, bool SOURCE>
+hipError_t launch_ring_k(cascade_ctx* ctx, MassParams& p) {
+  constexpr auto kern = paged_mass_ring_kernel<D, KG, SOURCE>;
+  const hipError_t e = allow_lds<kern>(ManyGeom<D>::LDS, ctx->device);
+  if (e != hipSuccess) return e;
+  p.key_blocks = (p.a.max_seq_len + 64 * KG - 1) / (64 * KG);
+  KernelTimer t(ctx, CASCADE_K_MASS);
+  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)((int64_t)p.a.n_rows * p.a.n_kv_heads * p.key_blocks)), dim3(64 * WAVES), ManyGeom<D>::LDS, ctx->stream, p);
+  return hipGetLastError();
+}
+template <int D, bool SOURCE>
+hipError_t launch_ring(cascade_ctx* ctx, MassParams& p) {
+  // Wider workgroups read the queries less often, narrower ones fill the chip.  Prompts of 16 rows x 1000 tokens behind 1000, 8 kv heads of 4 (1024 workgroups of 256 positions):
+  // 293 us with 256 positions, 310 with 128, 393 with 64; 8 rows x 300 behind 1000 (384): 94, 59, 60; 8 rows x 100 behind 500 (192): 64 positions 22.
+  const int64_t blocks = (int64_t)p.a.n_rows * p.a.n_kv_heads * ((p.a.max_seq_len + 255) / 256);
+  if (blocks >= 4 * ctx->n_cu) return launch_ring_k<D, 4, SOURCE>(ctx, p);
+  return blocks >= ctx->n_cu ? launch_ring_k<D, 2, SOURCE>(ctx, p) : launch_ring_k<D, 1, SOURCE>(ctx, p);
+}
+template <int D>
+hipError_t launch_bf16(cascade_ctx* ctx, MassParams& p) {
+  // 64 rows of 8 tokens x 4 heads behind 2000: 60 us straight from memory, 72 through the ring (the stream of keys bounds both); 16 rows of 16 x 4: 22.4 both, head_dim 64 15.2 and 12.8
+  if ((int64_t)p.a.max_new * p.group <= 32) return launch_k<uint16_t, D, 4, true>(ctx, p);
+  return p.a.source ? launch_ring<D, true>(ctx, p) : launch_ring<D, false>(ctx, p);
 }
 template <bool VEC>
 hipError_t launch_f32(cascade_ctx* ctx, MassParams& p) {
@@ -210,7 +437,8 @@ hipError_t launch_paged_mass(cascade_ctx* ctx, const paged_mass_args* a) {
   p.most_len = (int)std::min<int64_t>({a->max_seq_len, (int64_t)a->table_width * a->page_size, a->mass_cap});
   p.scale_log2e = (a->scale != 0.f ? a->scale : 1.f / sqrtf((float)a->head_dim)) * LOG2E;
   p.dev_status = ctx->dev_status;
-  if (a->dtype == CASCADE_BF16) return a->head_dim == 128 ? launch_k<uint16_t, 128, 4, true>(ctx, p) : launch_k<uint16_t, 64, 4, true>(ctx, p);
+  p.group_inv = p.group == 1 ? 0u : (unsigned)((1ull << 32) / p.group + 1);
+  if (a->dtype == CASCADE_BF16) return a->head_dim == 128 ? launch_bf16<128>(ctx, p) : launch_bf16<64>(ctx, p);
   // 16 bytes at a time where everything lies on such boundaries, otherwise element by element
   const bool vec = ((a->head_dim | a->q_stride | a->stride_page | a->stride_head | a->stride_pos) % 4) == 0 && (((uintptr_t)a->q | (uintptr_t)a->k_pages) & 15) == 0;
   return vec ? launch_f32<true>(ctx, p) : launch_f32<false>(ctx, p);

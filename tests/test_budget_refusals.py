@@ -90,7 +90,7 @@ def test_mass(lib, ctx):
                 (D, dict(dtype=2))]
              + [(S, {k: v}) for k, v in (("n_heads", 7), ("n_heads", 16), ("head_dim", 96), ("head_dim", 256), ("page_size", 8), ("page_size", 1040), ("n_rows", 5), ("n_tokens", 65),
                                          ("n_source", 65), ("max_seq_len", 1001), ("max_seq_len", 0), ("max_new", 0), ("stride_pos", 129), ("stride_head", -8), ("q_stride", 1016),
-                                         ("mass_stride_row", 999), ("mass_stride_head", 999), ("mass_stride_head", -1), ("max_new", 1 << 29))]
+                                         ("mass_stride_row", 999), ("mass_stride_head", 999), ("mass_stride_head", -1), ("max_new", 1 << 28))]
              + [(S, dict(dtype=B.F32, head_dim=257)), (B.OK, dict(n_rows=0)), (B.OK, dict(n_tokens=0))])
 
 
