@@ -139,6 +139,9 @@ __device__ __forceinline__ int group_of_row(const Groups& gr, int n_groups, int 
 }
 __device__ __forceinline__ void find_groups(const PagedParams& p, Groups& gr, int tid, int threads) {
   const paged_attn_args& a = p.a;
+  // (a row's lengths are on their way while the groups are looked at)
+  int s = tid, lo = 0, hi = 0, P = 0;
+  if (s < a.n_rows) { lo = a.q_off[s]; hi = a.q_off[s + 1]; P = a.prefix_len[s]; }
   bool bad = false;
   for (int g = tid; g <= p.n_groups; g += threads) {
     const int at = p.group_off[g];
@@ -155,9 +158,11 @@ __device__ __forceinline__ void find_groups(const PagedParams& p, Groups& gr, in
     for (int g = tid; g < p.n_groups; g += threads) gr.tiles[g] = 0;
     if (tid == 0 && blockIdx.x == 0) atomicOr(p.dev_status, CASCADE_FLAG_TREE_SIZE);
   } else {
-    for (int s = tid; s < a.n_rows; s += threads) {
-      const RowInfo r = check_row(p, s, a.q_off[s], a.q_off[s + 1], a.prefix_len[s]);
+    while (s < a.n_rows) {
+      const RowInfo r = check_row(p, s, lo, hi, P);
       atomicMin(&gr.tiles[group_of_row(gr, p.n_groups, s)], r.flag ? 0 : r.P / KT);
+      s += threads;
+      if (s < a.n_rows) { lo = a.q_off[s]; hi = a.q_off[s + 1]; P = a.prefix_len[s]; }
     }
   }
   __syncthreads();
@@ -248,7 +253,7 @@ __device__ __forceinline__ void write_nothing(const PagedParams& p, const RowInf
 template <int D, int NW>
 constexpr int few_per_unit() { return D == 64 && NW == 4 ? 3 : 8 / NW; }
 template <int D, int NW, bool TREE, int PASS>
-__global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_kernel(PagedParams p) {
+__device__ __forceinline__ void paged_few(const PagedParams& p, const int block, const int blocks) {
   static_assert(PASS != SHARED, "the tokens of a group come in any number");
   constexpr int NT = 64 * NW, KS = D / 32, DB = D / 16, DC = D / 8, VP = D + 16, OP = D + 4, NVC = KT * DC / 64, R = 16;
   extern __shared__ __align__(16) char few_smem[];
@@ -259,7 +264,7 @@ __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_ke
   __shared__ typename std::conditional<PASS == OWN, Groups, int>::type groups;
   if constexpr (PASS == OWN) find_groups(p, groups, tid, NT);
 
-  for (int item = blockIdx.x;; item += gridDim.x) {
+  for (int item = block;; item += blocks) {
     const int kvh = item % a.n_kv_heads;
     int part = item / a.n_kv_heads;
     // which row this part belongs to
@@ -572,6 +577,11 @@ __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_ke
   }
 }
 
+template <int D, int NW, bool TREE>
+__global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_kernel(PagedParams p) {
+  paged_few<D, NW, TREE, ALONE>(p, blockIdx.x, gridDim.x);
+}
+
 // ------------------------------------------------------------------------------------------------------- bf16, many query rows
 // Workgroup = (16 NQ NW query rows of a row of the batch, kv head, part of their tiles): its waves share every tile of 64 keys.  Tiles never pass through registers on
 // their way in: LDS-direct loads (global_load_lds_dwordx4, M0 = the LDS address of a wave's 1 KiB) write them into two rings of NS tiles, NS - 1 ahead of
@@ -691,8 +701,10 @@ __device__ __forceinline__ RowInfo block_group(const PagedParams& p, const Group
   return none;
 }
 
+template <int D, int NQ, int NW>
+constexpr int ring_per_simd() { return NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3) : 2); }
 template <int D, int NS, int NQ, int NW, bool TREE, int PASS>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3) : 2)) void paged_ring_kernel(PagedParams p) {
+__device__ __forceinline__ void paged_ring(const PagedParams& p, const int block, const int blocks) {
   using GM = RingGeom<D>;
   constexpr int NT = 64 * NW, RW = 16 * NQ * NW, KS = D / 32, DB = D / 16;
   constexpr int CPW = GM::CPT / NW;     // loads of K (and of V) that a wave makes per tile
@@ -711,25 +723,21 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
   // Workgroups are dealt round-robin to the 8 XCDs, one L2 each: those of a kv head stay on one XCD (or on 8 / H of them), where the blocks of a row meet in its keys.
   int kvh, b;
   {
-    const int h = blockIdx.x, x = h & 7, k = h >> 3;
+    const int h = block, x = h & 7, k = h >> 3;
     if (H % 8 == 0) { const int m = H >> 3; kvh = x + 8 * (k % m); b = k / m; }
-    else if (8 % H == 0 && (gridDim.x & 7) == 0) { kvh = x % H; b = k * (8 / H) + x / H; }
+    else if (8 % H == 0 && (blocks & 7) == 0) { kvh = x % H; b = k * (8 / H) + x / H; }
     else { kvh = h % H; b = h / H; }
   }
   const int part = b % p.parts;
-  int sb = 0, shared = 0;
+  static_assert(PASS != OWN && (PASS == ALONE || !TREE), "rows with so many tokens read all of their keys");
+  int sb = 0;
   RowInfo ri;
   if constexpr (PASS == ALONE) {
     ri = block_row(p, b / p.parts, RW, lane, &sb);
   } else {   // (the groups stand where tiles are loaded later)
     Groups& groups = *(Groups*)ring_smem;
     find_groups(p, groups, tid, NT);
-    if (PASS == SHARED) {
-      ri = block_group(p, groups, b / p.parts, RW, lane, &sb);
-    } else {
-      ri = block_row(p, b / p.parts, RW, lane, &sb);
-      if (ri.s >= 0 && !ri.flag) shared = groups.tiles[group_of_row(groups, p.n_groups, ri.s)];
-    }
+    ri = block_group(p, groups, b / p.parts, RW, lane, &sb);
     __syncthreads();
   }
   if (ri.s < 0) return;   // the grid is an upper bound of the number of blocks
@@ -737,15 +745,13 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
   auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
   const int lo = uniform(ri.lo), T = uniform(ri.T), P = uniform(ri.P), M = T * G, row0 = uniform(sb) * RW;
   const int i0 = uniform(token_of(p, row0)), i1 = uniform(token_of(p, min(row0 + RW, M) - 1));
-  Tiles ti = tiles_of(p, P, i0, i1, TREE, PASS == OWN ? uniform(shared) : 0);
+  Tiles ti = tiles_of(p, P, i0, i1, TREE);
   if (PASS == SHARED) ti.n_n = 0;
   const int nt = ti.n_p + ti.n_n, per = (nt + p.parts - 1) / p.parts, t_begin = part * per, t_end = min(nt, t_begin + per);
   const long long all_rows = (long long)a.n_tokens * a.n_heads;
-  const int part0 = PASS == ALONE ? 0 : p.part0;
-  if (PASS == OWN && part == 0 && shared == 0) write_no_shared(p, lo, T, kvh, row0, min(row0 + RW, M), tid, NT);
   if (t_begin >= t_end) {   // fewer tiles than parts: an empty one
     for (int r = row0 + tid; r < min(row0 + RW, M); r += NT) {
-      float* ml = p.ws_ml + ((part0 + part) * all_rows + (long long)(lo + r / G) * a.n_heads + kvh * G + r % G) * 2;
+      float* ml = p.ws_ml + (part * all_rows + (long long)(lo + r / G) * a.n_heads + kvh * G + r % G) * 2;
       ml[0] = -INFINITY;
       ml[1] = 0.f;
     }
@@ -1117,7 +1123,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
     const float l = rows4_sum(lsum[n]);
     if (qi[n] < 0) continue;
     if (PASS != ALONE || p.parts > 1) {
-      const long long w = (part0 + part) * all_rows + out_row[n];
+      const long long w = part * all_rows + out_row[n];
 #pragma unroll
       for (int db = 0; db < DB; ++db) *(f32x4*)(p.ws_o + w * D + 16 * db + 4 * g) = ot[n][db];
       if (g == 0) { p.ws_ml[w * 2] = m_ref[n]; p.ws_ml[w * 2 + 1] = l; }
@@ -1136,6 +1142,11 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
   }
 }
 
+template <int D, int NS, int NQ, int NW, bool TREE>
+__global__ __launch_bounds__(64 * NW, (ring_per_simd<D, NQ, NW>())) void paged_ring_kernel(PagedParams p) {
+  paged_ring<D, NS, NQ, NW, TREE, ALONE>(p, blockIdx.x, gridDim.x);
+}
+
 // ------------------------------------------------------------------------------------------------------------------------- f32
 // Workgroup = (16 query rows, kv head, part); its NW waves take every NW-th tile of 16 keys - one group, one page - and meet in LDS.  Both products run on
 // v_mfma_f32_16x16x4_f32 (one value per lane and operand, k = lane / 16 = g):
@@ -1147,14 +1158,14 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : (D == 64 ? (NQ == 1 ? 4 : 3)
 // 15 new tokens x 8 heads x 64 behind 256 keys: 9 us.  Many rows fetch every key again for each 16 of them: 8 rows of 200 tokens behind 1289 keys, 8 heads: 94 us at head_dim 64 (49 TFLOP/s; 30 at the rate
 // of a large product), 161 at 128 (57 TFLOP/s).
 template <int DB, int NW, bool VEC, bool TREE, int PASS>
-__global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
+__device__ __forceinline__ void paged_f32(const PagedParams& p, const int block) {
   extern __shared__ __align__(16) float f32_smem[];   // [NW][16 queries][16 DB + 4] outputs, [NW][16][2] maxima and sums
   __shared__ int s_parent[TREE ? CASCADE_MAX_TREE : 1];
   constexpr int OP = 16 * DB + 4, TS = 16;
   const paged_attn_args& a = p.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4, G = p.group, D = a.head_dim;
-  const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads, part = b % p.parts;
+  const int kvh = block % a.n_kv_heads, b = block / a.n_kv_heads, part = b % p.parts;
   int sb = 0, shared = 0;
   RowInfo ri;
   if constexpr (PASS == ALONE) {
@@ -1369,6 +1380,35 @@ __global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
   }
 }
 
+template <int DB, int NW, bool VEC, bool TREE>
+__global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
+  paged_f32<DB, NW, VEC, TREE, ALONE>(p, blockIdx.x);
+}
+
+// ---------------------------------------------------------------------------------------------- both passes of paged_attn_shared at once
+// The pass over shared keys is products and the trips to memory before and after them, the rows' own is the stream of their keys: in one launch each covers the other's waits.  The
+// first `shared_blocks` workgroups are the former's, one to a compute unit before any gets a second.
+struct BothParams {
+  PagedParams p;         // of the rows' own pass
+  int shared_parts, shared_blocks;
+};
+__host__ __device__ __forceinline__ PagedParams shared_pass(const BothParams& b) {
+  PagedParams p = b.p;
+  p.parts = b.shared_parts;
+  p.part0 = 0;
+  return p;
+}
+template <int D, int NQ, bool TREE>
+__global__ __launch_bounds__(256, 2) void paged_both_kernel(BothParams b) {
+  if ((int)blockIdx.x < b.shared_blocks) paged_ring<D, 2, NQ, 4, false, SHARED>(shared_pass(b), blockIdx.x, b.shared_blocks);
+  else paged_few<D, 4, TREE, OWN>(b.p, blockIdx.x - b.shared_blocks, gridDim.x - b.shared_blocks);
+}
+template <int DB, int NW, bool VEC, bool TREE>
+__global__ __launch_bounds__(64 * NW) void paged_both_f32_kernel(BothParams b) {
+  if ((int)blockIdx.x < b.shared_blocks) paged_f32<DB, NW, VEC, false, SHARED>(shared_pass(b), blockIdx.x);
+  else paged_f32<DB, NW, VEC, TREE, OWN>(b.p, blockIdx.x - b.shared_blocks);
+}
+
 // Joins the parts, a wave to a (token, query head): the parts' factors come from its lanes, so two trips to memory follow each other whatever their number.  Rows
 // that have fewer parts, or that could not be computed, left empty ones (l = 0), of which nothing else was written.  4.1 us for 32 rows of up to 16 parts; a thread
 // that goes from part to part took 9 to 11.
@@ -1528,10 +1568,10 @@ Cut choose(const paged_attn_args* a, int n_cu, size_t ws_bytes) {
 // eight waves to a part where every part has a compute unit of its own (trees, few of which are that small: one kernel)
 int few_waves(const paged_attn_args* a, const Cut& c, int n_cu) { return !a->parent && (int64_t)a->n_rows * a->n_kv_heads * c.parts <= n_cu ? 8 : 4; }
 
-template <int D, int NW, bool TREE, int PASS>
+template <int D, int NW, bool TREE>
 hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
   constexpr int v_bytes = NW * KT * (D + 16) * 2, o_bytes = NW * 16 * (D + 4 + 2) * 4, smem = v_bytes > o_bytes ? v_bytes : o_bytes;
-  constexpr auto kern = paged_few_kernel<D, NW, TREE, PASS>;
+  constexpr auto kern = paged_few_kernel<D, NW, TREE>;
   hipError_t e = allow_lds<kern>(smem, ctx->device);
   if (e != hipSuccess) return e;
   const int64_t items = (int64_t)p.a.n_rows * p.a.n_kv_heads * p.parts, slots = (int64_t)ctx->n_cu * few_per_unit<D, NW>();
@@ -1539,10 +1579,10 @@ hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
   CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)std::min(items, slots)), dim3(64 * NW), smem, ctx->stream, p);
   return hipGetLastError();
 }
-template <int D, int PASS>
+template <int D>
 hipError_t launch_few(cascade_ctx* ctx, const PagedParams& p, const Cut& c) {
-  if (p.a.parent) return launch_few_k<D, 4, true, PASS>(ctx, p);
-  return few_waves(&p.a, c, ctx->n_cu) == 8 ? launch_few_k<D, 8, false, PASS>(ctx, p) : launch_few_k<D, 4, false, PASS>(ctx, p);
+  if (p.a.parent) return launch_few_k<D, 4, true>(ctx, p);
+  return few_waves(&p.a, c, ctx->n_cu) == 8 ? launch_few_k<D, 8, false>(ctx, p) : launch_few_k<D, 4, false>(ctx, p);
 }
 
 // no more blocks of so many query rows than this, whatever the rows' lengths are; a row out of order is one
@@ -1553,14 +1593,14 @@ int64_t most_blocks(const PagedParams& p, int rows) {
   return std::min((int64_t)p.a.n_tokens * p.group / rows + p.a.n_rows, each * p.a.n_rows) * p.parts;
 }
 
-template <int D, int NS, int NQ, int NW, bool TREE, int PASS>
+template <int D, int NS, int NQ, int NW, bool TREE>
 hipError_t launch_ring_k(cascade_ctx* ctx, PagedParams& p) {
   constexpr int smem = ring_lds<D, NS, NQ, NW, TREE>();
-  constexpr auto kern = paged_ring_kernel<D, NS, NQ, NW, TREE, PASS>;
+  constexpr auto kern = paged_ring_kernel<D, NS, NQ, NW, TREE>;
   hipError_t e = allow_lds<kern>(smem, ctx->device);
   if (e != hipSuccess) return e;
   const paged_attn_args& a = p.a;
-  const int64_t blocks = most_blocks<PASS>(p, 16 * NQ * NW);
+  const int64_t blocks = most_blocks<ALONE>(p, 16 * NQ * NW);
   // (8 / n_kv_heads XCDs share a kv head: every one gets as many)
   const int64_t share = 8 % a.n_kv_heads == 0 ? 8 / a.n_kv_heads : 1;
   p.in_order = a.n_rows == 1 || a.n_rows > 64 || blocks * a.n_kv_heads <= ctx->n_cu;
@@ -1568,54 +1608,88 @@ hipError_t launch_ring_k(cascade_ctx* ctx, PagedParams& p) {
   CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)((blocks + share - 1) / share * share * a.n_kv_heads)), dim3(64 * NW), smem, ctx->stream, p);
   return hipGetLastError();
 }
-template <int D, bool TREE, int PASS>
+template <int D, bool TREE>
 hipError_t launch_ring(cascade_ctx* ctx, PagedParams& p, const Cut& c) {
-  if (c.shape == RING_64) return launch_ring_k<D, 2, 1, 4, TREE, PASS>(ctx, p);
+  if (c.shape == RING_64) return launch_ring_k<D, 2, 1, 4, TREE>(ctx, p);
   if constexpr (D == 64)
-    if (c.shape == RING_256) return launch_ring_k<D, 3, 2, 8, TREE, PASS>(ctx, p);
-  return launch_ring_k<D, 2, 2, 4, TREE, PASS>(ctx, p);
+    if (c.shape == RING_256) return launch_ring_k<D, 3, 2, 8, TREE>(ctx, p);
+  return launch_ring_k<D, 2, 2, 4, TREE>(ctx, p);
 }
-template <int DB, int NW, bool VEC, bool TREE, int PASS>
+template <int DB, int NW, bool VEC, bool TREE>
 hipError_t launch_f32_k(cascade_ctx* ctx, PagedParams& p) {
   constexpr int smem = (NW * 16 * (16 * DB + 4) + NW * 32) * 4;
-  constexpr auto kern = paged_f32_kernel<DB, NW, VEC, TREE, PASS>;
+  constexpr auto kern = paged_f32_kernel<DB, NW, VEC, TREE>;
   hipError_t e = allow_lds<kern>(smem, ctx->device);
   if (e != hipSuccess) return e;
-  const int64_t blocks = most_blocks<PASS>(p, 16) * p.a.n_kv_heads;
+  const int64_t blocks = most_blocks<ALONE>(p, 16) * p.a.n_kv_heads;
   p.in_order = p.a.n_rows == 1 || p.a.n_rows > 64 || blocks <= ctx->n_cu;
   KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
   CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)blocks), dim3(64 * NW), smem, ctx->stream, p);
   return hipGetLastError();
 }
-template <int DB, int NW, int PASS>
+// keys, values and queries 16 bytes at a time where everything lies on such boundaries, otherwise element by element
+bool f32_vectors(const paged_attn_args& a) {
+  return ((a.head_dim | a.q_stride | a.kv_stride | a.stride_page | a.stride_head | a.stride_pos) % 4) == 0 &&
+         (((uintptr_t)a.q | (uintptr_t)a.k_new | (uintptr_t)a.v_new | (uintptr_t)a.k_pages | (uintptr_t)a.v_pages) & 15) == 0;
+}
+template <int DB, int NW>
 hipError_t launch_f32_t(cascade_ctx* ctx, PagedParams& p) {
   const paged_attn_args& a = p.a;
-  // keys, values and queries 16 bytes at a time where everything lies on such boundaries, otherwise element by element
-  const bool vec = ((a.head_dim | a.q_stride | a.kv_stride | a.stride_page | a.stride_head | a.stride_pos) % 4) == 0 &&
-                   (((uintptr_t)a.q | (uintptr_t)a.k_new | (uintptr_t)a.v_new | (uintptr_t)a.k_pages | (uintptr_t)a.v_pages) & 15) == 0;
-  if constexpr (PASS != SHARED)   // (whose new tokens are none)
-    if (a.parent) return vec ? launch_f32_k<DB, NW, true, true, PASS>(ctx, p) : launch_f32_k<DB, NW, false, true, PASS>(ctx, p);
-  return vec ? launch_f32_k<DB, NW, true, false, PASS>(ctx, p) : launch_f32_k<DB, NW, false, false, PASS>(ctx, p);
+  const bool vec = f32_vectors(a);
+  if (a.parent) return vec ? launch_f32_k<DB, NW, true, true>(ctx, p) : launch_f32_k<DB, NW, false, true>(ctx, p);
+  return vec ? launch_f32_k<DB, NW, true, false>(ctx, p) : launch_f32_k<DB, NW, false, false>(ctx, p);
 }
-template <int PASS>
 hipError_t launch_f32(cascade_ctx* ctx, PagedParams& p) {
-  if (p.a.head_dim <= 64) return launch_f32_t<4, 16, PASS>(ctx, p);
-  return p.a.head_dim <= 128 ? launch_f32_t<8, 8, PASS>(ctx, p) : launch_f32_t<16, 4, PASS>(ctx, p);
+  if (p.a.head_dim <= 64) return launch_f32_t<4, 16>(ctx, p);
+  return p.a.head_dim <= 128 ? launch_f32_t<8, 8>(ctx, p) : launch_f32_t<16, 4>(ctx, p);
 }
-template <int D, int PASS>
+template <int D>
 hipError_t launch_bf16(cascade_ctx* ctx, PagedParams& p, const Cut& c) {
-  if constexpr (PASS == SHARED) return launch_ring<D, false, PASS>(ctx, p, c);
-  else {
-    if (c.shape == FEW) return launch_few<D, PASS>(ctx, p, c);
-    return p.a.parent ? launch_ring<D, true, PASS>(ctx, p, c) : launch_ring<D, false, PASS>(ctx, p, c);
-  }
+  if (c.shape == FEW) return launch_few<D>(ctx, p, c);
+  return p.a.parent ? launch_ring<D, true>(ctx, p, c) : launch_ring<D, false>(ctx, p, c);
 }
-template <int PASS>
-hipError_t launch_pass(cascade_ctx* ctx, PagedParams& p, const Cut& c) {
-  p.parts = c.parts;
-  p.part_tiles = c.part_tiles;
-  if (c.shape == F32) return launch_f32<PASS>(ctx, p);
-  return p.a.head_dim == 128 ? launch_bf16<128, PASS>(ctx, p, c) : launch_bf16<64, PASS>(ctx, p, c);
+
+// A launch of both passes: `p` is the own pass's, as for launch_pass.
+template <int D, int NQ, bool TREE>
+hipError_t launch_both_k(cascade_ctx* ctx, const PagedParams& p, const Cut& shared) {
+  constexpr int v_bytes = 4 * KT * (D + 16) * 2, o_bytes = 4 * 16 * (D + 4 + 2) * 4, few = v_bytes > o_bytes ? v_bytes : o_bytes;
+  constexpr int ring = ring_lds<D, 2, NQ, 4, false>(), smem = few > ring ? few : ring;
+  constexpr auto kern = paged_both_kernel<D, NQ, TREE>;
+  hipError_t e = allow_lds<kern>(smem, ctx->device);
+  if (e != hipSuccess) return e;
+  const int H = p.a.n_kv_heads;
+  BothParams b = {p, shared.parts, 0};
+  const int64_t share = 8 % H == 0 ? 8 / H : 1, blocks = most_blocks<SHARED>(shared_pass(b), 64 * NQ);   // (as launch_ring_k)
+  b.shared_blocks = (int)((blocks + share - 1) / share * share * H);
+  const int64_t items = (int64_t)p.a.n_rows * H * p.parts, slots = (int64_t)ctx->n_cu * 2;
+  KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
+  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)(b.shared_blocks + std::min(items, slots))), dim3(256), smem, ctx->stream, b);
+  return hipGetLastError();
+}
+template <int D>
+hipError_t launch_both(cascade_ctx* ctx, const PagedParams& p, const Cut& shared) {
+  if (shared.shape == RING_64) return p.a.parent ? launch_both_k<D, 1, true>(ctx, p, shared) : launch_both_k<D, 1, false>(ctx, p, shared);
+  return p.a.parent ? launch_both_k<D, 2, true>(ctx, p, shared) : launch_both_k<D, 2, false>(ctx, p, shared);
+}
+template <int DB, int NW, bool VEC, bool TREE>
+hipError_t launch_both_f32_k(cascade_ctx* ctx, PagedParams& p, const Cut& shared) {
+  constexpr int smem = (NW * 16 * (16 * DB + 4) + NW * 32) * 4;
+  constexpr auto kern = paged_both_f32_kernel<DB, NW, VEC, TREE>;
+  hipError_t e = allow_lds<kern>(smem, ctx->device);
+  if (e != hipSuccess) return e;
+  const int64_t own = most_blocks<OWN>(p, 16) * p.a.n_kv_heads;
+  p.in_order = p.a.n_rows == 1 || p.a.n_rows > 64 || own <= ctx->n_cu;
+  BothParams b = {p, shared.parts, 0};
+  b.shared_blocks = (int)(most_blocks<SHARED>(shared_pass(b), 16) * p.a.n_kv_heads);
+  KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
+  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)(b.shared_blocks + own)), dim3(64 * NW), smem, ctx->stream, b);
+  return hipGetLastError();
+}
+template <int DB, int NW>
+hipError_t launch_both_f32(cascade_ctx* ctx, PagedParams& p, const Cut& shared) {
+  const bool vec = f32_vectors(p.a);
+  if (p.a.parent) return vec ? launch_both_f32_k<DB, NW, true, true>(ctx, p, shared) : launch_both_f32_k<DB, NW, false, true>(ctx, p, shared);
+  return vec ? launch_both_f32_k<DB, NW, true, false>(ctx, p, shared) : launch_both_f32_k<DB, NW, false, false>(ctx, p, shared);
 }
 
 PagedParams params_of(const cascade_ctx* ctx, const paged_attn_args* a) {
@@ -1652,34 +1726,43 @@ hipError_t launch_merge(cascade_ctx* ctx, const PagedParams& p) {
 struct SharedCut {
   Cut shared, own;
 };
+// A pass over shared keys costs workgroups that stand beside the rows' own, and the join, 6 to 10 us; it saves reading them once for every row but the first of a group.  Measured on
+// inputs that change from call to call, shared and alone, us (bf16, head_dim 128, one token of 4 query heads to a kv head, unless said; in brackets MB saved, of MB that rows read by themselves):
+//   shares:   16 rows x 2048 keys x 8 kv heads, 4 tokens [126 of 141] 20.9, 23.0;  4 x 4096 x 32, 1 head [201 of 288] 30.7, 36.5;  32 x 512 x 32, 1 head [260 of 302] 26.0, 33.5;
+//             64 rows in 16 groups x 2048 x 8 [403 of 563] 54.8, 66.1;  16 x 2048 x 32, 16 tokens, 1 head [503 of 563] 44.8, 59.8;  64 x 4192 x 8 [1082 of 1255] 44, 100
+//   does not: 8 x 512 x 32, 1 head [59 of 75] 14.2, 12.5;  64 x 512 x 8 behind 300 of their own [132 of 213] 32.8, 28.7;  behind 1000 [132 of 396] 70.9, 61.8;  64 rows in 32 groups x 2048
+//             x 8 [268 of 563] 80.5, 77.3
+// With more than 16 query rows to a row of the batch the products decide, and they are as many either way: 16 x 2048 x 32, 24 tokens 60, 55; 60 tokens 83, 57; 16 x 2048 x 8, 8 tokens x 4 heads
+// 36, 25.  f32 is bound by products, 16 query rows at a time: 16 rows of one token x 1289 keys x 8 heads of 128 16.6, 28.1; 64 rows 32.7, 84.6, of 8 tokens 64.3, 84.1; but 16 rows of 15 tokens
+// 44.9, 30.3, and 16 rows x 256 keys 13.3, 10.2.
 SharedCut choose_shared(const paged_shared_args* a, int n_cu, size_t ws_bytes) {
   const paged_attn_args* t = &a->attn;
   SharedCut c = {{FEW, 0, 0}, {FEW, 0, 0}};
   const int G = t->n_heads / t->n_kv_heads, most = (int)std::min<size_t>(ws_bytes / part_bytes(t), MOST_PARTS);
-  if (t->window > 0 || a->n_groups >= t->n_rows || a->n_groups == 0 || t->n_rows > MOST_GROUPS || a->max_shared_len < KT || most < 2 ||
-      (double)t->n_tokens * G * G >= 4294967296.0)
-    return c;
+  const int shared = std::min(a->max_shared_len, t->max_prefix_len), tiles = shared / KT;
+  if (t->window > 0 || a->n_groups >= t->n_rows || a->n_groups == 0 || t->n_rows > MOST_GROUPS || tiles == 0 || most < 2 || (double)t->n_tokens * G * G >= 4294967296.0) return c;
+  const bool f32 = t->dtype == CASCADE_F32;
+  const double key = 2.0 * t->n_kv_heads * t->head_dim * (f32 ? 4 : 2), saved = (double)(t->n_rows - a->n_groups) * shared, all = (double)t->n_rows * t->max_prefix_len;
   // the groups as rows of a batch, as long as they are in the mean
-  paged_attn_args groups = *t;
-  groups.parent = nullptr;
-  groups.n_rows = a->n_groups;
-  groups.max_new = (t->n_tokens + a->n_groups - 1) / a->n_groups;
-  groups.max_prefix_len = std::min(a->max_shared_len, t->max_prefix_len) / KT * KT;
-  const size_t part = part_bytes(t);
-  if (t->dtype == CASCADE_F32) {
-    c.shared = choose(&groups, n_cu, (most - 1) * part);
+  const int64_t rows = ((int64_t)t->n_tokens + a->n_groups - 1) / a->n_groups * G, each = (int64_t)t->max_new * G;
+  if (f32 ? 2 * a->n_groups * ((rows + 15) / 16) > t->n_rows * ((each + 15) / 16) || shared < 512
+          : each > 16 || saved * key < (4 * saved < 3 * all ? 2e8 : 1e8) || 2 * saved < all)
+    return c;
+  if (f32) {
+    // a tile of 16 keys to every wave at least, parts for half of the chip
+    const int64_t units = (rows + 15) / 16 * a->n_groups * t->n_kv_heads;
+    c.shared = {F32, (int)std::min<int64_t>({std::max<int64_t>(1, n_cu / 2 / units), 16, most - 1, std::max(1, 4 * tiles / f32_waves(t))}), 0};
   } else {
-    float best = INFINITY;
-    const int tiles = groups.max_prefix_len / KT;
-    for (int shape = RING_64; shape <= (t->head_dim == 64 ? RING_256 : RING_128); ++shape)
-      for (int parts = 1; parts <= 16 && parts < most && parts <= tiles; parts = parts < 4 ? parts + 1 : parts * 2) {
-        const float us = ring_estimate_us(shape, &groups, parts, n_cu);
-        if (us < best) { best = us; c.shared = {shape, parts, 0}; }
-      }
+    // Workgroups for half of the chip, so that the rows' own find places beside them, of 32 tiles at most (64 rows x 4192 keys x 8 kv heads of 4 behind 90 to 600 of their own: 44.2 us with 4
+    // parts, 48.6 with 8, 50.1 with 16; 48 rows in 6 groups of up to 16384 keys, head_dim 64: 60.4 with 4, 37.6 with 8, 50.6 with 16)
+    const int64_t blocks = (rows + 63) / 64 * a->n_groups * t->n_kv_heads;
+    c.shared.shape = rows >= 128 && blocks >= n_cu ? RING_128 : RING_64;
+    const int64_t units = c.shared.shape == RING_64 ? blocks : (rows + 127) / 128 * a->n_groups * t->n_kv_heads;
+    c.shared.parts = (int)std::min<int64_t>({std::max<int64_t>({1, n_cu / 2 / units, (tiles + 31) / 32}), 16, most - 1, tiles});
   }
   paged_attn_args own = *t;
-  own.max_prefix_len = std::max(0, t->max_prefix_len - groups.max_prefix_len);
-  c.own = choose(&own, n_cu, (most - c.shared.parts) * part);
+  own.max_prefix_len = t->max_prefix_len - tiles * KT;
+  c.own = choose(&own, n_cu, (most - c.shared.parts) * part_bytes(t));
   return c;
 }
 
@@ -1690,8 +1773,10 @@ hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
   size_t ws_bytes;
   char* ws = parts_of(ctx, a, &ws_bytes);
   const Cut c = choose(a, ctx->n_cu, ws_bytes);
+  p.parts = c.parts;
+  p.part_tiles = c.part_tiles;
   place_parts(p, ws, c.parts);
-  const hipError_t e = launch_pass<ALONE>(ctx, p, c);
+  const hipError_t e = c.shape == F32 ? launch_f32(ctx, p) : (a->head_dim == 128 ? launch_bf16<128>(ctx, p, c) : launch_bf16<64>(ctx, p, c));
   return e != hipSuccess || c.parts == 1 ? e : launch_merge(ctx, p);
 }
 
@@ -1706,10 +1791,13 @@ hipError_t launch_paged_shared(cascade_ctx* ctx, const paged_shared_args* a) {
   p.n_groups = a->n_groups;
   p.most_shared = std::min(a->max_shared_len, p.most_prefix);
   place_parts(p, ws, c.shared.parts + c.own.parts);
-  hipError_t e = launch_pass<SHARED>(ctx, p, c.shared);
-  if (e != hipSuccess) return e;
   p.part0 = c.shared.parts;
-  e = launch_pass<OWN>(ctx, p, c.own);
+  p.parts = c.own.parts;
+  p.part_tiles = c.own.part_tiles;
+  const int D = a->attn.head_dim;
+  hipError_t e;
+  if (a->attn.dtype == CASCADE_BF16) e = D == 128 ? launch_both<128>(ctx, p, c.shared) : launch_both<64>(ctx, p, c.shared);
+  else e = D <= 64 ? launch_both_f32<4, 16>(ctx, p, c.shared) : (D <= 128 ? launch_both_f32<8, 8>(ctx, p, c.shared) : launch_both_f32<16, 4>(ctx, p, c.shared));
   if (e != hipSuccess) return e;
   p.parts = c.shared.parts + c.own.parts;
   return launch_merge(ctx, p);

@@ -17,8 +17,10 @@ class Shared(Problem):
         for g, (lo, hi) in enumerate(zip(groups, groups[1:])):
             n = max(shared[g], 0) // self.page
             for s in range(lo + 1, hi):
-                m = min(n, prefix[s] // self.page, prefix[lo] // self.page)
-                dropped = self.table[s, :m].copy()
+                m = min(n, -(-prefix[s] // self.page), prefix[lo] // self.page)          # (a shorter row: all of its pages)
+                dropped = self.table[s, :m]
+                dropped = dropped[dropped < self.k_pages.shape[0]]          # (a window has passed the others: they name no page)
+                assert ((dropped >= 0) & (dropped < self.k_pages.shape[0])).all()
                 for pages in (self.k_pages, self.v_pages):
                     pages[dev(dropped, np.int64)] = float("nan")
                 self.table[s, :m] = self.table[lo, :m]

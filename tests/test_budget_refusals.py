@@ -120,8 +120,8 @@ def test_evict(lib, ctx):
 
 def test_cuts():
     ask = dict(n_rows=64, n_groups=1, n_tokens=64, max_new=1, max_prefix_len=4800, max_shared_len=4192, n_heads=32, n_kv_heads=8, head_dim=128)
-    assert B.paged_shared_cut(**ask)[1] > 0
-    for alone in (dict(window=100), dict(n_groups=0), dict(n_groups=64), dict(max_shared_len=63)):
+    assert B.paged_shared_cut(**ask)[1] > 0 and B.paged_shared_cut(**{**ask, 'dtype': B.F32})[1] > 0
+    for alone in (dict(max_new=5), dict(n_rows=2), dict(max_prefix_len=20000), dict(window=100), dict(n_groups=0), dict(n_groups=64), dict(max_shared_len=63)):
         assert B.paged_shared_cut(**{**ask, **alone})[:2] == (0, 0), alone
     with pytest.raises(B.CascadeError):
         B.paged_shared_cut(**{**ask, "n_rows": 0})
