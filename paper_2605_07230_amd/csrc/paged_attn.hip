@@ -1399,7 +1399,7 @@ __host__ __device__ __forceinline__ PagedParams shared_pass(const BothParams& b)
   return p;
 }
 template <int D, int NQ, bool TREE>
-__global__ __launch_bounds__(256, 2) void paged_both_kernel(BothParams b) {
+__global__ __launch_bounds__(256, 2) void paged_both_ring_kernel(BothParams b) {
   if ((int)blockIdx.x < b.shared_blocks) paged_ring<D, 2, NQ, 4, false, SHARED>(shared_pass(b), blockIdx.x, b.shared_blocks);
   else paged_few<D, 4, TREE, OWN>(b.p, blockIdx.x - b.shared_blocks, gridDim.x - b.shared_blocks);
 }
@@ -1654,7 +1654,7 @@ template <int D, int NQ, bool TREE>
 hipError_t launch_both_k(cascade_ctx* ctx, const PagedParams& p, const Cut& shared) {
   constexpr int v_bytes = 4 * KT * (D + 16) * 2, o_bytes = 4 * 16 * (D + 4 + 2) * 4, few = v_bytes > o_bytes ? v_bytes : o_bytes;
   constexpr int ring = ring_lds<D, 2, NQ, 4, false>(), smem = few > ring ? few : ring;
-  constexpr auto kern = paged_both_kernel<D, NQ, TREE>;
+  constexpr auto kern = paged_both_ring_kernel<D, NQ, TREE>;
   hipError_t e = allow_lds<kern>(smem, ctx->device);
   if (e != hipSuccess) return e;
   const int H = p.a.n_kv_heads;
