@@ -584,7 +584,8 @@ int cascade_paged_shared(const cascade_ctx* ctx, const paged_shared_args* args, 
  * Token j is packed token q_off[s] + j of q and lse, or source[q_off[s] + j] (what paged_slots wrote for an accepted path: of a drafted tree the nodes that were kept
  * count, with the lse of their ancestors).  lse is paged_attn's.  A token whose source is -1 counts nothing and so does one whose lse is not finite; the other
  * sources outside the packed tokens set the flag.  Keys that no counted token attends do not reach the result, whatever they hold.
- * A row whose q_off is not in order or in n_tokens, that has more than max_new tokens or fewer positions than tokens, or whose length is
+ * With prefix_len a row whose seq_len is still that (paged_slots had no room for its tokens) is left as it is.
+ * A row whose q_off is not in order or in n_tokens, that has more than max_new tokens or fewer positions than tokens (with prefix_len: another number than it has more), or whose length is
  * negative or larger than max_seq_len, its table or mass_cap, is left as it is and sets the flag, as do entries of the table outside the pool (their positions get nothing).
  * Scores and sums are float32, in an order that depends on nothing but the call's sizes.
  *     q, lse       as in paged_attn, n_source packed tokens;  k_pages, block_table likewise (the call is one layer's)
@@ -598,6 +599,7 @@ typedef struct {
   const int32_t* seq_len;       /* [n_rows] */
   const int32_t* source;        /* [n_tokens], nullable => token t itself (n_source >= n_tokens) */
   const int32_t* first;         /* [n_rows], nullable => 0 */
+  const int32_t* prefix_len;    /* [n_rows], nullable: lengths before the tokens */
   int32_t n_tokens;             /* HOST: tokens that q_off may count */
   int32_t n_source;             /* HOST: tokens that q and lse hold */
   int32_t max_new;              /* HOST upper bound on any row's tokens */

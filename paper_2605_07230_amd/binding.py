@@ -112,7 +112,7 @@ class paged_shared_args(C.Structure):
 
 
 class paged_mass_args(C.Structure):
-    _fields_ = [("dtype", C.c_int), ("n_rows", _i32), ("q_off", _vp), ("seq_len", _vp), ("source", _vp), ("first", _vp), ("n_tokens", _i32), ("n_source", _i32),
+    _fields_ = [("dtype", C.c_int), ("n_rows", _i32), ("q_off", _vp), ("seq_len", _vp), ("source", _vp), ("first", _vp), ("prefix_len", _vp), ("n_tokens", _i32), ("n_source", _i32),
                 ("max_new", _i32), ("max_seq_len", _i32), ("n_heads", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("scale", _f32), ("window", _i32),
                 ("n_sink", _i32), ("q", _vp), ("q_stride", _i64), ("lse", _vp), ("k_pages", _vp), ("stride_page", _i64), ("stride_head", _i64),
                 ("stride_pos", _i64), ("n_pages", _i32), ("page_size", _i32), ("block_table", _vp), ("table_stride", _i64), ("table_width", _i32),
@@ -563,10 +563,10 @@ def paged_shared_cut(*, n_rows, n_groups, n_tokens, max_new, max_prefix_len, max
     return tuple(x.value for x in out)
 
 
-def paged_mass(ctx: Context, *, q_off, seq_len, block_table, q, lse, k_pages, mass, source=None, first=None, scale: float = 0.0, window: int = 0, n_sink: int = 0,
+def paged_mass(ctx: Context, *, q_off, seq_len, block_table, q, lse, k_pages, mass, source=None, first=None, prefix_len=None, scale: float = 0.0, window: int = 0, n_sink: int = 0,
                max_new: int, max_seq_len: int) -> None:
     """q [N,Hq,D] (tokens any stride apart) and lse [N,Hq] of an attention call; q_off [S+1], seq_len [S] and source [tokens] as paged_slots wrote them (source None:
-    the tokens themselves); k_pages [pages,Hkv,page_size,D] in any order of memory (last dim contiguous), block_table [S,width]; first [S]; mass [S,Hkv,positions]
+    the tokens themselves); k_pages [pages,Hkv,page_size,D] in any order of memory (last dim contiguous), block_table [S,width]; first, prefix_len [S]; mass [S,Hkv,positions]
     float32 (last dim contiguous), updated in place."""
     n, heads, D = q.shape
     q_stride, q_head, q_one = q.stride()
@@ -583,7 +583,7 @@ def paged_mass(ctx: Context, *, q_off, seq_len, block_table, q, lse, k_pages, ma
             and (mass_one == 1 or cap <= 1) and rows == seq_len.numel() and mass_heads == kv_heads and mass.dtype is lse.dtype is torch.float32)
     _check(ctx.lib.paged_mass_record(ctx.handle, _MASS(
         _dtype_code(q), rows, q_off.data_ptr(), seq_len.data_ptr(), 0 if source is None else source.data_ptr(), 0 if first is None else first.data_ptr(),
-        n if source is None else source.numel(), n, max_new, max_seq_len, heads, kv_heads, D, scale, window, n_sink, q.data_ptr(), q_stride, lse.data_ptr(),
+        0 if prefix_len is None else prefix_len.data_ptr(), n if source is None else source.numel(), n, max_new, max_seq_len, heads, kv_heads, D, scale, window, n_sink, q.data_ptr(), q_stride, lse.data_ptr(),
         k_pages.data_ptr(), page_stride, head_stride, pos_stride, pages, page_size, block_table.data_ptr(), table_stride, block_table.shape[1], cap,
         mass.data_ptr(), mass_row, mass_head)))
 

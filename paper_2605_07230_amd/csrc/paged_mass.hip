@@ -82,6 +82,11 @@ __device__ __forceinline__ MassRow row_of(const MassParams& p, int s, bool repor
   int flag = 0;
   if (lo < 0 || hi > a.n_tokens || lo > hi || hi - lo > a.max_new) flag = CASCADE_FLAG_TREE_SIZE;
   else if (L < hi - lo || L > p.most_len) flag = CASCADE_FLAG_CAPACITY;   // (negative lengths among them)
+  if (a.prefix_len) {
+    const int before = a.prefix_len[s];
+    if (!flag && before == L) return MassRow{s, 0, 0, 0, 0, 0};
+    if (!flag && before != L - (hi - lo)) flag = CASCADE_FLAG_CAPACITY;
+  }
   if (flag) {
     if (report) atomicOr(p.dev_status, flag);
     return MassRow{s, 0, 0, 0, 0, 0};

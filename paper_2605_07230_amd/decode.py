@@ -9,7 +9,7 @@ stochastic drafter and the target's forward pass.  What is real is the chain: th
 what the walk accepted, so attention reads what earlier steps committed.
 
 ``PagedLoop`` is the same chain for a batch of prompts whose prefixes lie in pages: prompts arrive in chunks, steps verify trees or draw
-one token per prompt, and rows take pages as they grow.
+one token per prompt, and rows take pages as they grow; rows may begin with the pages of another one, and may be held to a budget.
 
 Host logic only; every computation runs in the library's kernels.
 """
@@ -191,11 +191,13 @@ class PagedLoop:
     the prompts' tokens.  Lengths, tables and free pages live on the device: a step needs nothing from the host but a bound of the prefix lengths.
     A row grows to ``max_len``, rounded up to whole pages; one without room, there or in the pool, stays as it is, and ``ctx.device_status()`` says so.
     Calls run on the stream that was current when the loop was made; inputs have to be ready for it.  What is given under another current stream may be
-    dropped at once: its memory is not handed out again before the loop's stream has passed the call."""
+    dropped at once: its memory is not handed out again before the loop's stream has passed the call.
+    ``share`` lets rows begin with the pages of another one; with ``keep_mass`` the loop sums up what attention uses of every position, and ``evict`` holds rows to a budget by it."""
 
-    def __init__(self, inp, page_size: int = 64, n_pages: Optional[int] = None, max_len: int = 4096, max_chunk: int = 1024, device: str = "cuda:0"):
+    def __init__(self, inp, page_size: int = 64, n_pages: Optional[int] = None, max_len: int = 4096, max_chunk: int = 1024, device: str = "cuda:0",
+                 keep_mass: bool = False):
         width = -(-max_len // page_size)
-        self.inp, self.page_size, self.max_len, self.max_chunk = inp, page_size, width * page_size, max_chunk
+        self.inp, self.page_size, self.max_len, self.max_chunk, self.keep_mass = inp, page_size, width * page_size, max_chunk, keep_mass
         self.dev = torch.device(device)
         with torch.cuda.device(self.dev):
             self._allocate(inp, page_size, n_pages, width, max_chunk, device)
@@ -219,6 +221,16 @@ class PagedLoop:
         self.q_off = i32(S + 1)
         self.longest = 0                       # host bound on the rows' lengths
         self.rows = inp.n_rows
+        self.admitted: Optional[List[int]] = [0] * S      # tokens that the rows were given; None once steps have made rows longer
+        self.group_off = self.shared_len = None           # what share has set, for the attention calls
+        self.longest_shared = 0
+        self.held = i32(S)                                # positions of each row that lie in pages of several rows
+        if self.keep_mass:
+            self.mass = torch.zeros((1, S, inp.n_kv_heads, self.max_len), dtype=torch.float32, device=self.dev)
+            self.mass_next = torch.zeros_like(self.mass)
+            self.dropped, self.gone = i32(S), i32(S)      # positions that each row has given up, in all and in the last call
+            self.scratch = torch.empty(max(16, binding.paged_evict_workspace(self.ctx, **self._eviction(self.seq_len, self.held, 0))),
+                                       dtype=torch.uint8, device=self.dev)
 
     def _keep(self, *tensors) -> None:
         """Tensors of a caller: tells the allocator that the loop's stream uses them."""
@@ -237,6 +249,64 @@ class PagedLoop:
         self.free_count, self.free_next = self.free_next, self.free_count
         return slot_map, source
 
+    def _attend(self, prefix_len, **attn) -> None:
+        if self.group_off is None:
+            binding.paged_attn(self.ctx, prefix_len=prefix_len, **attn)
+        else:
+            binding.paged_attn_shared(self.ctx, prefix_len=prefix_len, group_off=self.group_off, shared_len=self.shared_len,
+                                      max_shared_len=min(self.longest_shared, attn["max_prefix_len"]), **attn)
+
+    def _weigh(self, q, lse, before, max_new: int, source=None) -> None:
+        """What the tokens that the last ``_place`` gave slots attended (behind their append); positions that cannot go are left out."""
+        binding.paged_mass(self.ctx, q_off=self.q_off, seq_len=self.seq_len, block_table=self.block_table, q=q, lse=lse, k_pages=self.k_pages[0], mass=self.mass[0],
+                           source=source, first=self.held, prefix_len=before, max_new=max_new, max_seq_len=self.longest)
+
+    def share(self, group_off, positions) -> None:
+        """Rows group_off[g] + 1 .. group_off[g + 1] - 1 (host lists; all rows, in order) get the first positions[g] positions of row group_off[g], in the same pages: whole
+        pages that this row was admitted to.  The others must be empty, and no step may have been made.  Rows of a group give these pages back together."""
+        ok = (len(group_off) == len(positions) + 1 and group_off[0] == 0 and group_off[-1] == self.rows and all(a <= b for a, b in zip(group_off, group_off[1:])))
+        if not ok or self.admitted is None or self.group_off is not None:
+            raise ValueError(f"groups of rows {list(group_off)}, {self.rows} rows: once, for all rows in order, before the first step")
+        for lo, hi, n in zip(group_off, group_off[1:], positions):
+            if n < 0 or n % self.page_size or (hi - lo > 1 and (n > self.admitted[lo] or any(self.admitted[lo + 1:hi]))):
+                raise ValueError(f"rows {lo} to {hi - 1} cannot share {n} positions: whole pages of {self.page_size} of what the first has, the others empty")
+        with torch.cuda.stream(self.ctx.stream):
+            there = []                                    # (the first row may have been refused its pages)
+            for lo, hi, n in zip(group_off, group_off[1:], positions):
+                pages = n // self.page_size
+                n = n if hi - lo > 1 else 0
+                there.append(torch.where(self.seq_len[lo] >= n, n, 0).to(torch.int32) if hi > lo else self.seq_len.new_zeros(()))
+                self.block_table[lo + 1:hi, :pages] = self.block_table[lo, :pages]
+                self.seq_len[lo + 1:hi] = there[-1]
+                self.held[lo:hi] = there[-1]
+                for s in range(lo + 1, hi):
+                    self.admitted[s] = n
+            self.shared_len = torch.stack(there) if there else self.seq_len.new_zeros(0)
+            self.group_off = torch.tensor(list(group_off), dtype=torch.int32, device=self.dev)
+        self.longest_shared = max([n for lo, hi, n in zip(group_off, group_off[1:], positions) if hi - lo > 1], default=0)
+
+    def _eviction(self, budget, n_first, n_recent):
+        return dict(seq_len=self.seq_len, budget=budget, n_first=n_first, n_recent=n_recent, block_table=self.block_table, k_pages=self.k_pages, v_pages=self.v_pages, mass=self.mass,
+                    mass_out=self.mass_next, free_pages=self.free_pages, free_count=self.free_count, seq_len_out=self.seq_next, free_count_out=self.free_next,
+                    dropped=self.gone, max_seq_len=self.max_len)
+
+    def evict(self, budget, n_first: int = 0, n_recent: int = 0) -> None:
+        """Rows with more than budget positions (one number, or one for each row) give up those that attention used least, each kv head its own; their last pages go back.
+        The first n_first positions, those in shared pages and the last n_recent stay.  ``dropped`` counts what each row has given up."""
+        if not self.keep_mass:
+            raise ValueError("positions are weighed if the loop is made with keep_mass")
+        budgets = [int(budget)] * self.rows if isinstance(budget, int) else [int(b) for b in budget]
+        if len(budgets) != self.rows or min(budgets) < 0 or n_first < 0 or n_recent < 0:
+            raise ValueError(f"budgets {budgets}, first {n_first}, recent {n_recent}: one budget, or one for each of {self.rows} rows")
+        with torch.cuda.stream(self.ctx.stream):
+            args = self._eviction(torch.tensor(budgets, dtype=torch.int32, device=self.dev), self.held.clamp(min=n_first), n_recent)
+            binding.paged_evict(self.ctx, workspace=self.scratch, **{**args, "max_seq_len": self.longest})
+            self.dropped += self.gone
+        self.seq_len, self.seq_next = self.seq_next, self.seq_len
+        self.free_count, self.free_next = self.free_next, self.free_count
+        self.mass, self.mass_next = self.mass_next, self.mass
+        self.longest = min(self.longest, max(max(budgets), max(n_first, self.longest_shared) + n_recent))
+
     def admit(self, q, k_new, v_new, new_len, out, lse=None):
         """A chunk of every row's prompt, packed row by row: its attention over what is there and over itself, then its keys and values go to
         the pages.  new_len: host lengths."""
@@ -246,6 +316,8 @@ class PagedLoop:
             return
         self._keep(q, k_new, v_new, out, lse)
         with torch.cuda.stream(self.ctx.stream):
+            if self.keep_mass and lse is None:
+                lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.dev)
             attn = dict(q_off=self.q_off, block_table=self.block_table, q=q, k_new=k_new, v_new=v_new, k_pages=self.k_pages[0], v_pages=self.v_pages[0], out=out, lse=lse,
                         max_new=max(new_len), max_prefix_len=self.longest)
             append = dict(k_new=k_new.unsqueeze(0), v_new=v_new.unsqueeze(0), k_pages=self.k_pages, v_pages=self.v_pages)
@@ -255,17 +327,20 @@ class PagedLoop:
             lens = torch.tensor(new_len, dtype=torch.int32, device=self.dev)
             before = self.seq_len.clone()
             slot_map, _ = self._place(q.shape[0], new_len=lens)
-            binding.paged_attn(self.ctx, prefix_len=before, **attn)
+            self._attend(before, **attn)
             binding.paged_append(self.ctx, slot_map=slot_map, **append)
-        self.longest = min(self.longest + max(new_len), self.max_len)
+            self.longest = min(self.longest + max(new_len), self.max_len)
+            if self.keep_mass:
+                self._weigh(q, lse, before, max(new_len))
+        if self.admitted is not None:
+            self.admitted = [n + more for n, more in zip(self.admitted, new_len)]
 
     def step(self, mode: int = binding.WALK_SEQUENTIAL) -> None:
         """One verification step of every prompt's tree over the pages, and the commit of what it accepts to them."""
         st = self.step_in
         with torch.cuda.stream(self.ctx.stream):   # and on its device
-            binding.paged_attn(self.ctx, q_off=st.row_node_off, parent=st.row_parent, prefix_len=self.seq_len, block_table=self.block_table, q=st.q, k_new=st.k_tree,
-                               v_new=st.v_tree, k_pages=self.k_pages[0], v_pages=self.v_pages[0], out=st.attn_out, lse=st.attn_lse, max_new=st.max_tree,
-                               max_prefix_len=self.longest)
+            self._attend(self.seq_len, q_off=st.row_node_off, parent=st.row_parent, block_table=self.block_table, q=st.q, k_new=st.k_tree, v_new=st.v_tree,
+                         k_pages=self.k_pages[0], v_pages=self.v_pages[0], out=st.attn_out, lse=st.attn_lse, max_new=st.max_tree, max_prefix_len=self.longest)
             st.lmhead()
             st.accept()
             st.select(mode)
@@ -273,7 +348,10 @@ class PagedLoop:
                                            path_nodes=st.path_nodes, n_nodes_total=st.q.shape[0])
             binding.paged_append(self.ctx, k_new=st.k_tree.unsqueeze(0), v_new=st.v_tree.unsqueeze(0), slot_map=slot_map, source=source, k_pages=self.k_pages,
                                  v_pages=self.v_pages)
-        self.longest = min(self.longest + st.max_depth + 1, self.max_len)
+            self.longest = min(self.longest + st.max_depth + 1, self.max_len)
+            if self.keep_mass:
+                self._weigh(st.q, st.attn_lse, self.seq_next, st.max_depth + 1, source)   # (the lengths before, until the next call)
+        self.admitted = None
 
     def draw(self, u, token, prob=None, **parameters) -> None:
         """Plain decoding: one token of every prompt from the logits of its tree's root (of the last ``step``), with each prompt's own sampling parameters."""

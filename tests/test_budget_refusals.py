@@ -82,7 +82,7 @@ def test_shared(lib, ctx):
 
 
 def test_mass(lib, ctx):
-    r = B.paged_mass_args(B.BF16, 4, 64, 64, 64, 64, 64, 64, 32, 1000, 8, 2, 128, 0.0, 0, 0, 64, 1024, 64, 64, 4096, 2048, 128, 10, 16, 64, 63, 63, 1000, 64, 2000, 1000)
+    r = B.paged_mass_args(B.BF16, 4, 64, 64, 64, 64, 64, 64, 64, 32, 1000, 8, 2, 128, 0.0, 0, 0, 64, 1024, 64, 64, 4096, 2048, 128, 10, 16, 64, 63, 63, 1000, 64, 2000, 1000)
     _refused(lib.paged_mass, ctx, r, [(E, {k: None}) for k in ("q_off", "seq_len", "q", "lse", "k_pages", "block_table", "mass")]
              + [(E, {k: -1}) for k in ("n_rows", "n_tokens", "n_source", "max_new", "max_seq_len", "window", "n_sink", "mass_cap", "n_pages", "table_width")]
              + [(E, {k: 72}) for k in ("q", "k_pages")]
@@ -96,7 +96,7 @@ def test_mass(lib, ctx):
 
 def test_mass_that_a_launch_cannot_count(lib):
     big = _context(1 << 20, 1 << 30, 32, 1 << 30, 128, 128)
-    r = B.paged_mass_args(B.BF16, 1 << 15, 64, 64, None, None, 0, 0, 1, 1 << 20, 128, 128, 128, 0.0, 0, 0, 64, 16384, 64, 64, 4096, 2048, 128, 10, 16, 64, 63, 63, 1 << 20, 64,
+    r = B.paged_mass_args(B.BF16, 1 << 15, 64, 64, None, None, None, 0, 0, 1, 1 << 20, 128, 128, 128, 0.0, 0, 0, 64, 16384, 64, 64, 4096, 2048, 128, 10, 16, 64, 63, 63, 1 << 20, 64,
                           1 << 30, 1 << 20)
     _refused(lib.paged_mass, big, r, [(S, dict(n_tokens=1, n_source=1)), (S, dict(n_tokens=(1 << 23) + 1, n_source=1 << 24, n_rows=1)), (B.OK, dict(n_rows=0))])
 

@@ -174,6 +174,19 @@ def test_entries_and_sources_outside_set_the_flag():
     p.check()
 
 
+def test_rows_that_got_no_room_stay_as_they_are():
+    for dtype, new in (("bf16", [3, 2]), ("bf16", [40, 30]), ("f32", [3, 2])):
+        p = Mass(12, [243, 252], new, heads=4, kv_heads=2, dtype=dtype)
+        ctx = p.context()
+        p.run(ctx, prefix_len=dev([243, 252 - new[1]]))
+        assert ctx.device_status() == binding.OK
+        assert torch.equal(p.mass[0].nan_to_num(-1), p.before[0].nan_to_num(-1))
+        p.check(rows=[1])
+        p.run(ctx, prefix_len=dev([243 - new[0], 251]))
+        assert ctx.device_status() == binding.ETREE
+        p.check(rows=[0])
+
+
 def test_sums_repeat():
     p = Mass(10, [1500, 700], [300, 1], heads=8, kv_heads=2)
     ctx = p.context()
