@@ -89,15 +89,16 @@ __device__ __forceinline__ void give_back(const EvictParams& p, int s) {
 // Workgroup = (layer, row, kv head): the pairs of its list, and its weights.
 // The weight that decides is found by radix selection of the ranks, 12, 10 and 10 bits: with the whole exponent and three bits of the fraction in the first digit, weights that spread
 // over some octaves spread over the bins.  Once no more than a wave of candidates begin like the one that decides they are ranked against each other, by weight and position, and the
-// other digits are left out.  A thread holds HELD ranks in registers (rows of up to HELD NT positions are read once); positions are dealt out in stripes of NT, so that
-// a stripe's ballots, counted per wave, place everything in the order of positions with one scan over all stripes.
+// other digits are left out.  A thread holds HELD consecutive positions in registers (rows of up to HELD NT positions are read once), so one scan over the threads' counts gives everything
+// its place in the order of positions.
 template <int NT, int HELD>
 __global__ __launch_bounds__(NT) void evict_stay_kernel(EvictParams p) {
-  constexpr int NW = NT / 64, BINS = 4096, WORDS = BINS + BINS / 16, SPAN = HELD * NT, COUNTS = (HELD * NW + 63) / 64 * 64;
+  constexpr int NW = NT / 64, BINS = 4096, WORDS = BINS + BINS / 16, SPAN = HELD * NT;
+  typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));   // (such loads need the boundary of a word)
   const paged_evict_args& a = p.a;
   __shared__ int s_bin[WORDS];   // (a word between runs of 16: threads that each go through a run meet in no bank)
   __shared__ int s_hole[WORDS];  // places given up, where a row has no more of them
-  __shared__ int s_sum[16];
+  __shared__ int s_sum[2][NW];
   __shared__ int s_digit, s_left, s_same, s_count;
   __shared__ int2 s_near[64];    // candidates: rank, position
   auto bin = [](int i) { return i + (i >> 4); };
@@ -110,6 +111,7 @@ __global__ __launch_bounds__(NT) void evict_stay_kernel(EvictParams p) {
   int2* list = p.list + (long long)blockIdx.x * (1 + p.most_moves);
   const RowPlan w = plan_row(p, s);
   for (int i = tid; i < WORDS; i += NT) s_bin[i] = 0;
+  if (tid == 0) s_count = 0;
   const long long at = layer * a.mass_stride_layer + s * a.mass_stride_row + kvh * a.mass_stride_head;
   const float* mass = a.mass + at;
   float* out = a.mass_out + at;
@@ -121,23 +123,42 @@ __global__ __launch_bounds__(NT) void evict_stay_kernel(EvictParams p) {
   }
   unsigned u[HELD];
   const int spans = (end - f + SPAN - 1) / SPAN;
-  auto stripes = [&](int span) { return min(HELD, (end - f - span * SPAN + NT - 1) / NT); };
+  auto first_of = [&](int span) { return f + span * SPAN + HELD * tid; };
   auto load = [&](int span) {
-    const int used = stripes(span);
-    float v[HELD];
+    const int y0 = first_of(span);
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-      v[i] = 0.f;
-      if (i >= used) continue;
-      const int y = f + span * SPAN + i * NT + tid;
-      if (y < end) v[i] = mass[y];
+    for (int i = 0; i < HELD; i += 4) {
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      if (y0 + i + 3 < end) v = *(const f32x4_any*)(mass + y0 + i);
+      else
+#pragma unroll
+        for (int c = 0; c < 3; ++c)
+          if (y0 + i + c < end) v[c] = mass[y0 + i + c];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) u[i + c] = rank_of(v[c]);
     }
-#pragma unroll
-    for (int i = 0; i < HELD; ++i) u[i] = rank_of(v[i]);
   };
   if (spans == 1) load(0);
-  for (int y = tid; y < f; y += NT) out[y] = mass[y];
+  // (places that are given up get the weights that come there below)
+  for (int y = tid; y < m; y += NT) out[y] = mass[y];
   for (int y = tid; y < w.r; y += NT) out[m + y] = mass[end + y];
+  // what is in front of this thread's counts, and their sum; two buffers in turn, so that one barrier does
+  int turn = 0;
+  auto before_me = [&](int v, int* total) {
+    const int incl = wave_scan_incl_i(v);
+    if (lane == 63) s_sum[turn][wave] = incl;
+    __syncthreads();
+    int base = 0, all = 0;
+#pragma unroll
+    for (int x = 0; x < NW; ++x) {
+      const int n = s_sum[turn][x];
+      base += x < wave ? n : 0;
+      all += n;
+    }
+    turn ^= 1;
+    *total = all;
+    return base + incl - v;
+  };
   // ---- what is kept: ranks above `least`, and of those equal to it the positions up to `last`; (rank >> shift) is compared
   unsigned least = 0xffffffffu;
   int last = -1, shift = 0, left = 0;
@@ -151,15 +172,13 @@ __global__ __launch_bounds__(NT) void evict_stay_kernel(EvictParams p) {
       shift = digit == 0 ? 20 : (digit == 1 ? 10 : 0);
       if (digit > 0)
         for (int i = tid; i < bin(bins); i += NT) s_bin[i] = 0;
-      if (tid == 0) s_count = 0;
       __syncthreads();
       for (int span = 0; span < spans; ++span) {
         if (spans > 1) load(span);
-        const int used = stripes(span);
+        const int y0 = first_of(span);
 #pragma unroll
         for (int i = 0; i < HELD; ++i) {
-          if (i >= used) continue;
-          const bool in = f + span * SPAN + i * NT + tid < end && (digit == 0 || u[i] >> (shift + bits) == least);
+          const bool in = y0 + i < end && (digit == 0 || u[i] >> (shift + bits) == least);
           if (in) atomicAdd(&s_bin[bin((u[i] >> shift) & (bins - 1))], 1);
         }
       }
@@ -169,13 +188,10 @@ __global__ __launch_bounds__(NT) void evict_stay_kernel(EvictParams p) {
       int mine = 0;
       if (tid * each < bins)
         for (int i = 0; i < each; ++i) mine += s_bin[bin(bins - 1 - (tid * each + i))];
-      const int incl = wave_scan_incl_i(mine);
-      if (lane == 63) s_sum[wave] = incl;
-      __syncthreads();
-      int upto = incl;
-      for (int v = 0; v < wave; ++v) upto += s_sum[v];
-      if (upto >= left && upto - mine < left) {   // one thread's
-        int before = upto - mine, d = bins - 1 - tid * each;
+      int total;
+      int before = before_me(mine, &total);
+      if (before < left && before + mine >= left) {   // one thread's
+        int d = bins - 1 - tid * each;
         while (before + s_bin[bin(d)] < left) before += s_bin[bin(d--)];
         s_digit = d;
         s_left = left - before;
@@ -189,13 +205,10 @@ __global__ __launch_bounds__(NT) void evict_stay_kernel(EvictParams p) {
       if (same <= 64) {
         for (int span = 0; span < spans; ++span) {
           if (spans > 1) load(span);
-          const int used = stripes(span);
+          const int y0 = first_of(span);
 #pragma unroll
-          for (int i = 0; i < HELD; ++i) {
-            if (i >= used) continue;
-            const int y = f + span * SPAN + i * NT + tid;
-            if (y < end && u[i] >> shift == least) s_near[atomicAdd(&s_count, 1)] = int2{(int)u[i], y};
-          }
+          for (int i = 0; i < HELD; ++i)
+            if (y0 + i < end && u[i] >> shift == least) s_near[atomicAdd(&s_count, 1)] = int2{(int)u[i], y0 + i};
         }
         __syncthreads();
         const int2 c = lane < same ? s_near[lane] : int2{0, 0x7fffffff};   // every wave for itself
@@ -212,105 +225,75 @@ __global__ __launch_bounds__(NT) void evict_stay_kernel(EvictParams p) {
         break;
       }
       by_order = digit == 2;
+      __syncthreads();   // the bins have been looked at
     }
   }
-  // Counts of `kinds` kinds of positions in all stripes and waves become what is in front of each, a wave to a kind; their sums go to s_sum.
-  auto scan = [&](int kinds) {
-    __syncthreads();
-    if (wave < kinds) {
-      int base = 0;
-#pragma unroll
-      for (int c = 0; c < COUNTS; c += 64) {
-        const int n = c + lane < HELD * NW ? s_bin[wave * COUNTS + c + lane] : 0, incl = wave_scan_incl_i(n);
-        s_bin[wave * COUNTS + c + lane] = base + incl - n;
-        base += __builtin_amdgcn_readlane(incl, 63);
-      }
-      if (lane == 0) s_sum[wave] = base;
-    }
-    __syncthreads();
-  };
-  const u64 below = (1ull << lane) - 1ull;
   const bool in_order = w.r > L - w.N;   // the last ones move onto places of their own: the other kernel takes them one run after the other
   int ties = 0, holes = 0, fills = 0, plain = 0;   // so far
   for (int span = 0; span < spans; ++span) {
     if (spans > 1) load(span);
-    const int used = stripes(span);
+    const int y0 = first_of(span);
     unsigned kept = 0;
 #pragma unroll
     for (int i = 0; i < HELD; ++i) {
-      const int y = f + span * SPAN + i * NT + tid;
       const unsigned x = u[i] >> shift;
-      if (y < end && keep > 0 && (x > least || (x == least && y <= last))) kept |= 1u << i;
+      if (y0 + i < end && keep > 0 && (x > least || (x == least && y0 + i <= last))) kept |= 1u << i;
     }
     if (by_order) {
-      __syncthreads();
+      unsigned tie = 0;
 #pragma unroll
-      for (int i = 0; i < HELD; ++i) {
-        const u64 who = i < used ? __ballot(((kept >> i) & 1) && u[i] == least) : 0ull;
-        if (lane == 0) s_bin[i * NW + wave] = __popcll(who);
-      }
-      scan(1);
+      for (int i = 0; i < HELD; ++i)
+        if (((kept >> i) & 1) && u[i] == least) tie |= 1u << i;
+      int all;
+      int at_tie = ties + before_me(__popc(tie), &all);
 #pragma unroll
-      for (int i = 0; i < HELD; ++i) {
-        if (i >= used) continue;
-        const bool tie = ((kept >> i) & 1) && u[i] == least;
-        const u64 who = __ballot(tie);
-        if (tie && ties + s_bin[i * NW + wave] + __popcll(who & below) >= left) kept &= ~(1u << i);
-      }
-      ties += s_sum[0];
+      for (int i = 0; i < HELD; ++i)
+        if ((tie >> i) & 1) {
+          if (at_tie >= left) kept &= ~(1u << i);
+          ++at_tie;
+        }
+      ties += all;
     }
     // three kinds of positions that the lists are made of: places given up below m; kept positions from m on; and, where the last ones come from behind all places, those of
-    // their places that nothing has to leave first
-    auto kind_of = [&](int i) {
-      const int y = f + span * SPAN + i * NT + tid;
-      const bool k = (kept >> i) & 1;
-      if (y >= end) return 3;
-      if (y < m) return k ? 3 : 0;
-      return k ? 1 : (!in_order && y < w.N ? 2 : 3);
-    };
-    __syncthreads();
+    // their places that nothing has to leave first.  Bits of this thread's positions:
+    auto bits_below = [&](int limit) { return limit <= y0 ? 0u : (limit - y0 >= HELD ? (1u << HELD) - 1u : (1u << (limit - y0)) - 1u); };
+    const unsigned there = bits_below(end), low = bits_below(m);
+    const unsigned hole = low & ~kept, fill = kept & ~low, free = in_order ? 0u : there & ~low & ~kept & bits_below(w.N);
+    int all;   // (at most 2^14 of each in a span)
+    const int at_both = before_me(__popc(hole) | __popc(fill) << 16, &all);
+    int h = at_both & 0xffff, q = at_both >> 16;
+    const int n_hole = all & 0xffff, n_fill = all >> 16;
+    const bool in_lds = spans == 1 && n_hole <= WORDS;
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-      const int kind = i < used ? kind_of(i) : 3;
-#pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        const u64 who = __ballot(kind == k);
-        if (lane == 0) s_bin[k * COUNTS + i * NW + wave] = __popcll(who);
+    for (int i = 0; i < HELD; ++i)
+      if ((hole >> i) & 1) {
+        if (in_lds) s_hole[h++] = y0 + i;
+        else list[1 + holes + h++].x = y0 + i;
       }
+    if (!in_lds) {
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if ((fill >> i) & 1) list[1 + fills + q++].y = y0 + i;
     }
-    scan(3);
-    const bool in_lds = spans == 1 && s_sum[0] <= WORDS;
-    int rank[HELD];
+    if (!in_order) {
+      int n_free;
+      int x = plain + before_me(__popc(free), &n_free);
 #pragma unroll
-    for (int i = 0; i < HELD; ++i) {
-      rank[i] = 0;
-      if (i >= used) continue;
-      const int kind = kind_of(i), y = f + span * SPAN + i * NT + tid;
-#pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        const u64 who = __ballot(kind == k);
-        if (kind == k) rank[i] = s_bin[k * COUNTS + i * NW + wave] + __popcll(who & below);
-      }
-      if (kind == 0) {
-        if (in_lds) s_hole[rank[i]] = y;
-        else list[1 + holes + rank[i]].x = y;
-      }
-      if (kind == 1 && !in_lds) list[1 + fills + rank[i]].y = y;
-      if (kind == 2) list[p.most_moves - (plain + rank[i])] = int2{y, y + L - w.N};
-      if (y < m && ((kept >> i) & 1)) out[y] = mass[y];
+      for (int i = 0; i < HELD; ++i)
+        if ((free >> i) & 1) list[p.most_moves - x++] = int2{y0 + i, y0 + i + L - w.N};
+      plain += n_free;
     }
-    holes += s_sum[0];
-    fills += s_sum[1];
-    plain += s_sum[2];
+    holes += n_hole;
+    fills += n_fill;
     if (in_lds) {
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < HELD; ++i) {
-        if (i >= used || kind_of(i) != 1) continue;
-        const int y = f + i * NT + tid, to = s_hole[rank[i]];
-        list[1 + rank[i]] = int2{to, y};
-        out[to] = mass[y];
-      }
+      for (int i = 0; i < HELD; ++i)
+        if ((fill >> i) & 1) {
+          const int to = s_hole[q];
+          list[1 + q++] = int2{to, y0 + i};
+          out[to] = mass[y0 + i];
+        }
       if (tid == 0) list[0] = int2{holes, plain};
       return;
     }
