@@ -22,6 +22,7 @@ struct MassParams {
   paged_mass_args a;
   int group, most_len;   // query heads of a kv head; the longest row that the bounds allow
   int key_blocks;        // workgroups that a row's keys may need
+  int wave_tiles;        // (few query rows) tiles that a wave goes through
   float scale_log2e;
   unsigned group_inv;    // floor(2^32 / group) + 1: a query row's token as a high product (rows times group stay below 2^32); 0 for one head
   int* dev_status;
@@ -118,16 +119,22 @@ __device__ __forceinline__ unsigned load_keys(const MassParams& p, const MassRow
   return there;
 }
 
-// The sums of a wave's groups: lane (l16, g) writes position 16 g + l16 of them.
+// The sums of a wave's groups: lane (l16, g) has position 16 g + l16 of them.
 template <int KW>
-__device__ __forceinline__ void write_sums(const MassParams& p, const MassRow& r, int kvh, int kb, const float (&sum)[KW]) {
-  const int lane = threadIdx.x & 63, g = lane >> 4;
+__device__ __forceinline__ float own_sum(const float (&sum)[KW]) {
+  const int g = (threadIdx.x & 63) >> 4;
   float mine = 0.f;
 #pragma unroll
   for (int kt = 0; kt < KW; ++kt) {
     const float all = rows4_sum(sum[kt]);
     if (g == kt) mine = all;
   }
+  return mine;
+}
+template <int KW>
+__device__ __forceinline__ void write_sums(const MassParams& p, const MassRow& r, int kvh, int kb, const float (&sum)[KW]) {
+  const int lane = threadIdx.x & 63;
+  const float mine = own_sum<KW>(sum);
   const int y = kb + lane;
   if (lane < 16 * KW && y >= r.first && y < r.L) {
     float* m = p.a.mass + r.s * p.a.mass_stride_row + kvh * p.a.mass_stride_head + y;
@@ -135,7 +142,87 @@ __device__ __forceinline__ void write_sums(const MassParams& p, const MassRow& r
   }
 }
 
-// ----------------------------------------------------------------------------------------------------- f32, and bf16 with few query rows
+// ------------------------------------------------------------------------------------------------------------- bf16, few query rows
+// Up to 16 NB query rows (single tokens, accepted paths): bound by the stream of keys.  A wave has a tile or two of 64 positions and everything else that it needs on its way before
+// them - query rows, lse, the sums so far - so one trip to memory follows the place of a tile, and no wave waits for another.  One token of 64 rows x 4200 keys, 8 kv heads
+// of 4, head_dim 128 (568 MB): 116 us = 4.9 TB/s from memory (a large copy: 4.9).
+template <int D, int NB>
+__global__ __launch_bounds__(64 * WAVES, NB == 1 ? 4 : 3) void paged_mass_few_kernel(MassParams p) {
+  constexpr int KW = 4;
+  typedef Operand<uint16_t, D, true> Op;
+  const paged_mass_args& a = p.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4, G = p.group;
+  const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads, kblk = b / a.n_rows;   // (long rows' last tiles come last, from all of them)
+  const MassRow row = row_of(p, b % a.n_rows, kblk == 0 && kvh == 0 && tid == 0);
+  const int lo = row.lo, n = row.n, M = n * G, Lp = row.Lp, W = a.window;
+  const int kb0 = 16 * KW * (WAVES * p.wave_tiles * kblk + wave), kb1 = min(row.L, kb0 + 16 * KW * WAVES * p.wave_tiles);   // tiles WAVES apart
+  if (n == 0 || kb0 >= row.L || kb1 <= row.first) return;
+  auto token_of = [&](int r) { return (int)(p.group_inv ? __umulhi((unsigned)r, p.group_inv) : (unsigned)r); };
+  Op q[NB];
+  float lse[NB][4];
+  int x[NB][4];   // positions of rows 4 g + c; -1: the row counts nothing
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int r = min(16 * nb + l16, M - 1), j = token_of(r);
+    int t = a.source ? a.source[lo + j] : lo + j;
+    if ((unsigned)t >= (unsigned)a.n_source) {
+      if (t != -1) atomicOr(p.dev_status, CASCADE_FLAG_PATH);
+      t = 0;
+    }
+    q[nb].load((const uint16_t*)a.q + t * a.q_stride + (kvh * G + r - j * G) * D, g, D);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const int rc = 16 * nb + 4 * g + c, jc = token_of(min(rc, M - 1)), tc = a.source ? a.source[lo + jc] : lo + jc;
+      x[nb][c] = rc < M && (unsigned)tc < (unsigned)a.n_source ? Lp + jc : -1;
+      lse[nb][c] = a.lse[(long long)max(min(tc, a.n_source - 1), 0) * a.n_heads + kvh * G + min(rc, M - 1) - jc * G];
+    }
+  }
+  bool all_count = true;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      if (!(fabsf(lse[nb][c]) < INFINITY)) x[nb][c] = -1;
+      all_count = all_count && x[nb][c] >= 0;
+      lse[nb][c] *= LOG2E;
+    }
+  all_count = __all(all_count);
+  for (int kb = kb0; kb < kb1; kb += 16 * KW * WAVES) {
+    if (kb + 16 * KW <= row.first) continue;
+    const int y = kb + lane;
+    float* const at = a.mass + row.s * a.mass_stride_row + kvh * a.mass_stride_head + y;
+    const bool wanted = y >= row.first && y < row.L;
+    const float before = wanted && y < Lp ? *at : 0.f;
+    Op key[KW];
+    const unsigned there = load_keys<Op, uint16_t, KW>(p, row, kvh, kb, key);
+    // whether every row sees all of the keys
+    const bool whole = all_count && there == (1u << KW) - 1 && kb + 16 * KW - 1 <= Lp && (W == 0 || Lp + n - 1 - kb < W);
+    float sum[KW];
+#pragma unroll
+    for (int kt = 0; kt < KW; ++kt) {
+      sum[kt] = 0.f;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        if (nb > 0 && 16 * nb >= M) continue;
+        f32x4 w = Op::product(q[nb], key[kt]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          w[c] = fast_exp2(fmaf(w[c], p.scale_log2e, -lse[nb][c]));
+          if (!whole) {
+            const int yk = kb + 16 * kt + l16;
+            const bool seen = yk <= x[nb][c] && (W == 0 || x[nb][c] - yk < W || yk < a.n_sink) && ((there >> kt) & 1);
+            w[c] = seen ? w[c] : 0.f;
+          }
+        }
+        sum[kt] += (w[0] + w[1]) + (w[2] + w[3]);
+      }
+    }
+    const float mine = own_sum<KW>(sum);
+    if (wanted) *at = before + mine;   // (a new token's own: before is 0)
+  }
+}
+
+// -------------------------------------------------------------------------------------------------------------------------------- f32
 // Workgroup = (row, kv head, 64 KW positions), a wave to 16 KW of them.  Query rows come straight from memory, 16 at a time, for each wave.
 template <typename T, int D, int KW, bool VEC>
 __global__ __launch_bounds__(64 * WAVES) void paged_mass_kernel(MassParams p) {
@@ -421,10 +508,22 @@ hipError_t launch_ring(cascade_ctx* ctx, MassParams& p) {
   if (blocks >= 4 * ctx->n_cu) return launch_ring_k<D, 4, SOURCE>(ctx, p);
   return blocks >= ctx->n_cu ? launch_ring_k<D, 2, SOURCE>(ctx, p) : launch_ring_k<D, 1, SOURCE>(ctx, p);
 }
+template <int D, int NB>
+hipError_t launch_few_k(cascade_ctx* ctx, MassParams& p) {
+  const int64_t tiles = (int64_t)p.a.n_rows * p.a.n_kv_heads * ((p.a.max_seq_len + 255) / 256);
+  // Two tiles to a wave spare queries and workgroups, four leave rows of different lengths ends of their own: one token of 64 rows of 2145 keys 66, 62, 61 us with one, two, four; of 90 to 4200
+  // keys 75, 71, 78; paths of 11 tokens, 16 rows x 32 heads of 600 to 2356 keys 53, 51, 49.
+  p.wave_tiles = tiles >= 8 * ctx->n_cu ? 2 : 1;
+  p.key_blocks = (p.a.max_seq_len + 256 * p.wave_tiles - 1) / (256 * p.wave_tiles);
+  KernelTimer t(ctx, CASCADE_K_MASS);
+  CASCADE_TIMED_LAUNCH(t, (paged_mass_few_kernel<D, NB>), dim3((unsigned)((int64_t)p.a.n_rows * p.a.n_kv_heads * p.key_blocks)), dim3(64 * WAVES), 0, ctx->stream, p);
+  return hipGetLastError();
+}
 template <int D>
 hipError_t launch_bf16(cascade_ctx* ctx, MassParams& p) {
   // 64 rows of 8 tokens x 4 heads behind 2000: 60 us straight from memory, 72 through the ring (the stream of keys bounds both); 16 rows of 16 x 4: 22.4 both, head_dim 64 15.2 and 12.8
-  if ((int64_t)p.a.max_new * p.group <= 32) return launch_k<uint16_t, D, 4, true>(ctx, p);
+  const int64_t rows = (int64_t)p.a.max_new * p.group;
+  if (rows <= 32) return rows <= 16 ? launch_few_k<D, 1>(ctx, p) : launch_few_k<D, 2>(ctx, p);
   return p.a.source ? launch_ring<D, true>(ctx, p) : launch_ring<D, false>(ctx, p);
 }
 template <bool VEC>
