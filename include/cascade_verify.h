@@ -638,7 +638,7 @@ int paged_mass(cascade_ctx* ctx, const paged_mass_args* args);
  *     mass, mass_out  element (layer, s, h, y) at layer*mass_stride_layer + s*mass_stride_row + h*mass_stride_head + y, float32, mass_cap positions each; they may not overlap
  *     k_pages, v_pages  strides as for paged_append; head_dim and all strides multiples of 16 bytes, a key at most 4096, buffers on 16-byte boundaries
  *     seq_len_out, free_count_out may not alias their inputs
- *     workspace       of paged_evict_workspace's bytes, 16-byte boundary; calls that may overlap need one each
+ *     workspace       of paged_evict_workspace's bytes (none up to 16384 positions: it may be NULL then), 16-byte boundary; calls that may overlap need one each
  */
 typedef struct {
   cascade_dtype dtype;

@@ -606,10 +606,10 @@ def _paged_evict_record(seq_len, budget, block_table, k_pages, v_pages, mass, ma
 
 
 def paged_evict(ctx: Context, *, seq_len, budget, block_table, k_pages, v_pages, mass, mass_out, free_pages, free_count, seq_len_out, free_count_out, n_first=None,
-                n_recent: int = 0, dropped=None, max_seq_len: int, workspace: torch.Tensor) -> None:
+                n_recent: int = 0, dropped=None, max_seq_len: int, workspace: Optional[torch.Tensor] = None) -> None:
     """k_pages/v_pages [L,pages,Hkv,page_size,D] as for paged_append, positions moved in place; mass/mass_out [L,S,Hkv,positions] float32 (last dim contiguous);
     seq_len/budget/n_first/seq_len_out/dropped [S] int32; block_table [S,width]; free_pages [any], free_count/free_count_out [1].  workspace:
-    paged_evict_workspace bytes."""
+    paged_evict_workspace bytes, if that is not 0."""
     _check(ctx.lib.paged_evict_record(ctx.handle, _paged_evict_record(seq_len, budget, block_table, k_pages, v_pages, mass, mass_out, free_pages, free_count,
                                                                       seq_len_out, free_count_out, n_first, n_recent, dropped, max_seq_len, workspace)))
 

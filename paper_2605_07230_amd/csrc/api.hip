@@ -672,8 +672,9 @@ int paged_evict(cascade_ctx* ctx, const paged_evict_args* a) {
   const int st = check_paged_evict(ctx, a);
   if (st != CASCADE_OK) return st;
   if (a->n_rows == 0 || a->n_layers == 0) return CASCADE_OK;
-  if (!a->workspace) return CASCADE_EINVAL;
-  if (a->workspace_bytes < plan_paged_evict(a)) return CASCADE_ESHAPE;
+  const int64_t lists = plan_paged_evict(a);
+  if (lists > 0 && !a->workspace) return CASCADE_EINVAL;
+  if (a->workspace_bytes < lists) return CASCADE_ESHAPE;
   return on_device(ctx, [&] { return launch_paged_evict(ctx, a); });
 }
 

@@ -86,41 +86,28 @@ __device__ __forceinline__ void give_back(const EvictParams& p, int s) {
   }
 }
 
-// Workgroup = (layer, row, kv head): the pairs of its list, and its weights.
+// What stays of a (layer, row, kv head): the pairs of its list, which lies in LDS (LOCAL) or in the workspace, and, by one workgroup (`lead`), its weights; at: where these begin.
+// Returns how many pairs there are of the first and of the second kind.
 // The weight that decides is found by radix selection of the ranks, 12, 10 and 10 bits: with the whole exponent and three bits of the fraction in the first digit, weights that spread
 // over some octaves spread over the bins.  Once no more than a wave of candidates begin like the one that decides they are ranked against each other, by weight and position, and the
 // other digits are left out.  A thread holds HELD consecutive positions in registers (rows of up to HELD NT positions are read once), so one scan over the threads' counts gives everything
 // its place in the order of positions.
-template <int NT, int HELD>
-__global__ __launch_bounds__(NT) void evict_stay_kernel(EvictParams p) {
+template <int NT, int HELD, bool LOCAL>
+__device__ __forceinline__ int2 decide(const EvictParams& p, const RowPlan& w, long long at, bool lead, int2* pairs, int cap) {
   constexpr int NW = NT / 64, BINS = 4096, WORDS = BINS + BINS / 16, SPAN = HELD * NT;
   typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));   // (such loads need the boundary of a word)
   const paged_evict_args& a = p.a;
   __shared__ int s_bin[WORDS];   // (a word between runs of 16: threads that each go through a run meet in no bank)
-  __shared__ int s_hole[WORDS];  // places given up, where a row has no more of them
   __shared__ int s_sum[2][NW];
   __shared__ int s_digit, s_left, s_same, s_count;
   __shared__ int2 s_near[64];    // candidates: rank, position
   auto bin = [](int i) { return i + (i >> 4); };
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if ((int)blockIdx.x >= p.units) {
-    give_back(p, ((int)blockIdx.x - p.units) * NW + wave);
-    return;
-  }
-  const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads, s = b % a.n_rows, layer = b / a.n_rows;
-  int2* list = p.list + (long long)blockIdx.x * (1 + p.most_moves);
-  const RowPlan w = plan_row(p, s);
   for (int i = tid; i < WORDS; i += NT) s_bin[i] = 0;
   if (tid == 0) s_count = 0;
-  const long long at = layer * a.mass_stride_layer + s * a.mass_stride_row + kvh * a.mass_stride_head;
   const float* mass = a.mass + at;
   float* out = a.mass_out + at;
-  const int L = w.ok ? w.L : 0, f = w.f, m = w.N - w.r, end = L - w.r, keep = m - f;   // `keep` of f .. end - 1; places f .. m - 1
-  if (w.N >= L) {
-    if (tid == 0) list[0] = int2{0, 0};
-    for (int y = tid; y < L; y += NT) out[y] = mass[y];
-    return;
-  }
+  const int L = w.L, f = w.f, m = w.N - w.r, end = L - w.r, keep = m - f;   // `keep` of f .. end - 1; places f .. m - 1
   unsigned u[HELD];
   const int spans = (end - f + SPAN - 1) / SPAN;
   auto first_of = [&](int span) { return f + span * SPAN + HELD * tid; };
@@ -140,8 +127,10 @@ __global__ __launch_bounds__(NT) void evict_stay_kernel(EvictParams p) {
   };
   if (spans == 1) load(0);
   // (places that are given up get the weights that come there below)
-  for (int y = tid; y < m; y += NT) out[y] = mass[y];
-  for (int y = tid; y < w.r; y += NT) out[m + y] = mass[end + y];
+  if (lead) {
+    for (int y = tid; y < m; y += NT) out[y] = mass[y];
+    for (int y = tid; y < w.r; y += NT) out[m + y] = mass[end + y];
+  }
   // what is in front of this thread's counts, and their sum; two buffers in turn, so that one barrier does
   int turn = 0;
   auto before_me = [&](int v, int* total) {
@@ -261,85 +250,58 @@ __global__ __launch_bounds__(NT) void evict_stay_kernel(EvictParams p) {
     const unsigned hole = low & ~kept, fill = kept & ~low, free = in_order ? 0u : there & ~low & ~kept & bits_below(w.N);
     int all;   // (at most 2^14 of each in a span)
     const int at_both = before_me(__popc(hole) | __popc(fill) << 16, &all);
-    int h = at_both & 0xffff, q = at_both >> 16;
-    const int n_hole = all & 0xffff, n_fill = all >> 16;
-    const bool in_lds = spans == 1 && n_hole <= WORDS;
+    int h = holes + (at_both & 0xffff), q = fills + (at_both >> 16);
 #pragma unroll
-    for (int i = 0; i < HELD; ++i)
-      if ((hole >> i) & 1) {
-        if (in_lds) s_hole[h++] = y0 + i;
-        else list[1 + holes + h++].x = y0 + i;
-      }
-    if (!in_lds) {
-#pragma unroll
-      for (int i = 0; i < HELD; ++i)
-        if ((fill >> i) & 1) list[1 + fills + q++].y = y0 + i;
+    for (int i = 0; i < HELD; ++i) {
+      if ((hole >> i) & 1) pairs[h++].x = y0 + i;
+      if ((fill >> i) & 1) pairs[q++].y = y0 + i;
     }
+    holes += all & 0xffff;
+    fills += all >> 16;
     if (!in_order) {
       int n_free;
       int x = plain + before_me(__popc(free), &n_free);
 #pragma unroll
       for (int i = 0; i < HELD; ++i)
-        if ((free >> i) & 1) list[p.most_moves - x++] = int2{y0 + i, y0 + i + L - w.N};
+        if ((free >> i) & 1) pairs[cap - 1 - x++] = int2{y0 + i, y0 + i + L - w.N};
       plain += n_free;
     }
-    holes += n_hole;
-    fills += n_fill;
-    if (in_lds) {
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < HELD; ++i)
-        if ((fill >> i) & 1) {
-          const int to = s_hole[q];
-          list[1 + q++] = int2{to, y0 + i};
-          out[to] = mass[y0 + i];
-        }
-      if (tid == 0) list[0] = int2{holes, plain};
-      return;
-    }
   }
-  if (tid == 0) list[0] = int2{holes, plain};
   __syncthreads();
-  for (int i = tid; i < holes; i += NT) {
-    const int2 pair = list[1 + i];
-    out[pair.x] = mass[pair.y];
-  }
+  if (lead)
+    for (int i = tid; i < holes; i += NT) {
+      const int2 pair = pairs[i];
+      out[pair.x] = mass[pair.y];
+    }
+  return int2{holes, plain};
 }
 
-// Workgroup = (unit, keys or values, part of the moves).
+// The moves of keys or of values of a unit, this workgroup's share of them (`mine` of `splits`).
 // Pairs of the first kind bring a kept position to a place that was given up.  Where it stood may be a place of the last n_recent: then the thread that has taken the old
 // key away brings the new one, and no other has anything to do with it.  The second kind are the other places of the last ones.  So nobody waits for anybody.
 // Only if more of the last ones move than positions go (n_recent > L - N), some move onto places of others of them: then the pairs go first, in workgroups that share the
 // 16-byte pieces of all keys, and the last ones follow in runs, each in registers before its places are written; every later run comes from behind those.
-__global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictParams p) {
+template <int NT>
+__device__ __forceinline__ void move(const EvictParams& p, const RowPlan& w, int layer, int s, int kvh, bool values, int mine, int splits, const int2* list, int cap, int2 counts) {
   const paged_evict_args& a = p.a;
   const int tid = threadIdx.x;
-  int b = blockIdx.x;
-  const int split = b % p.splits;
-  b /= p.splits;
-  const bool values = b & 1;
-  const int unit = b >> 1, kvh = unit % a.n_kv_heads, sl = unit / a.n_kv_heads, s = sl % a.n_rows, layer = sl / a.n_rows;
-  const int2* list = p.list + (long long)unit * (1 + p.most_moves);
-  const int2 counts = list[0];
-  const RowPlan w = plan_row(p, s);
-  if (!w.ok || w.N >= w.L) return;
   const int gone = w.L - w.N;
   const bool in_order = w.r > gone;
-  int pieces = p.pieces, slice = 0, splits = p.splits, mine = split;
+  int pieces = p.pieces, slice = 0;
   if (in_order) {   // whole lines of 128 bytes
-    const int slices = p.pieces % 8 == 0 ? min(p.splits, p.pieces / 8) : 1, per = p.pieces / 8 / max(slices, 1) * 8;
+    const int slices = p.pieces % 8 == 0 ? min(splits, p.pieces / 8) : 1, per = p.pieces / 8 / max(slices, 1) * 8;
     if (slices > 1 && p.pieces % (8 * slices) == 0) {
-      if (split >= slices) return;
+      if (mine >= slices) return;
       pieces = per;
-      slice = split * per;
-    } else if (split > 0) {
+      slice = mine * per;
+    } else if (mine > 0) {
       return;
     }
     splits = 1;
     mine = 0;
   }
   const long long esize = a.dtype == CASCADE_BF16 ? 2 : 4, stride_page = a.stride_page * esize, stride_pos = a.stride_pos * esize;
-  const int each = THREADS / pieces, entry = tid / pieces, piece = tid - entry * pieces;   // keys that the workgroup moves at a time; this thread's
+  const int each = NT / pieces, entry = tid / pieces, piece = tid - entry * pieces;   // keys that the workgroup moves at a time; this thread's
   if (each == 0) return;   // (the host asks for no more pieces than threads)
   const bool idle = entry >= each;
   char* const base = (char*)(values ? a.v_pages : a.k_pages) + (layer * a.stride_layer + kvh * a.stride_head) * esize + 16 * (slice + piece);
@@ -362,7 +324,7 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictParams p) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * each;
-      pair[u] = i < n ? list[i < counts.x ? 1 + i : p.most_moves - (i - counts.x)] : int2{-1, 0};
+      pair[u] = i < n ? list[i < counts.x ? i : cap - 1 - (i - counts.x)] : int2{-1, 0};
     }
   };
   auto look_up = [&]() {
@@ -426,11 +388,76 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictParams p) {
   }
 }
 
+struct Unit {
+  int kvh, s, layer;
+  long long mass;   // where its weights begin
+};
+__device__ __forceinline__ Unit unit_of(const EvictParams& p, int unit) {
+  const paged_evict_args& a = p.a;
+  const int kvh = unit % a.n_kv_heads, sl = unit / a.n_kv_heads, s = sl % a.n_rows, layer = sl / a.n_rows;
+  return Unit{kvh, s, layer, layer * a.mass_stride_layer + s * a.mass_stride_row + kvh * a.mass_stride_head};
+}
+__device__ __forceinline__ void copy_weights(const EvictParams& p, long long at, int n, int threads) {
+  for (int y = threadIdx.x; y < n; y += threads) p.a.mass_out[at + y] = p.a.mass[at + y];
+}
+
+// Rows whose list fits in LDS, all in one launch: the workgroups that share a unit's moves each find out by themselves what stays.
+template <int NT, int HELD>
+__global__ __launch_bounds__(NT, 4) void evict_kernel(EvictParams p) {
+  __shared__ int2 s_pairs[NT * HELD / 2];
+  if ((int)blockIdx.x >= p.units * p.splits) {
+    give_back(p, ((int)blockIdx.x - p.units * p.splits) * (NT / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    return;
+  }
+  const int split = blockIdx.x % p.splits;
+  const Unit unit = unit_of(p, blockIdx.x / p.splits);
+  const RowPlan w = plan_row(p, unit.s);
+  if (!w.ok || w.N >= w.L) {
+    if (w.ok && split == 0) copy_weights(p, unit.mass, w.L, NT);
+    return;
+  }
+  const int2 counts = decide<NT, HELD, true>(p, w, unit.mass, split == 0, s_pairs, NT * HELD / 2);
+  // keys by the even workgroups, values by the odd ones; one alone does both
+  const int shares = max(p.splits >> 1, 1);
+#pragma unroll 1
+  for (int v = p.splits > 1 ? split & 1 : 0; v < 2; v += p.splits > 1 ? 2 : 1)
+    move<NT>(p, w, unit.layer, unit.s, unit.kvh, v, p.splits > 1 ? split >> 1 : 0, shares, s_pairs, NT * HELD / 2, counts);
+}
+
+// Longer rows: the lists go through the workspace, {counts} and the pairs of each unit.
+constexpr int LONG_THREADS = 1024, LONG_HELD = 16;
+__global__ __launch_bounds__(LONG_THREADS) void evict_stay_kernel(EvictParams p) {
+  if ((int)blockIdx.x >= p.units) {
+    give_back(p, ((int)blockIdx.x - p.units) * (LONG_THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    return;
+  }
+  const Unit unit = unit_of(p, blockIdx.x);
+  const RowPlan w = plan_row(p, unit.s);
+  int2* list = p.list + (long long)blockIdx.x * (1 + p.most_moves);
+  if (!w.ok || w.N >= w.L) {
+    if (w.ok) copy_weights(p, unit.mass, w.L, LONG_THREADS);
+    return;
+  }
+  const int2 counts = decide<LONG_THREADS, LONG_HELD, false>(p, w, unit.mass, true, list + 1, p.most_moves);
+  if (threadIdx.x == 0) list[0] = counts;
+}
+__global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictParams p) {
+  const int split = blockIdx.x % p.splits, b = blockIdx.x / p.splits;
+  const Unit unit = unit_of(p, b >> 1);
+  const int2* list = p.list + (long long)(b >> 1) * (1 + p.most_moves);
+  const RowPlan w = plan_row(p, unit.s);
+  if (!w.ok || w.N >= w.L) return;
+  move<THREADS>(p, w, unit.layer, unit.s, unit.kvh, b & 1, split, p.splits, list + 1, p.most_moves, list[0]);
+}
+
 int most_moves(const paged_evict_args* a) { return a->max_seq_len / 2; }   // as many places as positions: at most half of them together
+
+constexpr int MOST_LOCAL = 1024 * 16;   // positions of a row whose list fits in LDS
 
 }  // namespace
 
 int64_t plan_paged_evict(const paged_evict_args* a) {
+  if (a->max_seq_len <= MOST_LOCAL) return 0;
   return (int64_t)a->n_layers * a->n_rows * a->n_kv_heads * (1 + most_moves(a)) * (int64_t)sizeof(int2);
 }
 
@@ -445,15 +472,23 @@ hipError_t launch_paged_evict(cascade_ctx* ctx, const paged_evict_args* a) {
   p.pieces = a->head_dim * (a->dtype == CASCADE_BF16 ? 2 : 4) / 16;
   const int page16 = a->page_size / 16;
   p.page16_inv = page16 == 1 ? 0u : (unsigned)((1ull << 32) / page16 + 1);
-  {
-    auto run = [&](auto kernel, int nt) {
-      const int waves = nt / 64;
+  auto waves_of_rows = [&](int nt) { return (a->n_rows + nt / 64 - 1) / (nt / 64); };
+  if (a->max_seq_len <= MOST_LOCAL) {
+    auto run = [&](auto kernel, int nt, int per_cu) {
+      // an even number of workgroups to a unit, as many as the chip holds at a time, with 64 keys to move at least
+      const int64_t want = std::min<int64_t>((int64_t)per_cu * ctx->n_cu / p.units, 2 * ((p.most_moves + 63) / 64));
+      p.splits = want < 2 ? 1 : (int)(want / 2 * 2);
       KernelTimer t(ctx, CASCADE_K_EVICT);
-      CASCADE_TIMED_LAUNCH(t, kernel, dim3((unsigned)(p.units + (a->n_rows + waves - 1) / waves)), dim3(nt), 0, ctx->stream, p);
+      CASCADE_TIMED_LAUNCH(t, kernel, dim3((unsigned)(p.units * p.splits + waves_of_rows(nt))), dim3(nt), 0, ctx->stream, p);
+      return hipGetLastError();
     };
-    if (a->max_seq_len <= 4 * 256) run(evict_stay_kernel<256, 4>, 256);
-    else if (a->max_seq_len <= 8 * 512) run(evict_stay_kernel<512, 8>, 512);
-    else run(evict_stay_kernel<1024, 16>, 1024);
+    if (a->max_seq_len <= 4 * 256) return run(evict_kernel<256, 4>, 256, 4);
+    if (a->max_seq_len <= 8 * 512) return run(evict_kernel<512, 8>, 512, 2);
+    return run(evict_kernel<1024, 16>, 1024, 1);
+  }
+  {
+    KernelTimer t(ctx, CASCADE_K_EVICT);
+    CASCADE_TIMED_LAUNCH(t, evict_stay_kernel, dim3((unsigned)(p.units + waves_of_rows(LONG_THREADS))), dim3(LONG_THREADS), 0, ctx->stream, p);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -165,15 +165,17 @@ class Evict:
         self.was = [t.clone() for t in (self.k_pages, self.v_pages, self.mass)]
 
     def context(self, stream=None):
-        return binding.Context(max_rows=len(self.length), max_nodes_total=1, max_nodes_per_tree=1, max_prefix=max(1, max(self.length)), n_heads=8,
+        return binding.Context(max_rows=len(self.length), max_nodes_total=1, max_nodes_per_tree=1, max_prefix=max(1, self.args["max_seq_len"]), n_heads=8,
                                head_dim=self.k_pages.shape[4], hidden=64, vocab=64, stream=stream)
 
     def workspace(self, ctx, **more):
-        return torch.empty(max(16, binding.paged_evict_workspace(ctx, **{**self.args, **more})), dtype=torch.uint8, device="cuda")
+        size = binding.paged_evict_workspace(ctx, **{**self.args, **{k: v for k, v in more.items() if k != "workspace"}})
+        return torch.empty(size, dtype=torch.uint8, device="cuda") if size else None
 
     def run(self, ctx=None, **more):
         ctx = ctx or self.context()
-        more.setdefault("workspace", self.workspace(ctx, **more))
+        if "workspace" not in more:
+            more["workspace"] = self.workspace(ctx, **more)
         binding.paged_evict(ctx, **{**self.args, **more})
         torch.cuda.synchronize()
 

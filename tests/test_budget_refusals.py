@@ -112,10 +112,14 @@ def test_evict(lib, ctx):
                + [(S, {k: v}) for k, v in (("n_rows", 5), ("max_seq_len", 1001), ("page_size", 24), ("head_dim", 4), ("stride_layer", 12), ("stride_pos", -8), ("mass_stride_layer", 999),
                                            ("mass_stride_row", 999), ("mass_stride_head", 999), ("mass_stride_head", -1), ("n_layers", 1 << 20), ("n_pages", 1 << 28))]
                + [(S, dict(table_width=1 << 28, table_stride=1 << 28)), (B.OK, dict(n_rows=0)), (B.OK, dict(n_layers=0))])
-    _refused(lib.paged_evict, ctx, r, changes + [(E, dict(workspace=None)), (S, dict(workspace_bytes=100))])
+    _refused(lib.paged_evict, ctx, r, changes)
     n = C.c_int64()
     _refused(lambda c, a: lib.paged_evict_workspace(c, a, C.byref(n)), ctx, r, changes)
-    assert lib.paged_evict_workspace(C.addressof(ctx), C.byref(r), C.byref(n)) == B.OK and n.value >= 2 * 4 * 2 * 500 * 8
+    assert lib.paged_evict_workspace(C.addressof(ctx), C.byref(r), C.byref(n)) == B.OK and n.value == 0
+    long = _context(4, 64, 32, 20000, 8, 128)
+    r.max_seq_len = 20000
+    assert lib.paged_evict_workspace(C.addressof(long), C.byref(r), C.byref(n)) == B.OK and n.value >= 2 * 4 * 2 * 10000 * 8
+    _refused(lib.paged_evict, long, r, [(E, dict(workspace=None)), (S, dict(workspace_bytes=n.value - 1)), (B.OK, dict(n_rows=0))])
 
 
 def test_cuts():

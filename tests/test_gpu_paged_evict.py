@@ -36,6 +36,13 @@ CASES = {
     "memory by position": dict(length=[300, 90], budget=[200, 80], recent=20, order=(0, 1, 3, 2, 4)),
     "memory by page": dict(length=[300, 90], budget=[200, 80], recent=20, order=(1, 0, 2, 3, 4)),
     "large pages": dict(length=[3000, 900], budget=[1200, 1024], recent=20, page=1024),
+    "very long": dict(length=[20000, 100], budget=[9000, 60], layers=1, kv_heads=2, page=64, recent=50, first=[7, 0], levels=1 << 20),
+    "very long, many go": dict(length=[40000], budget=[300], layers=1, kv_heads=1, page=128, recent=299, levels=3),
+    "very long, few go": dict(length=[17000], budget=[16990], layers=1, kv_heads=1, page=128, recent=300, levels=1 << 20),
+    "very long, as bound": dict(length=[33, 70], budget=[20, 50], most=17000, recent=3),
+    "sixteen thousand": dict(length=[16384, 4097], budget=[8000, 4000], layers=1, kv_heads=1, page=128, recent=10, levels=1 << 20),
+    "sixteen thousand, equal": dict(length=[16384], budget=[8192], layers=1, kv_heads=1, page=128, levels=1),
+    "four thousand, in order": dict(length=[4096, 4000], budget=[4000, 3990], layers=1, kv_heads=2, recent=2000, levels=1 << 20),
     "many rows": dict(length=[20 + 3 * i for i in range(70)], budget=[10 + i for i in range(70)], layers=1, kv_heads=1, recent=2),
 }
 
@@ -44,7 +51,9 @@ CASES = {
 def test_against_the_oracle(name):
     kw = dict(CASES[name])
     print(f"[paged_evict] {name}: {kw}", flush=True)
-    p = Evict(list(CASES).index(name), kw.pop("length"), kw.pop("budget"), **kw)
+    most = kw.pop("most", 0)
+    p = Evict(list(CASES).index(name), kw.pop("length"), kw.pop("budget"), **kw, cap=most or None)
+    p.args["max_seq_len"] = max(p.args["max_seq_len"], most)
     ctx = p.context()
     p.run(ctx)
     assert ctx.device_status() == binding.OK
@@ -138,7 +147,7 @@ def test_lists_that_have_no_room():
 
 def test_without_what_may_be_missing():
     p = Evict(25, [300, 90], [200, 80], recent=20)
-    p.run(dropped=None)
+    p.run(dropped=None, workspace=None)
     p.args["dropped"].copy_(dev([100, 10]))
     p.check()
 
@@ -146,29 +155,33 @@ def test_without_what_may_be_missing():
 def test_refusals():
     p = Evict(26, [300, 90], [200, 80], recent=20)
     ctx = p.context()
-    rec = binding._paged_evict_record(**p.args, workspace=p.workspace(ctx))
-    keep = p.workspace(ctx)
+    keep = torch.empty(4096, dtype=torch.uint8, device="cuda")
+    rec = binding._paged_evict_record(**p.args, workspace=keep)
 
     def call(**fields):
         a = binding.paged_evict_args.from_buffer_copy(rec)
-        a.workspace = keep.data_ptr()
         for k, v in fields.items():
             setattr(a, k, v)
         return ctx.lib.paged_evict(ctx.handle, C.byref(a))
 
     E = binding
-    for k in ("seq_len", "budget", "mass", "mass_out", "k_pages", "v_pages", "block_table", "free_pages", "free_count", "free_count_out", "seq_len_out", "workspace"):
+    for k in ("seq_len", "budget", "mass", "mass_out", "k_pages", "v_pages", "block_table", "free_pages", "free_count", "free_count_out", "seq_len_out"):
         assert call(**{k: None}) == E.EINVAL, k
     for k in ("n_layers", "n_rows", "n_recent", "max_seq_len", "mass_cap", "free_capacity", "n_pages", "table_width", "workspace_bytes"):
         assert call(**{k: -1}) == E.EINVAL, k
     assert call(dtype=2) == E.EDTYPE
     for k, v in (("page_size", 24), ("head_dim", 4), ("stride_pos", 4), ("stride_layer", -8), ("n_rows", 3), ("max_seq_len", 301), ("mass_stride_head", 3), ("mass_stride_row", 3),
-                 ("mass_stride_layer", 3), ("workspace_bytes", 64)):
+                 ("mass_stride_layer", 3)):
         assert call(**{k: v}) == E.ESHAPE, (k, v)
     for k, other in (("mass_out", "mass"), ("seq_len_out", "seq_len"), ("free_count_out", "free_count")):
         assert call(**{k: getattr(binding.paged_evict_args.from_buffer_copy(rec), other)}) == E.EINVAL, k
     for k in ("k_pages", "v_pages", "workspace"):
         assert call(**{k: getattr(binding.paged_evict_args.from_buffer_copy(rec), k) + 8}) == E.EINVAL, k
     assert call(n_rows=0) == E.OK and call(n_layers=0) == E.OK
+    p = Evict(27, [17000], [200])
+    ctx = p.context()
+    rec = binding._paged_evict_record(**p.args, workspace=None)
+    assert call(workspace=None) == E.EINVAL and call(workspace=keep.data_ptr(), workspace_bytes=64) == E.ESHAPE
+    p = Evict(26, [300, 90], [200, 80], recent=20)
     torch.cuda.synchronize()
     assert torch.equal(p.k_pages.view(torch.int16), p.was[0].view(torch.int16)) and (p.mass_out == -7).all() and ctx.device_status() == E.OK
