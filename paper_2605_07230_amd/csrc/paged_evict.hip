@@ -306,85 +306,69 @@ __device__ __forceinline__ void move(const EvictParams& p, const RowPlan& w, int
   const bool idle = entry >= each;
   char* const base = (char*)(values ? a.v_pages : a.k_pages) + (layer * a.stride_layer + kvh * a.stride_head) * esize + 16 * (slice + piece);
   const int32_t* table = a.block_table + s * a.table_stride;
-  auto place = [&](int y) -> char* {   // nullptr: outside the pool
-    const int e = page_index(p, y), page = table[e];
-    if ((unsigned)page >= (unsigned)a.n_pages) {
-      atomicOr(p.dev_status, CASCADE_FLAG_PAGE);
-      return nullptr;
-    }
-    return base + page * stride_page + (y - e * a.page_size) * stride_pos;
+  auto at = [&](int page, int y) {   // (outside the pool: its first page)
+    return base + ((unsigned)page < (unsigned)a.n_pages ? page : 0) * stride_page + (y - page_index(p, y) * a.page_size) * stride_pos;
+  };
+  auto good = [&](int from, int to) {
+    const bool ok = (unsigned)from < (unsigned)a.n_pages && (unsigned)to < (unsigned)a.n_pages;
+    if (!ok) atomicOr(p.dev_status, CASCADE_FLAG_PAGE);
+    return ok;
   };
   constexpr int U = 4;
   const int n = counts.x + (in_order ? 0 : counts.y), step = splits * U * each;
-  // A round's keys are on their way while the next round's places are looked up and the pairs of the one after that are read.
-  int2 pair[U];   // x < 0: none
-  char *to[U], *from[U];
-  const char* next[U];
-  auto read_pairs = [&](int i0) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * each;
-      pair[u] = i < n ? list[i < counts.x ? i : cap - 1 - (i - counts.x)] : int2{-1, 0};
-    }
-  };
-  auto look_up = [&]() {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      to[u] = from[u] = nullptr;
-      next[u] = nullptr;
-      if (pair[u].x >= 0) {
-        from[u] = place(pair[u].y);
-        to[u] = place(pair[u].x);
-        if (!in_order && pair[u].y < w.N) next[u] = place(pair[u].y + gone);
-      }
-    }
-  };
-  if (!idle) {
-    int i0 = mine * U * each + entry;
-    read_pairs(i0);
-    look_up();
-    read_pairs(i0 + step);
-    for (; i0 < n; i0 += step) {
-      u32x4 x[U], then[U];
-      char *here[U], *there[U];
-      bool chain[U];
+  // (Loads without conditions, so that a round's are on their way together: behind the last pair that one again, outside the pool its first page; what must not be written is not.)
+  if (!idle)
+    for (int i0 = mine * U * each + entry; i0 < n; i0 += step) {
+      u32x4 x[U];
+      int2 pair[U];
+      int from_page[U], to_page[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        here[u] = from[u] ? to[u] : nullptr;
-        there[u] = from[u];
-        chain[u] = from[u] && next[u];
-        if (here[u]) x[u] = *(const u32x4*)from[u];
-        if (chain[u]) then[u] = *(const u32x4*)next[u];
+        const int i = min(i0 + u * each, n - 1);
+        pair[u] = list[i < counts.x ? i : cap - 1 - (i - counts.x)];
       }
-      look_up();
-      read_pairs(i0 + 2 * step);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (here[u]) *(u32x4*)here[u] = x[u];
-        if (chain[u]) *(u32x4*)there[u] = then[u];
+        from_page[u] = table[page_index(p, pair[u].y)];
+        to_page[u] = table[page_index(p, pair[u].x)];
       }
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = *(const u32x4*)at(from_page[u], pair[u].y);
+      bool chain = false;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (i0 + u * each < n && good(from_page[u], to_page[u])) *(u32x4*)at(to_page[u], pair[u].x) = x[u];
+        chain |= !in_order && pair[u].y < w.N;
+      }
+      if (chain)   // places that these keys have left and that the last ones come to
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (i0 + u * each < n && pair[u].y < w.N) {
+            const int page = table[page_index(p, pair[u].y + gone)];
+            if (good(from_page[u], page)) *(u32x4*)at(from_page[u], pair[u].y) = *(const u32x4*)at(page, pair[u].y + gone);
+          }
     }
-  }
   if (!in_order) return;
   __syncthreads();
   const int m = w.N - w.r, end = w.L - w.r;
   for (int i0 = 0; i0 < w.r; i0 += U * each) {
     u32x4 x[U];
+    int from_page[U], to_page[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * each + entry;
-      to[u] = nullptr;
-      if (i < w.r && !idle) {
-        const char* from = place(end + i);
-        to[u] = from ? place(m + i) : nullptr;
-        if (to[u]) x[u] = *(const u32x4*)from;
-      }
+      const int i = min(i0 + u * each + entry, w.r - 1);
+      from_page[u] = table[page_index(p, end + i)];
+      to_page[u] = table[page_index(p, m + i)];
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = *(const u32x4*)at(from_page[u], end + min(i0 + u * each + entry, w.r - 1));
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the run is in registers
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (to[u]) *(u32x4*)to[u] = x[u];
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * each + entry;
+      if (!idle && i < w.r && good(from_page[u], to_page[u])) *(u32x4*)at(to_page[u], m + i) = x[u];
+    }
   }
 }
 
