@@ -123,9 +123,10 @@ def test_which_calls_share():
                                        max_shared_len=max(0, min(max(kw["shared"]), max(kw["prefix"]))), n_heads=kw["heads"], n_kv_heads=kw["kv_heads"],
                                        head_dim=kw.get("head_dim", 128), tree="tree" in kw, window=kw.get("window", 0), dtype=binding.BF16 if bf16 else binding.F32)
         assert (cut[1] > 0) == (name not in ALONE), (name, cut)
-    # both shapes of workgroups, one part and many
-    assert {binding.paged_shared_cut(n_rows=r, n_groups=1, n_tokens=r * t, max_new=t, max_prefix_len=4200, max_shared_len=4096, n_heads=32, n_kv_heads=8, head_dim=128)[:2]
-            for r, t in ((64, 1), (64, 4), (500, 4))} == {(64, 4), (64, 2), (128, 2)}
+    # both shapes of workgroups, few parts and many
+    cuts = [binding.paged_shared_cut(n_rows=r, n_groups=1, n_tokens=r * t, max_new=t, max_prefix_len=4200, max_shared_len=4096, n_heads=32, n_kv_heads=8, head_dim=128)[:2]
+            for r, t in ((8, 1), (64, 1), (500, 4))]
+    assert {c[0] for c in cuts} == {64, 128} and cuts[0][1] > cuts[1][1] > 1
 
 
 def small(dtype, seed):
