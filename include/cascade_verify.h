@@ -130,8 +130,8 @@ typedef enum {
   CASCADE_K_PAGED_MERGE = 12, /* their merge of keys in parts */
   CASCADE_K_SAMPLE = 13,     /* sample_tokens */
   CASCADE_K_MASS = 14,       /* paged_mass */
-  CASCADE_K_EVICT = 15,      /* paged_evict: what stays */
-  CASCADE_K_EVICT_MOVE = 16, /* paged_evict: the moves */
+  CASCADE_K_EVICT = 15,      /* paged_evict; of more than 16384 positions: what stays */
+  CASCADE_K_EVICT_MOVE = 16, /* the moves of such a call */
   CASCADE_K_COUNT = 17
 } cascade_kernel_id;
 int cascade_set_kernel_timing(cascade_ctx* ctx, int enable);
@@ -633,7 +633,7 @@ int paged_mass(cascade_ctx* ctx, const paged_mass_args* args);
  * Heads and layers of a row keep positions of their own, so what stands at a place of the cache has no common position any more: attention over the row takes no window,
  * and keys carry what they need to know of their positions.  Pages that rows share (paged_attn_shared) have to lie in the first n_first positions of each.
  * NaN counts as less than any mass.  A negative n_first or budget counts as 0.  A row whose length is negative or larger than max_seq_len, its table or mass_cap is left as it is
- * (seq_len_out = L, dropped 0, nothing of mass_out) and sets the flag.  Places whose page lies outside the pool are neither read nor written and set the flag; the entries
+ * (seq_len_out = L, dropped 0, nothing of mass_out) and sets the flag.  What would move from or to a page outside the pool does not, and sets the flag; the entries
  * are given back as they stand.  A free_count outside the list, or one behind which the entries have no room, sets it too: what has no place is not written.
  *     mass, mass_out  element (layer, s, h, y) at layer*mass_stride_layer + s*mass_stride_row + h*mass_stride_head + y, float32, mass_cap positions each; they may not overlap
  *     k_pages, v_pages  strides as for paged_append; head_dim and all strides multiples of 16 bytes, a key at most 4096, buffers on 16-byte boundaries

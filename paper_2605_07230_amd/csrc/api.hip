@@ -612,9 +612,9 @@ static int check_paged_mass(const cascade_ctx* ctx, const paged_mass_args* a) {
   if (a->n_rows > L.max_rows || a->n_tokens > L.max_nodes_total || a->n_source > L.max_nodes_total || a->max_seq_len > L.max_prefix || a->n_heads > L.n_heads ||
       a->head_dim > L.head_dim)
     return CASCADE_ESHAPE;
-  // query rows of a row and what a launch counts stay below 2^30 (256 threads to 64 keys at least)
+  // query rows of a row and what a launch counts stay below 2^31 (256 threads to 64 keys at least; bf16: to 256, but for calls that are smaller than the chip)
   if (a->max_seq_len > (1 << 30) || ((double)a->max_new + 256.0) * (a->n_heads / a->n_kv_heads) * (a->n_heads / a->n_kv_heads) >= 4294967296.0 || a->max_new > (1 << 29) || (int64_t)a->n_tokens * a->n_heads > (1 << 30) ||
-      (double)a->n_rows * a->n_kv_heads * ((a->max_seq_len + 63) / 64) > (double)(1 << 23))
+      (double)a->n_rows * a->n_kv_heads * (a->dtype == CASCADE_BF16 ? (a->max_seq_len + 255) / 256 : (a->max_seq_len + 63) / 64) > (double)(1 << 23))
     return CASCADE_ESHAPE;
   if (a->dtype == CASCADE_BF16) {
     if (a->head_dim != 64 && a->head_dim != 128) return CASCADE_ESHAPE;
