@@ -356,7 +356,35 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_mass_ring_kernel(MassPara
   wg_from &= ~(QB - 1);
 
   const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(size_t)many_smem);
+  // Whole blocks of tokens in a row, whose heads divide a block: a lane's rows lie at constant distances from the block's first (per block no vector instruction but the loads)
+  const bool regular = !SOURCE && QB % G == 0 && a.q_stride <= (1 << 24);
+  const int block_tokens = QB / G;
+  unsigned q_at[GM::LPW], lse_at;
+#pragma unroll
+  for (int i = 0; i < GM::LPW; ++i) {
+    const int in = (GM::LPW * wave + i) * GM::RPL + lane / GM::PPR, j = token_of(in);
+    q_at[i] = 2u * (unsigned)(j * (int)min(a.q_stride, (int64_t)1 << 24) + (in - j * G) * D + 8 * ((lane % GM::PPR) ^ GM::swz(in)));
+  }
+  {
+    const int j = token_of(lane);
+    lse_at = 4u * (unsigned)(j * a.n_heads + lane - j * G);
+  }
   auto request = [&](int r0, int stage) {   // (rows behind the last: that one again, and nothing for its lse)
+    if (regular && r0 + QB <= M) {
+      const long long t = lo + (long long)(r0 / QB) * block_tokens;   // (r0 is a multiple of QB)
+      const uintptr_t qs = (uintptr_t)((const uint16_t*)a.q + t * a.q_stride + kvh * G * D), ls = (uintptr_t)(a.lse + t * a.n_heads + kvh * G);
+      const auto uniform = [](uintptr_t x) {
+        return (const char*)(((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)x));
+      };
+#pragma unroll
+      for (int i = 0; i < GM::LPW; ++i) {
+        const unsigned l = lds0 + stage * GM::BLOCK + (GM::LPW * wave + i) * 1024;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(l), "v"(q_at[i]), "s"(uniform(qs)) : "memory");
+      }
+      const unsigned l = lds0 + STAGES * GM::BLOCK + stage * GM::LSE + wave * (QB * 4);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(l), "v"(lse_at), "s"(uniform(ls)) : "memory");
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < GM::LPW; ++i) {
       const int in = (GM::LPW * wave + i) * GM::RPL + lane / GM::PPR, r = min(r0 + in, M - 1), j = token_of(r);
