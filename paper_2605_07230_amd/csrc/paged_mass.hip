@@ -419,16 +419,18 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_mass_ring_kernel(MassPara
     if (r0 + QB <= from || r0 >= to) return;
     const uint16_t* qs = (const uint16_t*)(many_smem + ST * GM::BLOCK);
     float* ls = (float*)(many_smem + STAGES * GM::BLOCK + ST * GM::LSE) + wave * QB;
+    int own_at = 8 * (g ^ GM::swz(l16));
     auto operand = [&](Op& q, int qb) {
+      if constexpr (D == 128 && KG == 4) asm volatile("" : "+v"(own_at));   // (piece 4 ks + g is one xor away: these addresses, held for every ks, spilled here, and are faster held elsewhere)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) q.x[ks] = *(const bf16x8*)(qs + (16 * qb + l16) * D + 8 * ((4 * ks + g) ^ GM::swz(l16)));
+      for (int ks = 0; ks < KS; ++ks) q.x[ks] = *(const bf16x8*)(qs + (16 * qb + l16) * D + (own_at ^ 32 * ks));
     };
     // whether every row sees all of the wave's keys
     const int rows = min(QB, M - r0), x0 = Lp + token_of(r0), x1 = Lp + token_of(r0 + rows - 1);
     const float mine = ls[lane] * LOG2E;   // (the wave's own copy)
     ls[lane] = mine;
     __builtin_amdgcn_wave_barrier();
-    const bool whole = __all(fabsf(mine) < INFINITY) && there == (1u << KW) - 1 && kb + 16 * KW - 1 <= x0 && (W == 0 || x1 - kb < W);
+    const bool all_count = __all(fabsf(mine) < INFINITY), whole = all_count && there == (1u << KW) - 1 && kb + 16 * KW - 1 <= x0 && (W == 0 || x1 - kb < W);
     if (whole) {
       // the products of the next 16 rows stand among the exponentials of these
       Op q[2];
@@ -454,6 +456,9 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_mass_ring_kernel(MassPara
 #pragma unroll 1
       for (int i = 0; i < NQ; ++i) {
         const int qb = NQ * qw + i, r = r0 + 16 * qb + 4 * g;
+        if (r0 + 16 * qb >= M) break;
+        const int x_lo = Lp + token_of(r0 + 16 * qb), x_hi = Lp + token_of(min(r0 + 16 * qb + 15, M - 1));   // positions of these rows
+        if (kb > x_hi) continue;
         Op q;
         operand(q, qb);
         const f32x4 lse = *(const f32x4*)(ls + 16 * qb + 4 * g);
@@ -462,14 +467,18 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_mass_ring_kernel(MassPara
         for (int c = 0; c < 4; ++c) at[c] = fabsf(lse[c]) < INFINITY ? Lp + token_of(r + c) : -1;
 #pragma unroll
         for (int kt = 0; kt < KW; ++kt) {
-          const int y = kb + 16 * kt + l16;
+          const int y0 = kb + 16 * kt, y = y0 + l16;
+          if (y0 > x_hi || !((there >> kt) & 1)) continue;   // none of them sees any of these keys
           const f32x4 w = Op::product(q, key[kt]);
           f32x4 e;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const bool seen = y <= at[c] && (W == 0 || at[c] - y < W || y < a.n_sink) && ((there >> kt) & 1);
-            e[c] = seen ? fast_exp2(fmaf(w[c], p.scale_log2e, -lse[c])) : 0.f;
-          }
+          for (int c = 0; c < 4; ++c) e[c] = fast_exp2(fmaf(w[c], p.scale_log2e, -lse[c]));
+          if (!all_count || y0 + 15 > x_lo || (W > 0 && x_hi - y0 >= W))
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const bool seen = y <= at[c] && (W == 0 || at[c] - y < W || y < a.n_sink);
+              e[c] = seen ? e[c] : 0.f;
+            }
           sum[kt] += (e[0] + e[1]) + (e[2] + e[3]);
         }
       }
@@ -530,8 +539,9 @@ hipError_t launch_ring_k(cascade_ctx* ctx, MassParams& p) {
 }
 template <int D, bool SOURCE>
 hipError_t launch_ring(cascade_ctx* ctx, MassParams& p) {
-  // Wider workgroups read the queries less often, narrower ones fill the chip.  Prompts of 16 rows x 1000 tokens behind 1000, 8 kv heads of 4 (1024 workgroups of 256 positions):
-  // 293 us with 256 positions, 310 with 128, 393 with 64; 8 rows x 300 behind 1000 (384): 94, 59, 60; 8 rows x 100 behind 500 (192): 64 positions 22.
+  // Wider workgroups read the queries less often, narrower ones fill the chip.  With 256, 128 and 64 positions, prompts of 8 kv heads of 4: 16 rows x 1000 tokens behind 3000 (2048
+  // workgroups of 256 positions) 548, 581, 781 us; 32 x 100 behind 1000 (1280) 58, 68, 103; 16 x 1000 behind 1000 (1024) 273, 279, 347; rows of 500 to 1000 behind up to 2000 (768)
+  // 166, 120, 128; 8 x 300 behind 1000 (384) 74, 50, 54; 8 x 100 behind 500 (192) 24, 21, 22, with head_dim 64 (384) 64, 42, 37.
   const int64_t blocks = (int64_t)p.a.n_rows * p.a.n_kv_heads * ((p.a.max_seq_len + 255) / 256);
   if (blocks >= 4 * ctx->n_cu) return launch_ring_k<D, 4, SOURCE>(ctx, p);
   return blocks >= ctx->n_cu ? launch_ring_k<D, 2, SOURCE>(ctx, p) : launch_ring_k<D, 1, SOURCE>(ctx, p);

@@ -12,8 +12,7 @@ def test_hand_written_assembly(src, tmp_path):
     stats, text = _kernel_stats(src, tmp_path)
     bodies = re.findall(r"^(_ZN\S*_kernel\S*):[^\n]*\n(.*?)\.amdhsa_kernel", text, flags=re.S | re.M)
     assert len(stats) == len(bodies) > 0
-    # three workgroups to a compute unit leave 168 registers: 256 positions at head_dim 128 need four more, for what a block begins with
-    assert not [(name, spilled) for name, spilled in stats if int(spilled) > (4 if "ring_kernelILi128ELi4" in name else 0)]
+    assert not [(name, spilled) for name, spilled in stats if int(spilled) > 0]
     for name, body in bodies:
         m0 = [l.strip() for l in body.splitlines() if re.search(r"\bm0\b", l)]
         assert all(l.startswith("s_mov_b32 m0,") for l in m0), (name, m0[:5])
