@@ -589,7 +589,7 @@ int cascade_paged_shared(const cascade_ctx* ctx, const paged_shared_args* args, 
  * negative or larger than max_seq_len, its table or mass_cap, is left as it is and sets the flag, as do entries of the table outside the pool (their positions get nothing).
  * Scores and sums are float32, in an order that depends on nothing but the call's sizes.
  *     q, lse       as in paged_attn, n_source packed tokens;  k_pages, block_table likewise (the call is one layer's)
- *     mass         element (s, h, y) at s*mass_stride_row + h*mass_stride_head + y, float32, mass_cap positions each
+ *     mass         element (s, h, y) at s*mass_stride_row + h*mass_stride_head + y, float32, mass_cap positions each; rows and heads lie apart
  * bf16: head_dim 64 or 128, strides multiples of 8 elements, buffers on 16-byte boundaries.  f32: any head_dim up to 256.
  */
 typedef struct {
@@ -637,7 +637,7 @@ int paged_mass(cascade_ctx* ctx, const paged_mass_args* args);
  * are given back as they stand.  A free_count outside the list, or one behind which the entries have no room, sets it too: what has no place is not written.
  *     mass, mass_out  element (layer, s, h, y) at layer*mass_stride_layer + s*mass_stride_row + h*mass_stride_head + y, float32, mass_cap positions each; they may not overlap
  *     k_pages, v_pages  strides as for paged_append; head_dim and all strides multiples of 16 bytes, a key at most 4096, buffers on 16-byte boundaries
- *     seq_len_out, free_count_out may not alias their inputs
+ *     seq_len_out, dropped and free_count_out may not alias inputs or each other, nor v_pages k_pages; rows, heads, layers and pages lie apart
  *     workspace       of paged_evict_workspace's bytes (none up to 16384 positions: it may be NULL then), 16-byte boundary; calls that may overlap need one each
  */
 typedef struct {

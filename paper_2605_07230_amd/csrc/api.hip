@@ -5,8 +5,11 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
+#include <initializer_list>
 #include <mutex>
 #include <new>
+#include <utility>
 
 #include "common.h"
 
@@ -591,6 +594,20 @@ int cascade_paged_shared(const cascade_ctx* ctx, const paged_shared_args* a, int
   return CASCADE_OK;
 }
 
+// whether what `n` dimensions of (stride, count) count, `extent` elements each, lies apart: from the smallest stride up, each one passes all that is inside it
+static bool lies_apart(std::initializer_list<std::pair<int64_t, int64_t>> dims, int64_t extent) {
+  std::pair<int64_t, int64_t> d[4];
+  int n = 0;
+  for (const auto& x : dims)
+    if (x.second > 1) d[n++] = x;
+  std::sort(d, d + n);
+  for (int i = 0; i < n; ++i) {
+    if (d[i].first < extent || d[i].first > INT64_MAX / d[i].second / 2) return false;
+    extent += d[i].first * (d[i].second - 1);
+  }
+  return true;
+}
+
 static int check_paged_mass(const cascade_ctx* ctx, const paged_mass_args* a) {
   const bool some = a->n_rows != 0 && a->n_tokens != 0;
   if (some && (!a->q_off || !a->seq_len || !a->q || !a->lse || !a->k_pages || !a->block_table || !a->mass || a->n_pages == 0)) return CASCADE_EINVAL;
@@ -605,9 +622,7 @@ static int check_paged_mass(const cascade_ctx* ctx, const paged_mass_args* a) {
   if (a->table_width < 0 || a->table_stride < a->table_width) return CASCADE_EINVAL;
   if (a->stride_page < 0 || a->stride_head < 0 || a->stride_pos < 0 || a->q_stride < (int64_t)a->n_heads * a->head_dim) return CASCADE_ESHAPE;
   // (rows and heads of sums that lie on each other would be a race)
-  if (a->mass_stride_head < 0 || a->mass_stride_row < 0 || (a->n_kv_heads > 1 && a->mass_stride_head < a->mass_cap) ||
-      (a->n_rows > 1 && a->mass_stride_row < a->mass_cap))
-    return CASCADE_ESHAPE;
+  if (a->mass_stride_head < 0 || a->mass_stride_row < 0 || !lies_apart({{a->mass_stride_head, a->n_kv_heads}, {a->mass_stride_row, a->n_rows}}, a->mass_cap)) return CASCADE_ESHAPE;
   const cascade_limits& L = ctx->lim;
   if (a->n_rows > L.max_rows || a->n_tokens > L.max_nodes_total || a->n_source > L.max_nodes_total || a->max_seq_len > L.max_prefix || a->n_heads > L.n_heads ||
       a->head_dim > L.head_dim)
@@ -640,7 +655,11 @@ static int check_paged_evict(const cascade_ctx* ctx, const paged_evict_args* a) 
   if (some && (!a->seq_len || !a->budget || !a->seq_len_out || !a->free_count || !a->free_count_out)) return CASCADE_EINVAL;
   if (some && a->max_seq_len > 0 && (!a->mass || !a->mass_out || !a->k_pages || !a->v_pages || !a->block_table || a->n_pages == 0)) return CASCADE_EINVAL;
   if (some && a->free_capacity > 0 && !a->free_pages) return CASCADE_EINVAL;
-  if (some && (a->seq_len == a->seq_len_out || a->free_count == a->free_count_out || (a->mass && a->mass == a->mass_out))) return CASCADE_EINVAL;
+  // (one workgroup writes what others still read)
+  for (const void* in : {a->seq_len, a->budget, a->n_first})
+    if (some && in && (in == a->seq_len_out || in == a->dropped)) return CASCADE_EINVAL;
+  if (some && (a->seq_len_out == a->dropped || a->free_count == a->free_count_out || (a->mass && a->mass == a->mass_out) || (a->k_pages && a->k_pages == a->v_pages)))
+    return CASCADE_EINVAL;
   if (a->dtype != CASCADE_F32 && a->dtype != CASCADE_BF16) return CASCADE_EDTYPE;
   if (a->n_layers < 0 || a->n_rows < 0 || a->n_kv_heads <= 0 || a->head_dim <= 0 || a->n_recent < 0 || a->max_seq_len < 0 || a->mass_cap < 0 || a->free_capacity < 0 ||
       a->workspace_bytes < 0)
@@ -654,9 +673,10 @@ static int check_paged_evict(const cascade_ctx* ctx, const paged_evict_args* a) 
     if (strides[i] < 0 || (strides[i] * e) % 16) return CASCADE_ESHAPE;
   if ((a->head_dim * e) % 16) return CASCADE_ESHAPE;
   if (((uintptr_t)a->k_pages | (uintptr_t)a->v_pages | (uintptr_t)a->workspace) & 15) return CASCADE_EINVAL;
-  // (weights that lie on each other would be a race)
-  if (a->mass_stride_head < 0 || a->mass_stride_row < 0 || a->mass_stride_layer < 0 || (a->n_kv_heads > 1 && a->mass_stride_head < a->mass_cap) ||
-      (a->n_rows > 1 && a->mass_stride_row < a->mass_cap) || (a->n_layers > 1 && a->mass_stride_layer < a->mass_cap))
+  // (weights or keys that lie on each other would be a race)
+  if (a->mass_stride_head < 0 || a->mass_stride_row < 0 || a->mass_stride_layer < 0 ||
+      !lies_apart({{a->mass_stride_head, a->n_kv_heads}, {a->mass_stride_row, a->n_rows}, {a->mass_stride_layer, a->n_layers}}, a->mass_cap) ||
+      !lies_apart({{a->stride_pos, a->page_size}, {a->stride_head, a->n_kv_heads}, {a->stride_page, a->n_pages}, {a->stride_layer, a->n_layers}}, a->head_dim))
     return CASCADE_ESHAPE;
   const cascade_limits& L = ctx->lim;
   if (a->n_rows > L.max_rows || a->max_seq_len > L.max_prefix) return CASCADE_ESHAPE;

@@ -221,7 +221,7 @@ class PagedLoop:
         self.q_off = i32(S + 1)
         self.longest = 0                       # host bound on the rows' lengths
         self.rows = inp.n_rows
-        self.admitted: Optional[List[int]] = [0] * S      # tokens that the rows were given; None once steps have made rows longer
+        self.admitted: Optional[List[int]] = [0] * S      # tokens that the rows were given; None once steps or evictions have changed how many are there
         self.group_off = self.shared_len = None           # what share has set, for the attention calls
         self.longest_shared = 0
         self.held = i32(S)                                # positions of each row that lie in pages of several rows
@@ -263,10 +263,10 @@ class PagedLoop:
 
     def share(self, group_off, positions) -> None:
         """Rows group_off[g] + 1 .. group_off[g + 1] - 1 (host lists; all rows, in order) get the first positions[g] positions of row group_off[g], in the same pages: whole
-        pages that this row was admitted to.  The others must be empty, and no step may have been made.  Rows of a group give these pages back together."""
+        pages that this row was admitted to.  The others must be empty, and no step or eviction may have been made.  Rows of a group give these pages back together."""
         ok = (len(group_off) == len(positions) + 1 and group_off[0] == 0 and group_off[-1] == self.rows and all(a <= b for a, b in zip(group_off, group_off[1:])))
         if not ok or self.admitted is None or self.group_off is not None:
-            raise ValueError(f"groups of rows {list(group_off)}, {self.rows} rows: once, for all rows in order, before the first step")
+            raise ValueError(f"groups of rows {list(group_off)}, {self.rows} rows: once, for all rows in order, before the first step or eviction")
         for lo, hi, n in zip(group_off, group_off[1:], positions):
             if n < 0 or n % self.page_size or (hi - lo > 1 and (n > self.admitted[lo] or any(self.admitted[lo + 1:hi]))):
                 raise ValueError(f"rows {lo} to {hi - 1} cannot share {n} positions: whole pages of {self.page_size} of what the first has, the others empty")
@@ -305,6 +305,7 @@ class PagedLoop:
         self.seq_len, self.seq_next = self.seq_next, self.seq_len
         self.free_count, self.free_next = self.free_next, self.free_count
         self.mass, self.mass_next = self.mass_next, self.mass
+        self.admitted = None
         self.longest = min(self.longest, max(max(budgets), max(n_first, self.longest_shared) + n_recent))
 
     def admit(self, q, k_new, v_new, new_len, out, lse=None):

@@ -90,7 +90,9 @@ def test_mass(lib, ctx):
                 (D, dict(dtype=2))]
              + [(S, {k: v}) for k, v in (("n_heads", 7), ("n_heads", 16), ("head_dim", 96), ("head_dim", 256), ("page_size", 8), ("page_size", 1040), ("n_rows", 5), ("n_tokens", 65),
                                          ("n_source", 65), ("max_seq_len", 1001), ("max_seq_len", 0), ("max_new", 0), ("stride_pos", 129), ("stride_head", -8), ("q_stride", 1016),
-                                         ("mass_stride_row", 999), ("mass_stride_head", 999), ("mass_stride_head", -1), ("max_new", 1 << 28))]
+                                         ("mass_stride_row", 999), ("mass_stride_head", 999), ("mass_stride_head", -1), ("max_new", 1 << 28),
+                                         ("mass_stride_row", 1000), ("mass_stride_row", 1999), ("mass_stride_head", 2000), ("mass_stride_row", 1 << 62))]   # (sums on each other)
+             + [(S, dict(mass_stride_row=1000, mass_stride_head=3999)), (S, dict(mass_stride_row=1000, mass_stride_head=1000))]
              + [(S, dict(dtype=B.F32, head_dim=257)), (B.OK, dict(n_rows=0)), (B.OK, dict(n_tokens=0))])
 
 
@@ -102,7 +104,7 @@ def test_mass_that_a_launch_cannot_count(lib):
 
 
 def test_evict(lib, ctx):
-    r = B.paged_evict_args(B.BF16, 2, 4, 2, 128, 64, 64, 64, 10, 1000, 64, 128, 8000, 2000, 1000, 1000, 10, 16, 63, 64, 64, 40960, 4096, 2048, 128, 64, 63, 10, 64, 64, 128, 128, 64,
+    r = B.paged_evict_args(B.BF16, 2, 4, 2, 128, 64, 64, 64, 10, 1000, 64, 128, 8000, 2000, 1000, 1000, 10, 16, 63, 64, 128, 40960, 4096, 2048, 128, 64, 63, 10, 64, 64, 128, 128, 256,
                            64, 1 << 30)
     changes = ([(E, {k: None}) for k in ("seq_len", "budget", "mass", "mass_out", "k_pages", "v_pages", "block_table", "free_pages", "free_count", "free_count_out", "seq_len_out")]
                + [(E, {k: -1}) for k in ("n_layers", "n_rows", "n_kv_heads", "head_dim", "n_recent", "max_seq_len", "mass_cap", "free_capacity", "n_pages", "table_width",
@@ -110,7 +112,10 @@ def test_evict(lib, ctx):
                + [(E, {k: 72}) for k in ("k_pages", "v_pages", "workspace")]
                + [(E, dict(mass_out=64)), (E, dict(seq_len_out=64)), (E, dict(free_count_out=64)), (E, dict(n_pages=0)), (E, dict(table_stride=62)), (D, dict(dtype=2))]
                + [(S, {k: v}) for k, v in (("n_rows", 5), ("max_seq_len", 1001), ("page_size", 24), ("head_dim", 4), ("stride_layer", 12), ("stride_pos", -8), ("mass_stride_layer", 999),
-                                           ("mass_stride_row", 999), ("mass_stride_head", 999), ("mass_stride_head", -1), ("n_layers", 1 << 20), ("n_pages", 1 << 28))]
+                                           ("mass_stride_row", 999), ("mass_stride_head", 999), ("mass_stride_head", -1), ("n_layers", 1 << 20), ("n_pages", 1 << 28),
+                                           ("mass_stride_layer", 4000), ("mass_stride_row", 1000), ("mass_stride_head", 2000), ("stride_layer", 20480), ("stride_page", 2048),
+                                           ("stride_page", 0), ("stride_head", 1024), ("stride_pos", 120))]   # (weights, keys on each other)
+               + [(E, {k: v}) for k, v in (("dropped", 64), ("dropped", 128), ("budget", 128), ("n_first", 128), ("n_first", 256), ("v_pages", 64))]
                + [(S, dict(table_width=1 << 28, table_stride=1 << 28)), (B.OK, dict(n_rows=0)), (B.OK, dict(n_layers=0))])
     _refused(lib.paged_evict, ctx, r, changes)
     n = C.c_int64()

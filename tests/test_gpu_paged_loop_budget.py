@@ -201,3 +201,8 @@ def test_refusals():
             loop.evict(*args)
     torch.cuda.synchronize()
     assert loop.seq_len.tolist() == [64, 48, 6, 0] and loop.ctx.device_status() == binding.OK
+    again = decode.PagedLoop(inp, page_size=PAGE, max_len=320, max_chunk=100, keep_mass=True)
+    again.admit(q, kv, kv, [64, 0, 6, 0], torch.empty_like(q))
+    again.evict(50)
+    with pytest.raises(ValueError):                             # heads of the first row hold positions of their own by now
+        again.share([0, 2, 4], [48, 0])
