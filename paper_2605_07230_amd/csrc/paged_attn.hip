@@ -1387,7 +1387,8 @@ __global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
 
 // ---------------------------------------------------------------------------------------------- both passes of paged_attn_shared at once
 // The pass over shared keys is products and the trips to memory before and after them, the rows' own is the stream of their keys: in one launch each covers the other's waits.  The
-// first `shared_blocks` workgroups are the former's, one to a compute unit before any gets a second.
+// first `shared_blocks` workgroups are the former's, one to a compute unit before any gets a second.  64 rows of one token x 32 heads behind 4192 shared keys and 90 to 600 of their own, 8 kv
+// heads: 43 us with the join (51 in a launch each; every row by itself 100; 22 at the rate of a large copy): the chain in front of the first tile, the shared pass's tiles one after the other, the join.
 struct BothParams {
   PagedParams p;         // of the rows' own pass
   int shared_parts, shared_blocks;
