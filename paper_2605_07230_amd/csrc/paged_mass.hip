@@ -145,14 +145,29 @@ __device__ __forceinline__ void write_sums(const MassParams& p, const MassRow& r
 // Up to 16 NB query rows (single tokens, accepted paths): bound by the stream of keys.  A wave has a tile or two of 64 positions and everything else that it needs on its way before
 // them - query rows, lse, the sums so far - so one trip to memory follows the place of a tile, and no wave waits for another.  One token of 64 rows x 4200 keys, 8 kv heads
 // of 4, head_dim 128 (568 MB): 116 us = 4.9 TB/s from memory (a large copy: 4.9).
-template <int D, int NB>
+template <int D, int NB, bool DEALT>
 __global__ __launch_bounds__(64 * WAVES, NB == 1 ? 4 : 3) void paged_mass_few_kernel(MassParams p) {
   constexpr int KW = 4;
   typedef Operand<uint16_t, D, true> Op;
   const paged_mass_args& a = p.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4, G = p.group;
-  const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads, kblk = b / a.n_rows;   // (long rows' last tiles come last, from all of them)
-  const MassRow row = row_of(p, b % a.n_rows, kblk == 0 && kvh == 0 && tid == 0);
+  const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads;
+  int kblk;
+  MassRow row;
+  if constexpr (!DEALT) {
+    kblk = b / a.n_rows;   // (long rows' last tiles come last, from all of them)
+    row = row_of(p, b % a.n_rows, kblk == 0 && kvh == 0 && tid == 0);
+  } else {
+    MassRow mine = {0, 0, 0, 0, 0, 0};
+    if (lane < a.n_rows) mine = row_of(p, lane, b == 0 && kvh == 0 && wave == 0);
+    const int per = 16 * KW * WAVES * p.wave_tiles, cnt = mine.n > 0 ? (mine.L + per - 1) / per : 0, incl = wave_scan_incl_i(cnt);
+    const unsigned long long who = __ballot(incl > b);
+    if (!who) return;
+    const int l = __ffsll((long long)who) - 1;
+    auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+    kblk = b - of(incl - cnt);
+    row = MassRow{l, of(mine.lo), of(mine.n), of(mine.L), of(mine.Lp), of(mine.first)};
+  }
   const int lo = row.lo, n = row.n, M = n * G, Lp = row.Lp, W = a.window;
   const int kb0 = 16 * KW * (WAVES * p.wave_tiles * kblk + wave), kb1 = min(row.L, kb0 + 16 * KW * WAVES * p.wave_tiles);   // tiles WAVES apart
   if (n == 0 || kb0 >= row.L || kb1 <= row.first) return;
@@ -310,8 +325,35 @@ __global__ __launch_bounds__(64 * WAVES) void paged_mass_kernel(MassParams p) {
 // needed next (vmcnt), then one bare barrier makes everybody's visible and the oldest place free.  Such a load puts lane l's 16 bytes at 16 l, so rows cannot be padded;
 // slot q of row r holds piece q ^ swz(r), and the 16 rows of an operand meet in no bank.  lse of rows that are not there, and of tokens without a source, come from a place that
 // holds infinity: they count nothing.  Bound by products and exponentials, which take turns (matrix cores 21 % and vector ALU 46 % of the cycles where rows differ in length): 16 rows of 1000
-// tokens behind 3000, 8 kv heads of 4, 548 us = 840 TFLOP/s (a large product: 1214); rows of 500 to 1000 behind up to 2000 114.  Three places in the ring: two wait for memory,
+// tokens behind 3000, 8 kv heads of 4, 550 us = 835 TFLOP/s (a large product: 1214); 8 rows of 500 to 1000 behind up to 2000 110 to 115.  Three places in the ring: two wait for memory,
 // four leave room for two workgroups only.
+// Workgroup `b` of a kv head: with up to 64 rows the blocks of keys come in the order of the tokens that see them, min(n, L - y) for the block that begins at y, so what the launch ends
+// with is short: 8 rows of 500 to 1000 tokens behind up to 2000 122 -> 115 us (other lengths of them 149 -> 145, 132 -> 105), 16 rows of 100 to 1000 behind up to 4000 223 -> 195, 40 of up to 300
+// behind up to 3000 152 -> 120; rows of one length 277 -> 274, of 100 tokens 58 -> 62, for the search.  A lane to a row; how many blocks have at least w tokens is a sum over the rows, and
+// w is found bit by bit.
+template <int KEYS>
+__device__ __forceinline__ MassRow longest_first(const MassParams& p, int b, bool report, int* kblk) {
+  const paged_mass_args& a = p.a;
+  const int lane = threadIdx.x & 63;
+  if (a.n_rows > 64) {   // positions that all tokens see come first, rows one further with every block
+    *kblk = b / a.n_rows;
+    return row_of(p, (b + *kblk + (*kblk >> 2)) % a.n_rows, report && *kblk == 0 && lane == 0);
+  }
+  MassRow mine = {0, 0, 0, 0, 0, 0};
+  if (lane < a.n_rows) mine = row_of(p, lane, report && b == 0);
+  auto at_least = [&](int w) { return mine.n >= w ? (mine.L - w) / KEYS + 1 : 0; };   // (0 < w <= n <= L)
+  int w = 0;
+  for (int bit = 1 << (31 - __clz(a.max_new)); bit; bit >>= 1)
+    if (wave_sum_i(at_least(w | bit)) > b) w |= bit;
+  if (w == 0) return MassRow{0, 0, 0, 0, 0, 0};   // fewer blocks than that
+  const int above = at_least(w + 1), before = b - wave_sum_i(above), incl = wave_scan_incl_i(at_least(w) - above);   // of blocks with just w tokens the `before`-th
+  const int l = __ffsll((long long)__ballot(incl > before)) - 1;
+  auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+  // a row's blocks with w tokens follow one another: the last of them that has so many
+  *kblk = of((mine.L - w) / KEYS) - (of(incl) - 1 - before);
+  return MassRow{l, of(mine.lo), of(mine.n), of(mine.L), of(mine.Lp), of(mine.first)};
+}
+
 constexpr int QB = 64, STAGES = 3;   // query rows of a block, places of the ring
 __device__ const float s_nothing = INFINITY;
 
@@ -339,9 +381,9 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_mass_ring_kernel(MassPara
   __shared__ float s_join[KG < WAVES ? WAVES * 64 : 1];
   const paged_mass_args& a = p.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4, G = p.group;
-  const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads, kblk = b / a.n_rows;   // positions that all tokens see come first
-  // (rows one further with every block of keys: workgroups that meet on a compute unit are rarely all of the longest row)
-  const MassRow row = row_of(p, (b + kblk + (kblk >> 2)) % a.n_rows, kblk == 0 && kvh == 0 && tid == 0);
+  const int kvh = blockIdx.x % a.n_kv_heads, b = blockIdx.x / a.n_kv_heads;
+  int kblk;
+  const MassRow row = longest_first<KEYS>(p, b, kvh == 0 && wave == 0, &kblk);
   const int lo = row.lo, n = row.n, M = n * G, Lp = row.Lp, W = a.window;
   const int kb0 = KEYS * kblk, kb = kb0 + 16 * KW * (wave % KG), qw = wave / KG;
   if (n == 0 || kb0 >= row.L || kb0 + KEYS <= row.first) return;
@@ -554,8 +596,13 @@ hipError_t launch_few_k(cascade_ctx* ctx, MassParams& p) {
   // keys 75, 71, 78; paths of 11 tokens, 16 rows x 32 heads of 600 to 2356 keys 53, 51, 49.
   p.wave_tiles = tiles >= 8 * ctx->n_cu ? 2 : 1;
   p.key_blocks = (p.a.max_seq_len + 256 * p.wave_tiles - 1) / (256 * p.wave_tiles);
+  const dim3 grid((unsigned)((int64_t)p.a.n_rows * p.a.n_kv_heads * p.key_blocks));
+  // Of few rows the workgroups that have keys come one behind the other, the others last (one token of 4 rows of up to 16000 keys 25.6 -> 17.5 us, of 16 of up to 8000 47.7 -> 44.5; paths of 16 rows of
+  // 600 to 2356 keys 43.6 -> 44.2); of many rows the last tiles of all come last (64 of 2145 keys 62.6, row by row 66.4)
+  const bool dealt = p.a.n_rows > 2 && p.a.n_rows <= 16;
   KernelTimer t(ctx, CASCADE_K_MASS);
-  CASCADE_TIMED_LAUNCH(t, (paged_mass_few_kernel<D, NB>), dim3((unsigned)((int64_t)p.a.n_rows * p.a.n_kv_heads * p.key_blocks)), dim3(64 * WAVES), 0, ctx->stream, p);
+  if (dealt) CASCADE_TIMED_LAUNCH(t, (paged_mass_few_kernel<D, NB, true>), grid, dim3(64 * WAVES), 0, ctx->stream, p);
+  else CASCADE_TIMED_LAUNCH(t, (paged_mass_few_kernel<D, NB, false>), grid, dim3(64 * WAVES), 0, ctx->stream, p);
   return hipGetLastError();
 }
 template <int D>

@@ -86,6 +86,25 @@ def test_random_shapes(seed):
     p.check()
 
 
+@pytest.mark.parametrize("rows", [2, 3, 16, 17, 64, 65, 70])
+@pytest.mark.parametrize("most", [1, 40, 300])
+def test_rows_of_all_lengths(rows, most):
+    """Blocks of keys are dealt to workgroups by the rows' lengths: equal ones, rows without tokens, the longest one last, rows of one position."""
+    rng = np.random.default_rng(rows * 1000 + most)
+    new = [int(x) for x in rng.integers(0, most + 1, rows)]
+    new[0] = new[rows // 2] = most
+    length = [n + int(x) for n, x in zip(new, rng.integers(0, 700, rows))]
+    length[-1], new[-1] = 1300, most
+    if rows > 2:
+        length[1] = new[1] = 1
+        length[rows // 2] = length[0]
+    p = Mass(rows + most, length, new, heads=4, kv_heads=2, head_dim=64 if rows % 2 else 128, path=0)
+    ctx = p.context()
+    p.run(ctx)
+    assert ctx.device_status() == binding.OK
+    p.check()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_tokens_that_count_nothing(dtype):
     """Without a finite lse, or without a source."""
@@ -151,6 +170,21 @@ def test_rows_that_break_their_bounds_stay_as_they_are():
             if "q_off" not in change:
                 p.check(rows=[1])
             assert ctx.device_status() == binding.OK
+
+
+@pytest.mark.parametrize("rows", [4, 20, 70])
+@pytest.mark.parametrize("tokens", [1, 90])
+def test_one_of_many_that_breaks_its_bounds(rows, tokens):
+    for bad, value in ((0, -1), (2, 1 << 30), (rows - 1, tokens - 1)):
+        p = Mass(rows + bad, [tokens + 37 * (s % 7) for s in range(rows)], [tokens] * rows, heads=4, kv_heads=2)
+        lengths = list(p.length)
+        lengths[bad] = value
+        ctx = p.context()
+        p.run(ctx, seq_len=dev(lengths))
+        assert ctx.device_status() == binding.ETREE
+        assert torch.equal(p.mass[bad].nan_to_num(-1), p.before[bad].nan_to_num(-1))
+        p.check(rows=[s for s in range(rows) if s != bad])
+        assert ctx.device_status() == binding.OK
 
 
 def test_entries_and_sources_outside_set_the_flag():
