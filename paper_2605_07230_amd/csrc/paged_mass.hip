@@ -324,7 +324,7 @@ __global__ __launch_bounds__(64 * WAVES) void paged_mass_kernel(MassParams p) {
 // lse pass through a ring in LDS, filled by LDS-direct loads (M0 = the LDS address of a wave's 1 KiB) two blocks ahead of their use: a wave waits for its own loads of the block
 // needed next (vmcnt), then one bare barrier makes everybody's visible and the oldest place free.  Such a load puts lane l's 16 bytes at 16 l, so rows cannot be padded;
 // slot q of row r holds piece q ^ swz(r), and the 16 rows of an operand meet in no bank.  lse of rows that are not there, and of tokens without a source, come from a place that
-// holds infinity: they count nothing.  Bound by products and exponentials, which take turns (matrix cores 21 % and vector ALU 46 % of the cycles where rows differ in length): 16 rows of 1000
+// holds infinity: they count nothing.  Bound by products and exponentials, which take turns (matrix cores 28 % and vector ALU 44 % of the cycles where rows differ in length): 16 rows of 1000
 // tokens behind 3000, 8 kv heads of 4, 550 us = 835 TFLOP/s (a large product: 1214); 8 rows of 500 to 1000 behind up to 2000 110 to 115.  Three places in the ring: two wait for memory,
 // four leave room for two workgroups only.
 // Workgroup `b` of a kv head: with up to 64 rows the blocks of keys come in the order of the tokens that see them, min(n, L - y) for the block that begins at y, so what the launch ends
