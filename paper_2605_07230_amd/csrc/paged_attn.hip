@@ -597,7 +597,7 @@ __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_ke
 // measured.  Eight rows of 500-1000 new tokens behind 0-2000, 8 kv heads of 4 (157 GFLOP): 188 us = 835 TFLOP/s in 128-row workgroups (64 rows: 259, 256 rows, tried there: 221); 256-node trees of
 // 8 rows x 32 heads behind 4200 keys (141 GFLOP): 181-184 us, 183 where the prefixes are contiguous; 1800-2000 new tokens under a window of 1024, head_dim 64: 40.2
 // (half the products per exponential: 21 and 48 %; the chunks above with that head_dim 125, the trees 130).  Three workgroups per compute unit are what head_dim 64 runs best with, and they leave
-// 128-row workgroups 168 registers: 9 (chains) and 14 (trees) go to scratch.
+// 128-row workgroups 168 registers: 11 (chains) and 10 (trees) go to scratch.
 // Sums of the probabilities as they are, before they are rounded, cost less than products with ones (196 -> 184 us for the trees: registers) and give an exact lse.
 template <int D>
 struct RingGeom {
