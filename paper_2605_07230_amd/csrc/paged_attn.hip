@@ -167,6 +167,19 @@ __device__ __forceinline__ void find_groups(const PagedParams& p, Groups& gr, in
   }
   __syncthreads();
 }
+// A call with groups that paged_attn takes alone: its first workgroup, one more than the call needs, looks at their offsets, so that what find_groups reports does not depend on how a
+// call is cut, and nobody waits for it.
+__host__ __device__ __forceinline__ int checking_blocks(const PagedParams& p) { return p.n_groups > 0 ? 1 : 0; }
+__device__ __forceinline__ bool only_checks_groups(const PagedParams& p) {
+  if ((int)blockIdx.x >= checking_blocks(p)) return false;
+  bool bad = false;
+  for (long long g = threadIdx.x; g <= p.n_groups; g += blockDim.x) {
+    const int at = p.group_off[g];
+    bad |= g < p.n_groups ? at > p.group_off[g + 1] || (g == 0 && at != 0) : at != p.a.n_rows;
+  }
+  if (bad) atomicOr(p.dev_status, CASCADE_FLAG_TREE_SIZE);
+  return true;
+}
 // the parts of the other pass, for a row that shares nothing
 __device__ __forceinline__ void write_no_shared(const PagedParams& p, int lo, int T, int kvh, int row0, int row1, int tid, int threads) {
   const int G = p.group;
@@ -579,7 +592,7 @@ __device__ __forceinline__ void paged_few(const PagedParams& p, const int block,
 
 template <int D, int NW, bool TREE>
 __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_kernel(PagedParams p) {
-  paged_few<D, NW, TREE, ALONE>(p, blockIdx.x, gridDim.x);
+  if (!only_checks_groups(p)) paged_few<D, NW, TREE, ALONE>(p, blockIdx.x - checking_blocks(p), gridDim.x - checking_blocks(p));
 }
 
 // ------------------------------------------------------------------------------------------------------- bf16, many query rows
@@ -1144,7 +1157,7 @@ __device__ __forceinline__ void paged_ring(const PagedParams& p, const int block
 
 template <int D, int NS, int NQ, int NW, bool TREE>
 __global__ __launch_bounds__(64 * NW, (ring_per_simd<D, NQ, NW>())) void paged_ring_kernel(PagedParams p) {
-  paged_ring<D, NS, NQ, NW, TREE, ALONE>(p, blockIdx.x, gridDim.x);
+  if (!only_checks_groups(p)) paged_ring<D, NS, NQ, NW, TREE, ALONE>(p, blockIdx.x - checking_blocks(p), gridDim.x - checking_blocks(p));
 }
 
 // ------------------------------------------------------------------------------------------------------------------------- f32
@@ -1382,7 +1395,7 @@ __device__ __forceinline__ void paged_f32(const PagedParams& p, const int block)
 
 template <int DB, int NW, bool VEC, bool TREE>
 __global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
-  paged_f32<DB, NW, VEC, TREE, ALONE>(p, blockIdx.x);
+  if (!only_checks_groups(p)) paged_f32<DB, NW, VEC, TREE, ALONE>(p, blockIdx.x - checking_blocks(p));
 }
 
 // ---------------------------------------------------------------------------------------------- both passes of paged_attn_shared at once
@@ -1577,7 +1590,7 @@ hipError_t launch_few_k(cascade_ctx* ctx, const PagedParams& p) {
   if (e != hipSuccess) return e;
   const int64_t items = (int64_t)p.a.n_rows * p.a.n_kv_heads * p.parts, slots = (int64_t)ctx->n_cu * few_per_unit<D, NW>();
   KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
-  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)std::min(items, slots)), dim3(64 * NW), smem, ctx->stream, p);
+  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)(std::min(items, slots) + checking_blocks(p))), dim3(64 * NW), smem, ctx->stream, p);
   return hipGetLastError();
 }
 template <int D>
@@ -1606,7 +1619,7 @@ hipError_t launch_ring_k(cascade_ctx* ctx, PagedParams& p) {
   const int64_t share = 8 % a.n_kv_heads == 0 ? 8 / a.n_kv_heads : 1;
   p.in_order = a.n_rows == 1 || a.n_rows > 64 || blocks * a.n_kv_heads <= ctx->n_cu;
   KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
-  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)((blocks + share - 1) / share * share * a.n_kv_heads)), dim3(64 * NW), smem, ctx->stream, p);
+  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)((blocks + share - 1) / share * share * a.n_kv_heads + checking_blocks(p))), dim3(64 * NW), smem, ctx->stream, p);
   return hipGetLastError();
 }
 template <int D, bool TREE>
@@ -1625,7 +1638,7 @@ hipError_t launch_f32_k(cascade_ctx* ctx, PagedParams& p) {
   const int64_t blocks = most_blocks<ALONE>(p, 16) * p.a.n_kv_heads;
   p.in_order = p.a.n_rows == 1 || p.a.n_rows > 64 || blocks <= ctx->n_cu;
   KernelTimer t(ctx, CASCADE_K_PAGED_ATTN);
-  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)blocks), dim3(64 * NW), smem, ctx->stream, p);
+  CASCADE_TIMED_LAUNCH(t, kern, dim3((unsigned)(blocks + checking_blocks(p))), dim3(64 * NW), smem, ctx->stream, p);
   return hipGetLastError();
 }
 // keys, values and queries 16 bytes at a time where everything lies on such boundaries, otherwise element by element
@@ -1650,7 +1663,7 @@ hipError_t launch_bf16(cascade_ctx* ctx, PagedParams& p, const Cut& c) {
   return p.a.parent ? launch_ring<D, true>(ctx, p, c) : launch_ring<D, false>(ctx, p, c);
 }
 
-// A launch of both passes: `p` is the own pass's, as for launch_pass.
+// A launch of both passes: `p` is the own pass's.
 template <int D, int NQ, bool TREE>
 hipError_t launch_both_k(cascade_ctx* ctx, const PagedParams& p, const Cut& shared) {
   constexpr int v_bytes = 4 * KT * (D + 16) * 2, o_bytes = 4 * 16 * (D + 4 + 2) * 4, few = v_bytes > o_bytes ? v_bytes : o_bytes;
@@ -1769,8 +1782,11 @@ SharedCut choose_shared(const paged_shared_args* a, int n_cu, size_t ws_bytes) {
 
 }  // namespace
 
-hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
+// with n_groups: of a call that could share, whose groups are checked
+static hipError_t launch_alone(cascade_ctx* ctx, const paged_attn_args* a, const int32_t* group_off, int n_groups) {
   PagedParams p = params_of(ctx, a);
+  p.group_off = group_off;
+  p.n_groups = n_groups;
   size_t ws_bytes;
   char* ws = parts_of(ctx, a, &ws_bytes);
   const Cut c = choose(a, ctx->n_cu, ws_bytes);
@@ -1781,11 +1797,13 @@ hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) {
   return e != hipSuccess || c.parts == 1 ? e : launch_merge(ctx, p);
 }
 
+hipError_t launch_paged_attn(cascade_ctx* ctx, const paged_attn_args* a) { return launch_alone(ctx, a, nullptr, 0); }
+
 hipError_t launch_paged_shared(cascade_ctx* ctx, const paged_shared_args* a) {
   size_t ws_bytes;
   char* ws = parts_of(ctx, &a->attn, &ws_bytes);
   const SharedCut c = choose_shared(a, ctx->n_cu, ws_bytes);
-  if (c.shared.parts == 0) return launch_paged_attn(ctx, &a->attn);
+  if (c.shared.parts == 0) return launch_alone(ctx, &a->attn, a->group_off, a->n_groups);
   PagedParams p = params_of(ctx, &a->attn);
   p.group_off = a->group_off;
   p.shared_len = a->shared_len;
