@@ -479,10 +479,14 @@ def _paged_attn_record(q_off, prefix_len, block_table, q, k_new, v_new, k_pages,
         table_stride, table_one = block_table.stride()
         assert (pool_heads == kv_heads and pool_D == D and one == 1 == table_one and (page_stride, head_stride, pos_stride, 1) == v_pages.stride()
                 and pool == v_pages.shape and dtype is k_pages.dtype and dtype is v_pages.dtype)
-        width, kp, vp, table = block_table.shape[1], k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr()
+        table_rows, width = block_table.shape
+        kp, vp, table = k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr()
     else:
         pages, page_size, page_stride, head_stride, pos_stride, table_stride, width, kp, vp, table = 0, 16, 0, 0, 0, 0, 0, 0, 0, 0
-    return _PAGED_ATTN(_dtype_code(q), prefix_len.numel(), q_off.data_ptr(), 0 if parent is None else parent.data_ptr(), prefix_len.data_ptr(), n, max_new,
+    rows = prefix_len.numel()
+    # (what a kernel counts by rows or tokens, the outputs above all, holds so many)
+    assert q_off.numel() > rows and (k_pages is None or table_rows >= rows) and (lse is None or lse.numel() >= n * heads) and (parent is None or parent.numel() >= n)
+    return _PAGED_ATTN(_dtype_code(q), rows, q_off.data_ptr(), 0 if parent is None else parent.data_ptr(), prefix_len.data_ptr(), n, max_new,
                        max_prefix_len, heads, kv_heads, D, scale, window, n_sink, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), q_stride, kv_stride, kp, vp,
                        page_stride, head_stride, pos_stride, pages, page_size, table, table_stride, width, out.data_ptr(), 0 if lse is None else lse.data_ptr(),
                        *((0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())))
@@ -581,10 +585,12 @@ def paged_mass(ctx: Context, *, q_off, seq_len, block_table, q, lse, k_pages, ma
     mass_row, mass_head, mass_one = mass.stride()
     assert (q_head == D == pool_D and q_one == 1 == one == table_one and q.dtype is k_pages.dtype and lse.shape == (n, heads) and lse.is_contiguous()
             and (mass_one == 1 or cap <= 1) and rows == seq_len.numel() and mass_heads == kv_heads and mass.dtype is lse.dtype is torch.float32)
+    table_rows, width = block_table.shape
+    assert q_off.numel() > rows <= table_rows and (first is None or first.numel() >= rows) and (prefix_len is None or prefix_len.numel() >= rows)
     _check(ctx.lib.paged_mass_record(ctx.handle, _MASS(
         _dtype_code(q), rows, q_off.data_ptr(), seq_len.data_ptr(), 0 if source is None else source.data_ptr(), 0 if first is None else first.data_ptr(),
         0 if prefix_len is None else prefix_len.data_ptr(), n if source is None else source.numel(), n, max_new, max_seq_len, heads, kv_heads, D, scale, window, n_sink, q.data_ptr(), q_stride, lse.data_ptr(),
-        k_pages.data_ptr(), page_stride, head_stride, pos_stride, pages, page_size, block_table.data_ptr(), table_stride, block_table.shape[1], cap,
+        k_pages.data_ptr(), page_stride, head_stride, pos_stride, pages, page_size, block_table.data_ptr(), table_stride, width, cap,
         mass.data_ptr(), mass_row, mass_head)))
 
 
@@ -598,9 +604,12 @@ def _paged_evict_record(seq_len, budget, block_table, k_pages, v_pages, mass, ma
     assert (v_pages.shape == shape and v_pages.stride() == stride and stride[4] == 1 == table_one and k_pages.dtype is v_pages.dtype and m_layers == layers
             and m_heads == kv_heads and rows == seq_len.numel() == budget.numel() and mass_out.shape == mass.shape and mass_out.stride() == m_stride
             and (m_stride[3] == 1 or cap <= 1) and mass.dtype is mass_out.dtype is torch.float32)
+    table_rows, width = block_table.shape
+    assert (seq_len_out.numel() >= rows <= table_rows and (dropped is None or dropped.numel() >= rows) and (n_first is None or n_first.numel() >= rows)
+            and free_count.numel() > 0 < free_count_out.numel())
     at = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
     return _EVICT(_dtype_code(k_pages), layers, rows, kv_heads, D, seq_len.data_ptr(), budget.data_ptr(), at(n_first), n_recent, max_seq_len, mass.data_ptr(),
-                  mass_out.data_ptr(), *m_stride[:3], cap, pages, page_size, block_table.shape[1], k_pages.data_ptr(), v_pages.data_ptr(), *stride[:4],
+                  mass_out.data_ptr(), *m_stride[:3], cap, pages, page_size, width, k_pages.data_ptr(), v_pages.data_ptr(), *stride[:4],
                   block_table.data_ptr(), table_stride, free_pages.numel(), free_pages.data_ptr(), free_count.data_ptr(), free_count_out.data_ptr(),
                   seq_len_out.data_ptr(), at(dropped), *((0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())))
 
