@@ -610,7 +610,7 @@ __global__ __launch_bounds__(64 * NW, (few_per_unit<D, NW>())) void paged_few_ke
 // measured.  Eight rows of 500-1000 new tokens behind 0-2000, 8 kv heads of 4 (157 GFLOP): 188 us = 835 TFLOP/s in 128-row workgroups (64 rows: 259, 256 rows, tried there: 221); 256-node trees of
 // 8 rows x 32 heads behind 4200 keys (141 GFLOP): 181-184 us, 183 where the prefixes are contiguous; 1800-2000 new tokens under a window of 1024, head_dim 64: 40.2
 // (half the products per exponential: 21 and 48 %; the chunks above with that head_dim 125, the trees 130).  Three workgroups per compute unit are what head_dim 64 runs best with, and they leave
-// 128-row workgroups 168 registers: 11 (chains) and 10 (trees) go to scratch.
+// 128-row workgroups 168 registers: 6 (chains) and 4 (trees) go to scratch.
 // Sums of the probabilities as they are, before they are rounded, cost less than products with ones (196 -> 184 us for the trees: registers) and give an exact lse.
 template <int D>
 struct RingGeom {
@@ -872,14 +872,12 @@ __device__ __forceinline__ void paged_ring(const PagedParams& p, const int block
   // query fragments (B operand of S^T): lane = (query l16, d group g)
   Frag8 qf[NQ][KS];
   int qi[NQ];            // the token, -1 behind the last
-  long long out_row[NQ];
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int r = row0 + 16 * (wave + NW * n) + l16;
     const bool ok = r < M;
     const int i = ok ? token_of(p, r) : 0, hg = ok ? r - i * G : 0;
     qi[n] = ok ? i : -1;
-    out_row[n] = (long long)(lo + i) * a.n_heads + kvh * G + hg;
     const uint16_t* qp = (const uint16_t*)a.q + (lo + i) * a.q_stride + (kvh * G + hg) * D + 8 * g;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -1134,16 +1132,19 @@ __device__ __forceinline__ void paged_ring(const PagedParams& p, const int block
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const float l = rows4_sum(lsum[n]);
-    if (qi[n] < 0) continue;
+    const int r = row0 + 16 * (wave + NW * n) + l16;   // (worked out again: held through the tiles these places cost the 128-row workgroups at head_dim 64 ten registers in scratch memory)
+    if (r >= M) continue;
+    const int i = token_of(p, r);
+    const long long out_row = (long long)(lo + i) * a.n_heads + kvh * G + r - i * G;
     if (PASS != ALONE || p.parts > 1) {
-      const long long w = part * all_rows + out_row[n];
+      const long long w = part * all_rows + out_row;
 #pragma unroll
       for (int db = 0; db < DB; ++db) *(f32x4*)(p.ws_o + w * D + 16 * db + 4 * g) = ot[n][db];
       if (g == 0) { p.ws_ml[w * 2] = m_ref[n]; p.ws_ml[w * 2 + 1] = l; }
       continue;
     }
     const float inv = 1.f / l;
-    uint16_t* o = (uint16_t*)a.out + out_row[n] * D;
+    uint16_t* o = (uint16_t*)a.out + out_row * D;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       uint2 w;
@@ -1151,7 +1152,7 @@ __device__ __forceinline__ void paged_ring(const PagedParams& p, const int block
       w.y = pack_bf16x2(ot[n][db][2] * inv, ot[n][db][3] * inv);
       *(uint2*)(o + 16 * db + 4 * g) = w;
     }
-    if (g == 0 && a.lse) a.lse[out_row[n]] = m_ref[n] * LN2 + logf(l);
+    if (g == 0 && a.lse) a.lse[out_row] = m_ref[n] * LN2 + logf(l);
   }
 }
 
