@@ -271,7 +271,8 @@ __device__ __forceinline__ void paged_few(const PagedParams& p, const int block,
   constexpr int NT = 64 * NW, KS = D / 32, DB = D / 16, DC = D / 8, VP = D + 16, OP = D + 4, NVC = KT * DC / 64, R = 16;
   extern __shared__ __align__(16) char few_smem[];
   const paged_attn_args& a = p.a;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // (a register less where both passes are one kernel: the thread's number is not held)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tid = 64 * wave + lane;
   const int l16 = lane & 15, g = lane >> 4, G = p.group;
   uint16_t* vt = (uint16_t*)few_smem + (size_t)wave * KT * VP;
   __shared__ typename std::conditional<PASS == OWN, Groups, int>::type groups;
@@ -1177,7 +1178,7 @@ __device__ __forceinline__ void paged_f32(const PagedParams& p, const int block)
   __shared__ int s_parent[TREE ? CASCADE_MAX_TREE : 1];
   constexpr int OP = 16 * DB + 4, TS = 16;
   const paged_attn_args& a = p.a;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tid = 64 * wave + lane;   // (as in paged_few)
   const int l16 = lane & 15, g = lane >> 4, G = p.group, D = a.head_dim;
   const int kvh = block % a.n_kv_heads, b = block / a.n_kv_heads, part = b % p.parts;
   int sb = 0, shared = 0;
