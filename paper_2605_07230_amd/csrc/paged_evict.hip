@@ -89,13 +89,13 @@ __device__ __forceinline__ void give_back(const EvictParams& p, int s) {
   }
 }
 
-// What stays of a (layer, row, kv head): the pairs of its list, which lies in LDS (LOCAL) or in the workspace, and, by one workgroup (`lead`), its weights; at: where these begin.
+// What stays of a (layer, row, kv head): the pairs of its list, which lies in LDS or in the workspace, and, by one workgroup (`lead`), its weights; at: where these begin.
 // Returns how many pairs there are of the first and of the second kind.
 // The weight that decides is found by radix selection of the ranks, 12, 10 and 10 bits: with the whole exponent and three bits of the fraction in the first digit, weights that spread
 // over some octaves spread over the bins.  Once no more than a wave of candidates begin like the one that decides they are ranked against each other, by weight and position, and the
 // other digits are left out.  A thread holds HELD consecutive positions in registers (rows of up to HELD NT positions are read once), so one scan over the threads' counts gives everything
 // its place in the order of positions.
-template <int NT, int HELD, bool LOCAL>
+template <int NT, int HELD>
 __device__ __forceinline__ int2 decide(const EvictParams& p, const RowPlan& w, long long at, bool lead, int2* pairs, int cap) {
   constexpr int NW = NT / 64, BINS = 4096, WORDS = BINS + BINS / 16, SPAN = HELD * NT;
   typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));   // (such loads need the boundary of a word)
@@ -403,7 +403,7 @@ __global__ __launch_bounds__(NT, 4) void evict_kernel(EvictParams p) {
     if (w.ok && split == 0) copy_weights(p, unit.mass, w.L, NT);
     return;
   }
-  const int2 counts = decide<NT, HELD, true>(p, w, unit.mass, split == 0, s_pairs, NT * HELD / 2);
+  const int2 counts = decide<NT, HELD>(p, w, unit.mass, split == 0, s_pairs, NT * HELD / 2);
   // keys by the even workgroups, values by the odd ones; one alone does both
   const int shares = max(p.splits >> 1, 1);
 #pragma unroll 1
@@ -425,7 +425,7 @@ __global__ __launch_bounds__(LONG_THREADS) void evict_stay_kernel(EvictParams p)
     if (w.ok) copy_weights(p, unit.mass, w.L, LONG_THREADS);
     return;
   }
-  const int2 counts = decide<LONG_THREADS, LONG_HELD, false>(p, w, unit.mass, true, list + 1, p.most_moves);
+  const int2 counts = decide<LONG_THREADS, LONG_HELD>(p, w, unit.mass, true, list + 1, p.most_moves);
   if (threadIdx.x == 0) list[0] = counts;
 }
 __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictParams p) {

@@ -238,8 +238,9 @@ __global__ __launch_bounds__(64 * WAVES, NB == 1 ? 4 : 3) void paged_mass_few_ke
 
 // -------------------------------------------------------------------------------------------------------------------------------- f32
 // Workgroup = (row, kv head, 64 KW positions), a wave to 16 KW of them.  Query rows come straight from memory, 16 at a time, for each wave.
-template <typename T, int D, int KW, bool VEC>
+template <int D, int KW, bool VEC>
 __global__ __launch_bounds__(64 * WAVES) void paged_mass_kernel(MassParams p) {
+  typedef Operand<float, D, VEC> Op;
   const paged_mass_args& a = p.a;
   __shared__ long long s_q[STAGE];   // where a query row lies
   __shared__ __align__(16) int s_x[STAGE];      // its position; -1: it counts nothing
@@ -251,8 +252,8 @@ __global__ __launch_bounds__(64 * WAVES) void paged_mass_kernel(MassParams p) {
   const int kb0 = 16 * KW * WAVES * kblk;
   if (n == 0 || kb0 >= row.L || kb0 + 16 * KW * WAVES <= row.first) return;
   const int kb = kb0 + 16 * KW * wave;
-  Operand<T, D, VEC> key[KW];
-  const unsigned there = load_keys<Operand<T, D, VEC>, T, KW>(p, row, kvh, kb, key);
+  Op key[KW];
+  const unsigned there = load_keys<Op, float, KW>(p, row, kvh, kb, key);
   // ---- the query rows that see some of them, in blocks of 16
   int from = 0, to = M;
   if (!there) to = 0;
@@ -292,15 +293,15 @@ __global__ __launch_bounds__(64 * WAVES) void paged_mass_kernel(MassParams p) {
     const bool all_count = __syncthreads_and(counts || c0 + tid >= M);
     for (int r0 = max(c0, from); r0 < min(c0 + STAGE, to); r0 += 16) {
       const int i0 = r0 - c0, rows = min(16, M - r0);
-      Operand<T, D, VEC> q;
-      q.load((const T*)a.q + s_q[i0 + min(l16, rows - 1)], g, a.head_dim);
+      Op q;
+      q.load((const float*)a.q + s_q[i0 + min(l16, rows - 1)], g, a.head_dim);
       const f32x4 lse = *(const f32x4*)(s_lse + i0 + 4 * g);
       // whether every row sees all of the wave's keys
       const int x0 = Lp + r0 / G, x1 = Lp + (r0 + rows - 1) / G;
       const bool whole = all_count && rows == 16 && there == (1u << KW) - 1 && kb + 16 * KW - 1 <= x0 && (W == 0 || x1 - kb < W);
 #pragma unroll
       for (int kt = 0; kt < KW; ++kt) {
-        f32x4 w = Operand<T, D, VEC>::product(q, key[kt]);
+        f32x4 w = Op::product(q, key[kt]);
 #pragma unroll
         for (int c = 0; c < 4; ++c) w[c] = fast_exp2(fmaf(w[c], p.scale_log2e, -lse[c]));
         if (!whole) {
@@ -552,13 +553,13 @@ __global__ __launch_bounds__(64 * WAVES, 3) void paged_mass_ring_kernel(MassPara
   write_sums<KW>(p, row, kvh, kb, sum);
 }
 
-template <typename T, int D, int KW, bool VEC>
+template <int D, int KW, bool VEC>
 hipError_t launch_k(cascade_ctx* ctx, MassParams& p) {
   constexpr int KEYS = 16 * KW * WAVES;
   p.key_blocks = (p.a.max_seq_len + KEYS - 1) / KEYS;
   const int64_t blocks = (int64_t)p.a.n_rows * p.a.n_kv_heads * p.key_blocks;
   KernelTimer t(ctx, CASCADE_K_MASS);
-  CASCADE_TIMED_LAUNCH(t, (paged_mass_kernel<T, D, KW, VEC>), dim3((unsigned)blocks), dim3(64 * WAVES), 0, ctx->stream, p);
+  CASCADE_TIMED_LAUNCH(t, (paged_mass_kernel<D, KW, VEC>), dim3((unsigned)blocks), dim3(64 * WAVES), 0, ctx->stream, p);
   return hipGetLastError();
 }
 template <auto KERNEL>
@@ -614,8 +615,8 @@ hipError_t launch_bf16(cascade_ctx* ctx, MassParams& p) {
 }
 template <bool VEC>
 hipError_t launch_f32(cascade_ctx* ctx, MassParams& p) {
-  if (p.a.head_dim <= 64) return launch_k<float, 64, 4, VEC>(ctx, p);
-  return p.a.head_dim <= 128 ? launch_k<float, 128, 2, VEC>(ctx, p) : launch_k<float, 256, 1, VEC>(ctx, p);
+  if (p.a.head_dim <= 64) return launch_k<64, 4, VEC>(ctx, p);
+  return p.a.head_dim <= 128 ? launch_k<128, 2, VEC>(ctx, p) : launch_k<256, 1, VEC>(ctx, p);
 }
 
 }  // namespace
