@@ -552,16 +552,18 @@ int paged_attn_workspace(const cascade_ctx* ctx, const paged_attn_args* args, in
  * workspace that a cut could use. */
 int cascade_paged_cut(const cascade_ctx* ctx, const paged_attn_args* args, int32_t* query_rows, int32_t* key_parts, int32_t* waves);
 
-/* paged_attn_shared — paged_attn for rows that have a prefix in common (many images of one prompt, the guidance rows of all of them): out and lse are those of
+/* paged_attn_shared — paged_attn for rows next to each other that have a prefix in common (many images of one prompt): out and lse are those of
  * paged_attn with `attn`, but for rounding.  Rows group_off[g] .. group_off[g+1] - 1 of the batch are group g; the pages of their positions 0 .. shared_len[g] - 1 are
  * the same ones in the same order (each row's table names them).  Those keys and values are read once for the whole group, through the table of
  * its first row, and meet the tokens of all its rows as one product; the rows' other positions and new tokens are taken as paged_attn takes them, and the results are joined.
  * Where a row of the group has fewer positions in its cache than shared_len[g], the group shares as many as that row has; a group of one row, fewer than 64 positions (negative
  * numbers among them) and a row that paged_attn would not compute make the group's rows read everything by themselves.  group_off has to begin with 0, not to
- * decrease, and to end with n_rows; if it does not no group shares anything and the flag is set.
+ * decrease, and to end with n_rows; if it does not no group shares anything and the flag is set.  A group is a run of rows: in a batch that has every prompt's conditional and
+ * unconditional row in turn, as a verification step has, no two rows with a common prefix lie next to each other; a program that wants theirs read once has its calls' rows in another order.
  * Calls that a pass over shared keys would not make faster are paged_attn's own (cascade_paged_shared says which): those with a window, without groups, recorded into a graph
  * without a workspace, with more than 512 rows, more than 16 query rows to a row of the batch and kv head (their products decide, and they are as many either way), or too little
- * to share.  Workspace as for paged_attn: both passes leave partial results there.
+ * to share.  What that is follows from the bounds alone: every row counts as max_prefix_len positions, so one row that is much longer than the others makes all of them read everything
+ * by themselves.  Workspace as for paged_attn: both passes leave partial results there.
  */
 typedef struct {
   paged_attn_args attn;

@@ -1403,7 +1403,7 @@ __global__ __launch_bounds__(64 * NW) void paged_f32_kernel(PagedParams p) {
 // ---------------------------------------------------------------------------------------------- both passes of paged_attn_shared at once
 // The pass over shared keys is products and the trips to memory before and after them, the rows' own is the stream of their keys: in one launch each covers the other's waits.  The
 // first `shared_blocks` workgroups are the former's, one to a compute unit before any gets a second.  64 rows of one token x 32 heads behind 4192 shared keys and 90 to 600 of their own, 8 kv
-// heads: 43 us with the join (51 in a launch each; every row by itself 100; 22 at the rate of a large copy): the chain in front of the first tile, the shared pass's tiles one after the other, the join.
+// heads: 42 us with the join (51 in a launch each; every row by itself 100; 22 at the rate of a large copy): the chain in front of the first tile, the shared pass's tiles one after the other, the join.
 struct BothParams {
   PagedParams p;         // of the rows' own pass
   int shared_parts, shared_blocks;
@@ -1745,12 +1745,14 @@ struct SharedCut {
 // A pass over shared keys costs workgroups that stand beside the rows' own, and the join, 6 to 10 us; it saves reading them once for every row but the first of a group.  Measured on
 // inputs that change from call to call, shared and alone, us (bf16, head_dim 128, one token of 4 query heads to a kv head, unless said; in brackets MB saved, of MB that rows read by themselves):
 //   shares:   16 rows x 2048 keys x 8 kv heads, 4 tokens [126 of 141] 20.9, 23.0;  4 x 4096 x 32, 1 head [201 of 288] 30.7, 36.5;  32 x 512 x 32, 1 head [260 of 302] 26.0, 33.5;
-//             64 rows in 16 groups x 2048 x 8 [403 of 563] 54.8, 66.1;  16 x 2048 x 32, 16 tokens, 1 head [503 of 563] 44.8, 59.8;  64 x 4192 x 8 [1082 of 1255] 44, 100
+//             64 rows in 16 groups x 2048 x 8 [403 of 563] 54.8, 66.1;  16 x 2048 x 32, 16 tokens, 1 head [503 of 563] 44.8, 59.8;  64 x 4192 x 8 [1082 of 1255] 42, 100
 //   does not: 8 x 512 x 32, 1 head [59 of 75] 14.2, 12.5;  64 x 512 x 8 behind 300 of their own [132 of 213] 32.8, 28.7;  behind 1000 [132 of 396] 70.9, 61.8;  64 rows in 32 groups x 2048
 //             x 8 [268 of 563] 80.5, 77.3
 // With more than 16 query rows to a row of the batch the products decide, and they are as many either way: 16 x 2048 x 32, 24 tokens 60, 55; 60 tokens 83, 57; 16 x 2048 x 8, 8 tokens x 4 heads
 // 36, 25.  f32 is bound by products, 16 query rows at a time: 16 rows of one token x 1289 keys x 8 heads of 128 16.6, 28.1; 64 rows 32.7, 84.6, of 8 tokens 64.3, 84.1; but 16 rows of 15 tokens
 // 44.9, 30.3, and 16 rows x 256 keys 13.3, 10.2.
+// The launch knows bounds, not lengths: every row counts as max_prefix_len positions.  64 rows behind 4192 shared keys share beside a row of 8000 keys of
+// its own (70 us; everything alone 193) and do not beside one of 8384 (202).
 SharedCut choose_shared(const paged_shared_args* a, int n_cu, size_t ws_bytes) {
   const paged_attn_args* t = &a->attn;
   SharedCut c = {{FEW, 0, 0}, {FEW, 0, 0}};

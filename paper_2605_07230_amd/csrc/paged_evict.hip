@@ -1,13 +1,15 @@
 // paged_evict kernels for gfx950: rows over their budget give up the positions that gathered the least attention weight, in every layer and kv head their own.
 //
 // Attention over a cache does not ask in which order keys lie, so nothing is compacted: a kept position moves only if it lies behind the places that remain, and it moves into a
-// place that was given up.  With N of L positions left that is at most (L - N) rows of keys and values, whatever N is, where closing the gaps would move nearly all N.  Only the
-// last n_recent positions stay in order, so that the next call finds the newest ones at the end again.
+// place that was given up.  With N of L positions left that is at most L - N of them, whatever N is, where closing the gaps would move nearly all N.  The last n_recent positions stay in
+// order, so that the next call finds the newest ones at the end again: if any position goes, all of these move too.
 //
 // What stays (the N-th largest weight by radix selection, then the lists of places and of positions that go there) is found by every workgroup that shares a unit's moves, with the
 // list in its LDS; only rows of more than 16384 positions take two launches, with lists in memory.  Bound by the moves, scattered keys of 256 bytes, where there are many: 30 layers
 // of 8 rows x 8 kv heads, 1289 to 2356 positions down to 1024 (1.2 GB read and written) 279 us, 4.4 TB/s, of which choosing takes 20; a layer of two rows, 500 positions down to 312,
-// 12 us, one workgroup's chain.
+// 12 us, one workgroup's chain.  Where n_recent is more than what goes, the recent ones are what a call costs: rows of 1024 and a few more down to 1024 with 256 recent, 30 layers of 8 rows x 8
+// kv heads: one more 127 us (at the rate of a large copy 106), 16 more 133 (111), 64 more 149 (129); head_dim 64 79 (54), 84 (57), 92 (66); a layer of two rows x 8 kv heads 13 to 14 (1), x 32
+// heads 18.5 (4).
 #include <algorithm>
 
 #include "common.h"
@@ -283,7 +285,8 @@ __device__ __forceinline__ int2 decide(const EvictParams& p, const RowPlan& w, l
 // Pairs of the first kind bring a kept position to a place that was given up.  Where it stood may be a place of the last n_recent: then the thread that has taken the old
 // key away brings the new one, and no other has anything to do with it.  The second kind are the other places of the last ones.  So nobody waits for anybody.
 // Only if more of the last ones move than positions go (n_recent > L - N), some move onto places of others of them: then the pairs go first, in workgroups that share the
-// 16-byte pieces of all keys, and the last ones follow in runs, each in registers before its places are written; every later run comes from behind those.
+// 16-byte pieces of all keys - whole lines of 128 bytes, so at keys of 128 bytes one workgroup moves all keys of a unit and one all values -, and the last ones follow in runs, each in
+// registers before its places are written; every later run comes from behind those.
 template <int NT>
 __device__ __forceinline__ void move(const EvictParams& p, const RowPlan& w, int layer, int s, int kvh, bool values, int mine, int splits, const int2* list, int cap, int2 counts) {
   const paged_evict_args& a = p.a;

@@ -598,8 +598,11 @@ hipError_t launch_few_k(cascade_ctx* ctx, MassParams& p) {
   p.wave_tiles = tiles >= 8 * ctx->n_cu ? 2 : 1;
   p.key_blocks = (p.a.max_seq_len + 256 * p.wave_tiles - 1) / (256 * p.wave_tiles);
   const dim3 grid((unsigned)((int64_t)p.a.n_rows * p.a.n_kv_heads * p.key_blocks));
-  // Of few rows the workgroups that have keys come one behind the other, the others last (one token of 4 rows of up to 16000 keys 25.6 -> 17.5 us, of 16 of up to 8000 47.7 -> 44.5; paths of 16 rows of
-  // 600 to 2356 keys 43.6 -> 44.2); of many rows the last tiles of all come last (64 of 2145 keys 62.6, row by row 66.4)
+  // Of few rows the workgroups that have keys come one behind the other, the others last; of others the last tiles of all rows come last.  The second way and the first, one token, 8 kv heads of 4,
+  // us: rows of 100 to 16000 keys: 3 rows 14.1, 12.3; 4 19.9, 12.2; 8 41.0, 25.5; 16 66.6, 56.0; of 90 to 4200: 4 9.3, 9.1; 8 11.8, 9.9; 16 21.0, 19.1; all of 2145: 4 8.6, 9.2; 8 11.1, 11.6;
+  // 16 18.3, 19.4 (32 kv heads: of 90 to 4200 8 27.7, 28.1; 16 74.6, 75.4; of 2145 8 33.8, 38.3; 16 64.9, 68.4; paths of 16 rows 45.4, 45.6).  Two rows leave nothing to gain (6.6, 6.9; paths 9.7,
+  // 10.2).  Of 17 to 64 rows it is 5 to 17 % less where they differ (32: 38.8, 32.1; 64: 70.7, 65.6) and 2 to 10 % more where they do not (32: 35.5, 39.2; 64: 62.6, 66.6), as images
+  // that began together: neither is the rule for them, and the search is left out
   const bool dealt = p.a.n_rows > 2 && p.a.n_rows <= 16;
   KernelTimer t(ctx, CASCADE_K_MASS);
   if (dealt) CASCADE_TIMED_LAUNCH(t, (paged_mass_few_kernel<D, NB, true>), grid, dim3(64 * WAVES), 0, ctx->stream, p);

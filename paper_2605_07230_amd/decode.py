@@ -263,7 +263,9 @@ class PagedLoop:
 
     def share(self, group_off, positions) -> None:
         """Rows group_off[g] + 1 .. group_off[g + 1] - 1 (host lists; all rows, in order) get the first positions[g] positions of row group_off[g], in the same pages: whole
-        pages that this row was admitted to.  The others must be empty, and no step or eviction may have been made.  Rows of a group give these pages back together."""
+        pages that this row was admitted to.  The others must be empty, and no step or eviction may have been made.  Rows of a group give these pages back together.
+        Groups are runs of rows: with guidance, whose conditional and unconditional rows alternate, there are none.  Attention reads shared pages once for a group where a call has few
+        tokens to a row (up to 16 query rows to a kv head); chunks and large trees share the memory."""
         ok = (len(group_off) == len(positions) + 1 and group_off[0] == 0 and group_off[-1] == self.rows and all(a <= b for a, b in zip(group_off, group_off[1:])))
         if not ok or self.admitted is None or self.group_off is not None:
             raise ValueError(f"groups of rows {list(group_off)}, {self.rows} rows: once, for all rows in order, before the first step or eviction")
